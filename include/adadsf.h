@@ -499,6 +499,101 @@ int dsf_stack_prefill(const dsf_layer_desc* desc, const dsf_layer_weights* weigh
                       void* const* cache_v, int32_t* cache_len, int cap, float* thr_out,
                       void* workspace, size_t workspace_bytes, hipStream_t stream);
 
+/* ----------------------------------------- paged key/value caches */
+
+/* The caches above reserve cap slots per layer and sequence; how many of them
+ * a layer fills is known only after routing. Here the slots of all sequences
+ * lie in pages of one pool instead, and a call takes any number of new tokens
+ * per sequence (one when decoding, a chunk of a prompt, both in one batch).
+ *
+ * Elements of a pool: those of the call's dtype (type DSF_F32 with DSF_F32,
+ * DSF_BF16 with DSF_BF16), or 8-bit e4m3 codes (type DSF_E4M3, with either
+ * dtype) that share one power of two per slot and kv head:
+ *   value = code * 2^(byte - 127),  byte in k_exp / v_exp.
+ * Writing takes the least power of two that brings the row's largest finite
+ * magnitude to 448 or less (2^-126 at least; an all-zero row has 2^-126) and
+ * rounds to the nearest code, ties to even; infinities become the largest
+ * code, NaN stays NaN. Powers of two leave that rounding the only one: codes
+ * widen to bf16 and fp32 exactly. */
+enum { DSF_E4M3 = 2 };
+
+typedef struct dsf_paged_cache {
+  void* k;               /* [n_pages, n_kv_heads, page_size, head_dim] */
+  void* v;               /* the same */
+  uint8_t* k_exp;        /* DSF_E4M3: [n_pages, n_kv_heads, page_size]; else null */
+  uint8_t* v_exp;
+  int32_t type;          /* DSF_F32, DSF_BF16 or DSF_E4M3 */
+  int32_t n_pages;
+  int32_t n_kv_heads;
+  int32_t page_size;     /* slots per page: 16, 32, 64, 128 or 256 */
+  int32_t head_dim;      /* 32, 64 or 128 */
+  int32_t reserved;      /* must be 0 */
+} dsf_paged_cache;
+
+/* One step's batch. Sequence b brings n_b = row_start[b + 1] - row_start[b]
+ * rows (new tokens), row_start[b] onwards, and has kv_len[b] slots with them:
+ * row i is slot kv_len[b] - n_b + i, in page pages[b][slot / page_size]. Rows
+ * that no sequence has (behind the last one) are neither read nor written. Of
+ * a sequence with more than max_rows rows, those past max_rows are left out.
+ * The arrays are device memory, so a captured step can be replayed with
+ * others: n_rows and max_rows are then upper bounds. row_start ascends within
+ * [0, n_rows]; values outside, lengths outside [0, max_pages * page_size] and
+ * page numbers outside [0, n_pages) are clamped by the kernels (the result is
+ * then unspecified). max_pages * page_size is at most 2^24. */
+typedef struct dsf_paged_batch {
+  const int32_t* row_start; /* [B + 1] */
+  const int32_t* kv_len;    /* [B] */
+  const int32_t* pages;     /* [B, max_pages]; entries past a sequence's last slot are not used */
+  int32_t B;
+  int32_t max_pages;
+  int32_t n_rows;           /* rows of the step's tensors */
+  int32_t max_rows;         /* at least every sequence's rows */
+} dsf_paged_batch;
+
+/* The batch's new keys and values into their slots. k, v: row r, kv head h at
+ * k + r * k_row + h * k_head, head_dim elements of dtype there (strides in
+ * elements, multiples of 8; base 16-byte aligned), so the K and V columns of
+ * the QKV projection's rows, or a decode cache of dsf_stack_prefill, serve as
+ * they are. A row whose slot would be negative (more rows than kv_len) is not
+ * written. Slots are written by one row each unless sequences share the page
+ * they are written to, which is the caller's to avoid. */
+int dsf_paged_cache_write(const dsf_paged_cache* cache, const dsf_paged_batch* batch, int dtype, const void* k,
+                          int64_t k_row, int64_t k_head, const void* v, int64_t v_row, int64_t v_head,
+                          hipStream_t stream);
+
+/* The inverse: the slots of the batch's rows into k and v, widened from codes
+ * where the pool has them (zeros for a negative slot). With n_b = kv_len[b]
+ * that is the whole sequence. */
+int dsf_paged_cache_read(const dsf_paged_cache* cache, const dsf_paged_batch* batch, int dtype, void* k,
+                         int64_t k_row, int64_t k_head, void* v, int64_t v_row, int64_t v_head, hipStream_t stream);
+
+/* Workspace bytes of dsf_paged_attention for a batch of these sizes (B,
+ * n_rows, max_rows, max_pages; the device arrays are not read and may be
+ * null, as may the pool's pointers). 0 on a bad argument. No initialisation
+ * needed; calls that overlap in time, and graphs whose replays may, need
+ * separate workspaces. */
+size_t dsf_paged_attention_workspace_size(const dsf_paged_cache* cache, const dsf_paged_batch* batch, int dtype,
+                                          int Hq);
+
+/* Attention of the batch's rows over their sequences' pages. Row i of
+ * sequence b is slot p = kv_len[b] - n_b + i (its key and value are in the
+ * cache already) and sees the slots j <= p, with window > 0 those of them
+ * with j > p - window:
+ *   out[r, h, :] = sum_j softmax_j(q[r, h] . k_j / sqrt(hd)) v_j
+ * over kv head h / (Hq / Hkv). A row that sees nothing (p < 0) gives zeros.
+ * q, out: row r, head h at q + r * q_row + h * q_head, in dtype (strides as
+ * above; out does not overlap q or the pool). Scores, maximum, sum and
+ * accumulation are fp32. bf16: the probabilities go into the product with v
+ * as bf16 (off by 2^-8 at most each; sequences of up to 64 rows times heads
+ * per kv head have a second part that brings it to 2^-16). What lies in slots a row does not see
+ * has no effect on it, infinite and NaN values included. Work is split over
+ * the slots where rows are few, the shares added in a fixed order: equal
+ * inputs give equal bits; another batch around a sequence may split it
+ * elsewhere and round differently. */
+int dsf_paged_attention(const dsf_paged_cache* cache, const dsf_paged_batch* batch, int dtype, int Hq, const void* q,
+                        int64_t q_row, int64_t q_head, int window, void* out, int64_t out_row, int64_t out_head,
+                        void* workspace, size_t workspace_bytes, hipStream_t stream);
+
 /* ------------------------- alignment objective (Section 3.5, Eqs. 9-11) */
 
 /* Workspace bytes of dsf_align_hidden and dsf_kl_align for n_rows rows (0 on

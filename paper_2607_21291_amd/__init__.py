@@ -12,5 +12,6 @@ from ._binding import (  # noqa: F401
     make_desc, retention_from_similarity, router_backward, router_backward_workspace_size, router_score, scatter_residual, sim_finalize, sim_stats, sim_workspace_size,
     sparse_block_forward, stack_forward, timing_enable, timing_read, topk_select, version, workspace_size,
     workspace_status, WS_STATUS_SK_TIMEOUT, backward_workspace_size, sparse_block_backward, GRAD_FIELDS,
-    LayerGrads,
+    LayerGrads, E4M3, PAGE_SIZES, PagedBatch, PagedCache, paged_attention, paged_attention_workspace_size,
+    paged_cache_read, paged_cache_write,
 )

@@ -7,6 +7,7 @@ kernels. A missing library raises immediately: there is no fallback path.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional, Sequence
@@ -17,6 +18,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libadadsf.so")
 
 F32, BF16 = 0, 1
+E4M3 = 2  # elements of a paged cache only
+PAGE_SIZES = (16, 32, 64, 128, 256)
 BLOCK_NEOX_PARALLEL, BLOCK_QWEN_SEQ = 0, 1
 FLAG_DENSE, FLAG_GATE = 1, 2
 CLIP = {"none": 0, "plain": 1, "budget": 2}
@@ -37,6 +40,7 @@ EXPORTS = [
     "dsf_align_stack_forward", "dsf_decode_workspace_size", "dsf_decode_step", "dsf_stack_prefill",
     "dsf_workspace_status", "dsf_decode_static_scratch_bytes", "dsf_decode_step_static",
     "dsf_backward_workspace_size", "dsf_sparse_block_backward",
+    "dsf_paged_cache_write", "dsf_paged_cache_read", "dsf_paged_attention_workspace_size", "dsf_paged_attention",
 ]
 WS_STATUS_SK_TIMEOUT = 1
 
@@ -64,6 +68,16 @@ GRAD_FIELDS = ["w_qkv", "b_qkv", "w_o", "b_o", "w_up", "b_up", "w_down", "b_down
 
 class LayerGrads(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in GRAD_FIELDS]
+
+
+class _PagedCacheStruct(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_exp", "v_exp")] + \
+        [(n, ctypes.c_int32) for n in ("type", "n_pages", "n_kv_heads", "page_size", "head_dim", "reserved")]
+
+
+class _PagedBatchStruct(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("row_start", "kv_len", "pages")] + \
+        [(n, ctypes.c_int32) for n in ("B", "max_pages", "n_rows", "max_rows")]
 
 
 class LayerWeights(ctypes.Structure):
@@ -119,6 +133,10 @@ def lib() -> ctypes.CDLL:
         "dsf_backward_workspace_size": ([vp, i32, i32, i32, i32], sz),
         "dsf_sparse_block_backward": ([vp, vp, i32, vp, vp, i32, i32, i32, vp, vp, i32, vp, vp, vp, sz, vp], i32),
         "dsf_decode_step_static": ([vp, vp, i32, i32, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, i32, vp], i32),
+        "dsf_paged_cache_write": ([vp, vp, i32, vp, i64, i64, vp, i64, i64, vp], i32),
+        "dsf_paged_cache_read": ([vp, vp, i32, vp, i64, i64, vp, i64, i64, vp], i32),
+        "dsf_paged_attention_workspace_size": ([vp, vp, i32, i32], sz),
+        "dsf_paged_attention": ([vp, vp, i32, i32, vp, i64, i64, i32, vp, i64, i64, vp, sz, vp], i32),
     }
     for name, (args, res) in sig.items():
         fn = getattr(L, name)
@@ -411,6 +429,129 @@ def stack_prefill(desc: LayerDesc, weights: Sequence[LayerWeights], ks: Sequence
                                    ctypes.addressof(karr), _ptr(x), B, T, ctypes.addressof(ck), ctypes.addressof(cv),
                                    _ptr(cache_len), cap, _ptr(thr_out), _ptr(workspace), workspace.numel(),
                                    _stream(stream)))
+
+
+class PagedCache:
+    """Pages of one layer's keys and values: k, v [n_pages, n_kv_heads, page_size, head_dim] of torch.float32,
+    torch.bfloat16 or torch.float8_e4m3fn codes, these with k_exp, v_exp uint8 [n_pages, n_kv_heads, page_size]
+    (a code counts 2^(byte - 127)). Keeps the tensors; the calls take it wherever they take a cache."""
+
+    def __init__(self, k, v, k_exp=None, v_exp=None):
+        types = {torch.float32: F32, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}
+        if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype or k.dtype not in types:
+            raise ValueError("k and v: [n_pages, n_kv_heads, page_size, head_dim], both float32, bfloat16 or float8_e4m3fn")
+        codes = types[k.dtype] == E4M3
+        for t in (k_exp, v_exp):
+            if (t is not None) != codes or (codes and (t.dtype != torch.uint8 or t.shape != k.shape[:3])):
+                raise ValueError("k_exp and v_exp: uint8 [n_pages, n_kv_heads, page_size] for float8_e4m3fn pages, "
+                                 "None for others")
+        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        self.device = _one_device(*(t for t in (k, v, k_exp, v_exp) if t is not None))
+        n_pages, heads, page, hd = k.shape
+        self.n_kv_heads, self.head_dim = heads, hd
+        self._struct = _PagedCacheStruct(_ptr(k), _ptr(v), _ptr(k_exp), _ptr(v_exp), types[k.dtype], n_pages, heads, page,
+                                         hd, 0)
+        self._addr = ctypes.addressof(self._struct)
+
+    @classmethod
+    def empty(cls, n_pages: int, n_kv_heads: int, page_size: int, head_dim: int, dtype, device):
+        """A pool of uninitialised pages (no slot is read before it is written)."""
+        shape = (n_pages, n_kv_heads, page_size, head_dim)
+        k, v = (torch.empty(shape, dtype=dtype, device=device) for _ in range(2))
+        exps = [None, None]
+        if dtype == torch.float8_e4m3fn:
+            exps = [torch.empty(shape[:3], dtype=torch.uint8, device=device) for _ in range(2)]
+        return cls(k, v, *exps)
+
+
+class PagedBatch:
+    """One step's sequences on paged caches: row_start int32 [B + 1], kv_len int32 [B], pages int32 [B, max_pages]
+    on the device, for tensors of n_rows rows; max_rows: at least every sequence's rows. Keeps the tensors, whose
+    values may change between calls (also between replays of a captured one)."""
+
+    def __init__(self, row_start, kv_len, pages, n_rows: int, max_rows: int):
+        B = kv_len.shape[0]
+        if any(t.dtype != torch.int32 for t in (row_start, kv_len, pages)):
+            raise ValueError("row_start, kv_len and pages must be int32")
+        if kv_len.dim() != 1 or row_start.shape != (B + 1,) or pages.dim() != 2 or pages.shape[0] != B:
+            raise ValueError("row_start [B + 1], kv_len [B], pages [B, max_pages]")
+        self.row_start, self.kv_len, self.pages, self.n_rows = row_start, kv_len, pages, n_rows
+        self.device = _one_device(row_start, kv_len, pages)
+        self._struct = _PagedBatchStruct(_ptr(row_start), _ptr(kv_len), _ptr(pages), B, pages.shape[1], n_rows, max_rows)
+        self._addr = ctypes.addressof(self._struct)
+
+
+def _one_device(*tensors):
+    device = tensors[0].device
+    if any(t.device != device for t in tensors):
+        raise ValueError("the tensors lie on different devices")
+    return device
+
+
+def _paged_rows(name: str, t, cache: PagedCache, batch: PagedBatch, heads: Optional[int] = None):
+    """Pointer and strides of rows [n_rows, heads, head_dim] (last dimension contiguous)."""
+    shape = t.shape
+    if len(shape) != 3 or shape[0] != batch.n_rows or shape[2] != cache.head_dim or (heads is not None and shape[1] != heads):
+        raise ValueError(f"{name}: [n_rows, heads, head_dim] = [{batch.n_rows}, {heads or 'heads'}, {cache.head_dim}] "
+                         f"expected, got {list(shape)}")
+    if t.device != cache.device or t.device != batch.device:
+        raise ValueError(f"{name} lies on {t.device}, the cache on {cache.device}, the batch on {batch.device}")
+    row, head, last = t.stride()
+    if last != 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    # strides of dimensions of size one say nothing
+    return t.data_ptr(), row if shape[0] > 1 else 0, head if shape[1] > 1 else 0
+
+
+def _on_device(device, stream, call):
+    """call(stream handle) with `device` current; the stream is the given one or that device's current one."""
+    if device.type != "cuda":
+        raise ValueError(f"the tensors lie on {device}, not on a GPU")
+    if stream is not None and stream.device != device:
+        raise ValueError(f"the stream belongs to {stream.device}, the tensors to {device}")
+    if device.index == torch.cuda.current_device():
+        return call(_stream(stream))
+    with torch.cuda.device(device):
+        return call(_stream(stream))
+
+
+def paged_cache_write(cache: PagedCache, batch: PagedBatch, k, v, stream=None):
+    """k, v [n_rows, n_kv_heads, head_dim] (views of wider rows, too) into the slots of the batch's rows."""
+    kp, vp = _paged_rows("k", k, cache, batch, cache.n_kv_heads), _paged_rows("v", v, cache, batch, cache.n_kv_heads)
+    if v.dtype != k.dtype:
+        raise ValueError("k and v have different dtypes")
+    _check("dsf_paged_cache_write", _on_device(cache.device, stream, lambda s: lib().dsf_paged_cache_write(
+        cache._addr, batch._addr, _dtype_code(k), *kp, *vp, s)))
+
+
+def paged_cache_read(cache: PagedCache, batch: PagedBatch, k, v, stream=None):
+    """The slots of the batch's rows into k, v [n_rows, n_kv_heads, head_dim]; other rows stay as they are."""
+    kp, vp = _paged_rows("k", k, cache, batch, cache.n_kv_heads), _paged_rows("v", v, cache, batch, cache.n_kv_heads)
+    if v.dtype != k.dtype:
+        raise ValueError("k and v have different dtypes")
+    _check("dsf_paged_cache_read", _on_device(cache.device, stream, lambda s: lib().dsf_paged_cache_read(
+        cache._addr, batch._addr, _dtype_code(k), *kp, *vp, s)))
+
+
+def paged_attention_workspace_size(cache: PagedCache, batch: PagedBatch, dtype: int, n_heads: int) -> int:
+    return lib().dsf_paged_attention_workspace_size(cache._addr, batch._addr, dtype, n_heads)
+
+
+def paged_attention(cache: PagedCache, batch: PagedBatch, q, out, window: int = 0, workspace=None, stream=None):
+    """q [n_rows, n_heads, head_dim] over the pages; out the same shape. Rows of no sequence stay as they are."""
+    qp, op = _paged_rows("q", q, cache, batch), _paged_rows("out", out, cache, batch, q.shape[1])
+    if out.dtype != q.dtype:
+        raise ValueError("q and out have different dtypes")
+    dtype = _dtype_code(q)
+    if workspace is None:
+        need = max(paged_attention_workspace_size(cache, batch, dtype, q.shape[1]), 256)
+        # on the stream that uses it, so that its memory is not handed on before that
+        with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    elif workspace.device != cache.device:
+        raise ValueError(f"workspace lies on {workspace.device}, the cache on {cache.device}")
+    _check("dsf_paged_attention", _on_device(cache.device, stream, lambda s: lib().dsf_paged_attention(
+        cache._addr, batch._addr, dtype, q.shape[1], *qp, window, *op, _ptr(workspace), workspace.nbytes, s)))
 
 
 def timing_enable(max_records: int, kinds: Optional[Sequence[str]] = None):

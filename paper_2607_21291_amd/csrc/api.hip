@@ -1326,6 +1326,147 @@ extern "C" int dsf_stack_prefill(const dsf_layer_desc* desc, const dsf_layer_wei
   return DSF_OK;
 }
 
+// ------------------------------------------------------------ paged caches
+
+// The checks that every call on a paged cache shares. device: the pointers
+// too (dsf_paged_attention_workspace_size needs none).
+static int check_paged(const dsf_paged_cache* c, const dsf_paged_batch* b, int dtype, bool device, PagedPool* pool,
+                       PagedBatch* pb) {
+  int rc = check_dtype(dtype);
+  if (rc) return rc;
+  DSF_CHECK(c && b, DSF_EINVAL, "cache and batch must not be null");
+  DSF_CHECK(c->type == DSF_E4M3 || c->type == dtype, DSF_EUNSUPPORTED,
+            "cache type %d with dtype %d: it must be DSF_E4M3 or the dtype", c->type, dtype);
+  DSF_CHECK(c->head_dim == 32 || c->head_dim == 64 || c->head_dim == 128, DSF_EUNSUPPORTED,
+            "head_dim must be 32, 64 or 128");
+  DSF_CHECK(c->page_size == 16 || c->page_size == 32 || c->page_size == 64 || c->page_size == 128 || c->page_size == 256,
+            DSF_EUNSUPPORTED, "page_size must be 16, 32, 64, 128 or 256");
+  DSF_CHECK(c->n_pages > 0 && c->n_kv_heads > 0, DSF_EINVAL, "n_pages and n_kv_heads must be positive");
+  DSF_CHECK(c->n_kv_heads <= 1024, DSF_EUNSUPPORTED, "at most 1024 kv heads");
+  DSF_CHECK(c->reserved == 0, DSF_EINVAL, "reserved must be 0");
+  DSF_CHECK(b->B >= 0 && b->n_rows >= 0 && b->max_rows >= 0, DSF_EINVAL, "B, n_rows and max_rows must be >= 0");
+  DSF_CHECK(b->B <= 65536, DSF_EUNSUPPORTED, "at most 65536 sequences");
+  DSF_CHECK(b->max_pages > 0, DSF_EINVAL, "max_pages must be positive");
+  DSF_CHECK(int64_t(b->max_pages) * c->page_size <= (int64_t(1) << 24), DSF_EUNSUPPORTED,
+            "max_pages * page_size must be at most 2^24");
+  const bool codes = c->type == DSF_E4M3;
+  if (device && b->B > 0 && b->n_rows > 0 && b->max_rows > 0) {
+    DSF_CHECK(c->k && c->v && b->row_start && b->kv_len && b->pages, DSF_EINVAL, "null pointer");
+    DSF_CHECK(codes == (c->k_exp != nullptr) && codes == (c->v_exp != nullptr), DSF_EINVAL,
+              "k_exp and v_exp belong to DSF_E4M3 caches, and only to them");
+    DSF_CHECK(aligned16(c->k) && aligned16(c->v), DSF_EINVAL, "the cache's k and v must be 16-byte aligned");
+    DSF_CHECK(((reinterpret_cast<uintptr_t>(b->row_start) | reinterpret_cast<uintptr_t>(b->kv_len) |
+                reinterpret_cast<uintptr_t>(b->pages)) & 3u) == 0,
+              DSF_EINVAL, "row_start, kv_len and pages must be 4-byte aligned");
+  }
+  int shift = 4;
+  while (1 << shift < c->page_size) ++shift;
+  *pool = PagedPool{c->k, c->v, codes ? c->k_exp : nullptr, codes ? c->v_exp : nullptr, c->n_pages, c->n_kv_heads,
+                    c->head_dim, codes};
+  *pb = PagedBatch{b->row_start, b->kv_len, b->pages, b->B, b->max_pages, b->n_rows, b->max_rows, shift};
+  return DSF_OK;
+}
+
+// Rows of heads at the given strides (elements).
+static int check_paged_rows(const char* name, const void* p, int64_t row, int64_t head, int n_rows, int heads, int hd) {
+  DSF_CHECK(p, DSF_EINVAL, "%s is null", name);
+  DSF_CHECK(aligned16(p), DSF_EINVAL, "%s must be 16-byte aligned", name);
+  DSF_CHECK(row >= 0 && head >= 0 && row % 8 == 0 && head % 8 == 0, DSF_EINVAL,
+            "%s: strides must be non-negative multiples of 8 elements", name);
+  const int64_t most = int64_t(1) << 40;
+  DSF_CHECK(row <= most && head <= most && row * (n_rows - 1) <= most && head * (heads - 1) <= most, DSF_EINVAL,
+            "%s: strides too large", name);
+  return DSF_OK;
+}
+// and written ones: no two heads in one place
+static int check_paged_out(const char* name, int64_t row, int64_t head, int n_rows, int heads, int hd) {
+  DSF_CHECK((heads == 1 || head >= hd) && (n_rows == 1 || row >= hd), DSF_EINVAL, "%s: rows or heads overlap", name);
+  const bool heads_inside = heads == 1 || n_rows == 1 || row >= head * (heads - 1) + hd;
+  const bool rows_inside = heads == 1 || n_rows == 1 || head >= row * (n_rows - 1) + hd;
+  DSF_CHECK(heads_inside || rows_inside, DSF_EINVAL, "%s: rows and heads overlap", name);
+  return DSF_OK;
+}
+
+static int paged_copy(bool write, const dsf_paged_cache* cache, const dsf_paged_batch* batch, int dtype, void* k,
+                      int64_t k_row, int64_t k_head, void* v, int64_t v_row, int64_t v_head, hipStream_t stream) {
+  PagedPool pool;
+  PagedBatch pb;
+  int rc = check_paged(cache, batch, dtype, true, &pool, &pb);
+  if (rc) return rc;
+  DSF_CHECK(int64_t(pb.n_rows) * pool.Hkv < (int64_t(1) << 31), DSF_EINVAL, "problem too large");
+  if (pb.B == 0 || pb.n_rows == 0 || pb.max_rows == 0) return DSF_OK;
+  if ((rc = check_paged_rows("k", k, k_row, k_head, pb.n_rows, pool.Hkv, pool.hd))) return rc;
+  if ((rc = check_paged_rows("v", v, v_row, v_head, pb.n_rows, pool.Hkv, pool.hd))) return rc;
+  if (!write) {
+    if ((rc = check_paged_out("k", k_row, k_head, pb.n_rows, pool.Hkv, pool.hd))) return rc;
+    if ((rc = check_paged_out("v", v_row, v_head, pb.n_rows, pool.Hkv, pool.hd))) return rc;
+  }
+  rc = check_device();
+  if (rc) return rc;
+  DSF_HIP(launch_paged_copy(dtype, write, pool, pb, k, k_row, k_head, v, v_row, v_head, stream));
+  return DSF_OK;
+}
+
+extern "C" int dsf_paged_cache_write(const dsf_paged_cache* cache, const dsf_paged_batch* batch, int dtype,
+                                     const void* k, int64_t k_row, int64_t k_head, const void* v, int64_t v_row,
+                                     int64_t v_head, hipStream_t stream) {
+  return paged_copy(true, cache, batch, dtype, const_cast<void*>(k), k_row, k_head, const_cast<void*>(v), v_row, v_head,
+                    stream);
+}
+
+extern "C" int dsf_paged_cache_read(const dsf_paged_cache* cache, const dsf_paged_batch* batch, int dtype, void* k,
+                                    int64_t k_row, int64_t k_head, void* v, int64_t v_row, int64_t v_head,
+                                    hipStream_t stream) {
+  return paged_copy(false, cache, batch, dtype, k, k_row, k_head, v, v_row, v_head, stream);
+}
+
+static int check_paged_heads(int Hq, const PagedPool& pool, const PagedBatch& pb) {
+  DSF_CHECK(Hq > 0 && Hq % pool.Hkv == 0, DSF_EINVAL, "need Hq %% Hkv == 0");
+  DSF_CHECK(int64_t(pb.n_rows) * Hq < (int64_t(1) << 27), DSF_EINVAL, "problem too large: n_rows * Hq must be below 2^27");
+  return DSF_OK;
+}
+
+extern "C" size_t dsf_paged_attention_workspace_size(const dsf_paged_cache* cache, const dsf_paged_batch* batch,
+                                                     int dtype, int Hq) {
+  PagedPool pool;
+  PagedBatch pb;
+  if (check_paged(cache, batch, dtype, false, &pool, &pb) || check_paged_heads(Hq, pool, pb)) return 0;
+  return paged_attention_workspace_bytes(dtype, Hq, pool, pb);
+}
+
+extern "C" int dsf_paged_attention(const dsf_paged_cache* cache, const dsf_paged_batch* batch, int dtype, int Hq,
+                                   const void* q, int64_t q_row, int64_t q_head, int window, void* out, int64_t out_row,
+                                   int64_t out_head, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  PagedAttnArgs a;
+  int rc = check_paged(cache, batch, dtype, true, &a.pool, &a.pb);
+  if (rc) return rc;
+  if ((rc = check_paged_heads(Hq, a.pool, a.pb))) return rc;
+  DSF_CHECK(window >= 0, DSF_EINVAL, "window must be >= 0");
+  if (a.pb.B == 0 || a.pb.n_rows == 0 || a.pb.max_rows == 0) return DSF_OK;
+  if ((rc = check_paged_rows("q", q, q_row, q_head, a.pb.n_rows, Hq, a.pool.hd))) return rc;
+  if ((rc = check_paged_rows("out", out, out_row, out_head, a.pb.n_rows, Hq, a.pool.hd))) return rc;
+  if ((rc = check_paged_out("out", out_row, out_head, a.pb.n_rows, Hq, a.pool.hd))) return rc;
+  DSF_CHECK(workspace, DSF_EINVAL, "workspace is null");
+  DSF_CHECK((reinterpret_cast<uintptr_t>(workspace) & 255u) == 0, DSF_EINVAL, "workspace must be 256-byte aligned");
+  const size_t need = paged_attention_workspace_bytes(dtype, Hq, a.pool, a.pb);
+  DSF_CHECK(workspace_bytes >= need, DSF_EWORKSPACE, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
+  rc = check_device();
+  if (rc) return rc;
+  a.dtype = dtype;
+  a.Hq = Hq;
+  // a window past the longest sequence hides nothing
+  a.window = window >= a.pb.max_pages << a.pb.page_shift ? 0 : window;
+  a.q = q;
+  a.q_row = q_row;
+  a.q_head = q_head;
+  a.out = out;
+  a.o_row = out_row;
+  a.o_head = out_head;
+  a.workspace = workspace;
+  DSF_HIP(launch_paged_attention(a, stream));
+  return DSF_OK;
+}
+
 // ------------------------------------------- alignment objective (Sec. 3.5)
 
 extern "C" size_t dsf_align_workspace_size(int64_t n_rows) {

@@ -325,4 +325,35 @@ hipError_t launch_kv_fill(int dtype, const void* ks, const void* vs, void* ck, v
 hipError_t launch_kept_min_score(const float* scores, const int32_t* idx, int B, int T, int k, float* thr,
                                  hipStream_t s);
 
+
+// ---- paged caches (kernels_paged.hip, kernels_pagedattn.hip) ----
+// Pages [n_pages, Hkv, page, hd] of keys and values; ke, ve: exponent bytes
+// [n_pages, Hkv, page] where `codes` (else elements of the call's dtype).
+struct PagedPool {
+  void* k; void* v;
+  uint8_t* ke; uint8_t* ve;
+  int n_pages, Hkv, hd;
+  bool codes;
+};
+struct PagedBatch {
+  const int32_t* row_start;  // [B + 1]
+  const int32_t* kv_len;     // [B]
+  const int32_t* pages;      // [B, max_pages]
+  int B, max_pages, n_rows, max_rows;
+  int page_shift;  // log2 of the page's slots
+};
+// k, v: rows [n_rows, Hkv, hd] at the given row and head strides (elements)
+hipError_t launch_paged_copy(int dtype, bool write, const PagedPool& pool, const PagedBatch& pb, void* k, int64_t k_row,
+                             int64_t k_head, void* v, int64_t v_row, int64_t v_head, hipStream_t s);
+struct PagedAttnArgs {
+  int dtype, Hq, window;
+  PagedPool pool;
+  PagedBatch pb;
+  const void* q; int64_t q_row, q_head;
+  void* out; int64_t o_row, o_head;
+  void* workspace;
+};
+size_t paged_attention_workspace_bytes(int dtype, int Hq, const PagedPool& pool, const PagedBatch& pb);
+hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t s);
+
 }  // namespace dsf
