@@ -2,12 +2,16 @@
 //
 // The query heads of a kv head and a sequence's new tokens are the rows of
 // one problem, token-major (row m = token * G + head), so that a tile of rows
-// reads a key or value once for all of them. Rows are cut into tiles of BM,
-// a sequence's slots into splits of equal length where there are too few
-// tiles for the chip (paged_item); a workgroup takes one (tile, split, kv
-// head), keeps the running maximum and sum of the softmax in fp32, and writes
-// the result, or its share of it, which paged_join_kernel adds up in the order of the splits.
+// reads a key or value once for all of them. A workgroup keeps the running
+// maximum and sum of the softmax of a tile's rows in fp32. Where there are
+// too few tiles for the chip the slots are divided too, by rules that every
+// workgroup works out for itself from the sequences' lengths on the device
+// (the host knows only bounds): chunks of tokens and fp32 in splits of equal
+// length (paged_item), sequences of few rows in equal shares of all the slots
+// (paged_flat). The shares of a tile go to the workspace and
+// paged_join_kernel adds them up in their order.
 #include <algorithm>
+#include <type_traits>
 
 #include "paged.h"
 
@@ -24,6 +28,7 @@ struct PagedKernelArgs {
   int items;       // per kv head: the grid's, and no more than that have a place in part_o
   int target;      // of them to cut the work into (0: no splits)
   int split_min;   // least blocks of 64 slots per split
+  int unit_shift;  // paged_flat: log2 of the slots per unit
   float* part_o;   // [item][kv head][BM][HD]
   float2* part_ml; // [item][kv head][BM]: maximum (log2 units), sum
 };
@@ -63,7 +68,13 @@ __device__ __forceinline__ PagedShape paged_shape(const PagedKernelArgs& a, int 
   w.blocks = (max(s.kv - w.lo, 0) + 63) >> 6;
   return w;
 }
+// Lane l's shape, in every lane.
+__device__ __forceinline__ PagedShape shape_of(const PagedShape& w, int l) {
+  auto at = [l](int v) { return __builtin_amdgcn_readlane(v, l); };
+  return PagedShape{at(w.n), at(w.row0), at(w.kv), at(w.M), at(w.tiles), at(w.lo), at(w.blocks)};
+}
 struct PagedItem {
+  PagedShape w;
   int b;       // -1: none
   int first;   // the sequence's first item
   int local;   // this one's number among them
@@ -93,7 +104,8 @@ __device__ __forceinline__ PagedItem paged_item(const PagedKernelArgs& a, int it
   PagedShape w = {};
   if (lane < a.pb.B) w = paged_shape(a, lane);
   const int per = paged_split_blocks(a, w, lane);
-  PagedItem it = {-1, 0, 0, 0, 0};
+  PagedItem it = {};
+  it.b = -1;
   int first = 0;
   for (int b0 = 0; b0 < a.pb.B; b0 += 64) {
     if (b0) {
@@ -110,11 +122,87 @@ __device__ __forceinline__ PagedItem paged_item(const PagedKernelArgs& a, int it
       it.local = item - it.first;
       it.len = per << 6;
       it.splits = __builtin_amdgcn_readlane(splits, l);
+      it.w = shape_of(w, l);
       return it;
     }
     first += __builtin_amdgcn_readlane(end, 63);
   }
   return it;
+}
+
+// Sequences of few rows: the slots of all tiles, in units of 64 (more where
+// their number could pass 2^30), as one line that a kv head's workgroups
+// share evenly. Workgroup j has the units from start(j) to start(j + 1), so
+// at most its first and its last tile are shared with others; it leaves the
+// share of a tile that began before it at place 2 j, of one that goes on
+// behind it at place 2 j + 1. Short work is not cut up: with tiles for
+// everybody, none longer than kWholeUnits, each workgroup has whole tiles.
+constexpr int kWholeUnits = 16;  // 1024 slots
+constexpr int kLeastUnits = 4;   // of a share
+struct PagedFlat {
+  int wgs;    // with work
+  int q, r;   // units each, and one more for the first r
+  bool whole; // workgroup j has tile j
+  __device__ __forceinline__ int start(int j) const { return j * q + min(j, r); }
+  __device__ __forceinline__ int of(int u) const { return u < r * (q + 1) ? u / (q + 1) : r + (u - r * (q + 1)) / q; }
+};
+__device__ __forceinline__ int paged_units(const PagedKernelArgs& a, const PagedShape& w) {  // of a tile
+  return max((max(w.kv - w.lo, 0) + (1 << a.unit_shift) - 1) >> a.unit_shift, 1);
+}
+__device__ __forceinline__ int wave_most(int v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = max(v, __shfl_xor(v, o, 64));
+  return v;
+}
+__device__ __forceinline__ PagedFlat paged_flat(const PagedKernelArgs& a, const PagedShape& w, int lane) {
+  int units = w.tiles ? w.tiles * paged_units(a, w) : 0, tiles = w.tiles, most = w.tiles ? paged_units(a, w) : 0;
+  for (int b0 = 64; b0 < a.pb.B; b0 += 64) {
+    if (b0 + lane < a.pb.B) {
+      const PagedShape x = paged_shape(a, b0 + lane);
+      if (x.tiles) {
+        const int n = paged_units(a, x);
+        units += x.tiles * n;
+        tiles += x.tiles;
+        most = max(most, n);
+      }
+    }
+  }
+  units = __builtin_amdgcn_readlane(wave_prefix(units), 63);
+  tiles = __builtin_amdgcn_readlane(wave_prefix(tiles), 63);
+  most = __builtin_amdgcn_readfirstlane(wave_most(most));
+  PagedFlat f;
+  f.whole = most << a.unit_shift <= kWholeUnits << 6 && tiles <= a.items;
+  f.wgs = f.whole ? tiles : min(max(units / kLeastUnits, 1), a.items);
+  if (units == 0) f.wgs = 0;
+  f.q = f.wgs ? units / f.wgs : 0;
+  f.r = units - f.q * f.wgs;
+  return f;
+}
+// The sequence and tile of position `pos`, a unit or (whole) a tile.
+struct PagedSpot {
+  PagedShape w;
+  int b;           // -1: none
+  int tile;        // of the sequence
+  int from, until; // units (whole: tiles) that the tile spans, on the line
+};
+__device__ __forceinline__ PagedSpot paged_spot(const PagedKernelArgs& a, PagedShape w, bool whole, int pos, int lane) {
+  int base = 0;
+  for (int b0 = 0; b0 < a.pb.B; b0 += 64) {
+    if (b0) {
+      w = PagedShape{};
+      if (b0 + lane < a.pb.B) w = paged_shape(a, b0 + lane);
+    }
+    const int each = whole ? 1 : paged_units(a, w), c = w.tiles * each, end = wave_prefix(c);
+    const uint64_t over = __builtin_amdgcn_ballot_w64(base + end > pos);
+    if (over) {
+      const int l = __builtin_ctzll(over), n = __builtin_amdgcn_readlane(each, l);
+      const int first = base + __builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(c, l);
+      const int t = (pos - first) / n;
+      return PagedSpot{shape_of(w, l), b0 + l, t, first + t * n, first + t * n + n};
+    }
+    base += __builtin_amdgcn_readlane(end, 63);
+  }
+  return PagedSpot{PagedShape{}, -1, 0, 0, 0};
 }
 
 // One item's tile and slots. Splits outermost: the tiles of one split read
@@ -139,7 +227,7 @@ __device__ __forceinline__ void paged_range(const PagedKernelArgs& a, const Page
 }
 __device__ __forceinline__ PagedWork paged_work(const PagedKernelArgs& a, const PagedItem& it) {
   PagedWork k;
-  const PagedShape w = paged_shape(a, it.b);
+  const PagedShape& w = it.w;
   k.b = it.b;
   k.n = w.n;
   k.row0 = w.row0;
@@ -168,10 +256,20 @@ struct PagedTable {
   }
 };
 
+// LDS transpose load: within each 16-lane group G, lane 16 G + 4 a + b
+// receives element b of the 8-byte rows addressed by lanes 16 G + a + 4 j,
+// j = 0..3.
+__device__ __forceinline__ bf16x4 lds_read_tr(const char* p) {
+  typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
+  return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(__attribute__((address_space(3))) const char*)p);
+}
+
 // Maximum and sum over a lane and the lane 32 beside it.
 __device__ __forceinline__ float pair32_max(float v) {
   auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  float r;  // (fmaxf would first quiet what it cannot see to be a number already)
+  asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a[0]), "v"(a[1]));
+  return r;
 }
 __device__ __forceinline__ float pair32_sum(float v) {
   auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -195,6 +293,8 @@ struct SlotTile {
   }
 };
 
+#define DSF_INLINE __attribute__((always_inline))  // for lambdas over register arrays
+
 // 16 slots from `slot` on of one kv head to LDS at `lds` (a tile's row 16 i):
 // bf16 by DMA, each lane 16 bytes at a time; slots at or past `end` become
 // zeros. All 16 lie in one page.
@@ -205,15 +305,23 @@ struct DmaSlots {
     using S = SlotTile<HD>;
     const int mask = (1 << a.pb.page_shift) - 1;
     const int64_t row = ((int64_t(page) * a.pool.Hkv + kvh) << a.pb.page_shift) + (slot & mask);
-    const int bytes = min(max(end - slot, 0), 16) * S::kRowBytes;
-    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<char*>(static_cast<const char*>(pool)) + row * S::kRowBytes, (short)0, bytes, 0x00020000);
+    const uint64_t base = reinterpret_cast<uint64_t>(pool) + row * S::kRowBytes;
+    // buffer resource: base, no stride, the bytes of the slots that count, raw 32-bit format
+    auto uniform = [](uint32_t x) { return uint32_t(__builtin_amdgcn_readfirstlane(int(x))); };
+    const u32x4 rsrc = {uniform(uint32_t(base)), uniform(uint32_t(base >> 32) & 0xffffu),
+                        uniform(uint32_t(min(max(end - slot, 0), 16) * S::kRowBytes)), 0x00020000u};
+    const uint32_t at = uniform(uint32_t(size_t((__attribute__((address_space(3))) char*)lds)));
 #pragma unroll
     for (int e = 0; e < 16 * S::kRowBytes / 1024; ++e) {
       const int byte = 1024 * e + 16 * lane;
       const int r = byte / S::kRowBytes, c = byte % S::kRowBytes / 16;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(lds + 1024 * e), 16,
-                                               r * S::kRowBytes + ((c ^ S::swz(r)) << 4), 0, 0, 0);
+      asm volatile(
+          "s_mov_b32 m0, %0\n\t"
+          "s_nop 0\n\t"
+          "buffer_load_dwordx4 %1, %2, 0 offen lds"
+          :
+          : "s"(at + 1024 * e), "v"(r * S::kRowBytes + ((c ^ S::swz(r)) << 4)), "s"(rsrc)
+          : "memory");
     }
   }
 };
@@ -225,7 +333,7 @@ struct CodeSlots {
   static constexpr int kCpr = HD / 16;                       // 16-byte loads per slot
   static constexpr int kLoads = kCpr >= 4 ? 16 * kCpr / 64 : 1;
   u32x4 c[kLoads];
-  uint32_t e[kLoads];
+  uint32_t e;  // exponent byte of slot lane & 15
   __device__ __forceinline__ void load(const void* pool, const uint8_t* exps, const PagedKernelArgs& a, int page, int kvh,
                                        int slot, int end, int lane) {
     const int mask = (1 << a.pb.page_shift) - 1;
@@ -236,17 +344,16 @@ struct CodeSlots {
         const_cast<char*>(static_cast<const char*>(pool)) + row * HD, (short)0, rows * HD, 0x00020000);
     const auto re = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(exps) + row, (short)0, rows, 0x00020000);
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
+    for (int i = 0; i < kLoads; ++i)
       c[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rc, 1024 * i + 16 * lane, 0, 0));
-      e[i] = __builtin_amdgcn_raw_buffer_load_b8(re, 64 / kCpr * i + lane / kCpr, 0, 0);
-    }
+    e = __builtin_amdgcn_raw_buffer_load_b8(re, lane & 15, 0, 0);
   }
   __device__ __forceinline__ void store(char* lds, int lane) const {
     using S = SlotTile<HD>;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int r = 64 / kCpr * i + lane / kCpr, ch = 2 * (lane % kCpr);
-      const float s = paged_scale(e[i]);
+      const float s = paged_scale(__builtin_amdgcn_ds_bpermute((r & 15) << 2, int(e)));
       if (r < 16) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -299,43 +406,40 @@ __device__ __forceinline__ float not_finite_sum(float c) {
 
 // ---------------------------------------------------------- chunks of tokens
 
-// Eight transpose loads: for four steps of 16 slots (two of `steps` 16-slot
-// halves each) the V^T operand of v_mfma_f32_32x32x16_bf16 for 32 dims. Issue
-// and wait in one statement; the DMA in flight fills the other stage.
-template <int ROW>
-__device__ __forceinline__ void lds_read_tr8(uint32_t addr0, uint32_t addr1, u32x2 (&v)[8]) {
-  asm volatile(
-      "ds_read_b64_tr_b16 %0, %8\n\t"
-      "ds_read_b64_tr_b16 %1, %9\n\t"
-      "ds_read_b64_tr_b16 %2, %8 offset:%10\n\t"
-      "ds_read_b64_tr_b16 %3, %9 offset:%10\n\t"
-      "ds_read_b64_tr_b16 %4, %8 offset:%11\n\t"
-      "ds_read_b64_tr_b16 %5, %9 offset:%11\n\t"
-      "ds_read_b64_tr_b16 %6, %8 offset:%12\n\t"
-      "ds_read_b64_tr_b16 %7, %9 offset:%12\n\t"
-      "s_waitcnt lgkmcnt(0)"
-      : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]), "=&v"(v[6]), "=&v"(v[7])
-      : "v"(addr0), "v"(addr1), "n"(16 * ROW), "n"(32 * ROW), "n"(48 * ROW)
-      : "memory");
-}
-
-// A workgroup of four waves takes 128 NQ rows, a wave 32 NQ of them, and 64
-// slots at a time, staged by all four (two stages).
+// A workgroup of four waves takes 128 rows, a wave 32 of them, and 64 slots
+// at a time, staged by all four.
 //
 // S^T = K Q^T with v_mfma_f32_32x32x16_bf16: lane (r32, hi) holds of row r32
-// the scores of slots 32 kb + 8 (i / 4) + 4 hi + i % 4, i < 16, so a row's
+// the scores of slots 8 (i / 4) + 4 hi + i % 4 of 32, i < 16, so a row's
 // maximum needs one exchange between two lanes, and its probabilities lie as
 // the B operand of O^T += V^T P^T wants them if the product takes the slots
 // in that order: step s covers 16 slots, element j of lane (., hi) being slot
 // 16 s + 4 hi + j % 4 + 8 (j / 4). Probabilities are rounded to bf16 for that
 // product (off by 2^-8 at most each, and the row's sum is of the rounded
-// ones); maximum, sum and accumulators are fp32.
-template <int HD, bool E8, int NQ>
-__global__ __launch_bounds__(256) void paged_chunk_kernel(PagedKernelArgs a) {
+// ones); maximum, sum and accumulators are fp32. The maximum a row is scaled
+// by follows the true one at a distance: it moves when a tile's is over 2^8
+// times it, so weights stay below 2^8 and the accumulators are rarely
+// rescaled.
+//
+// The matrix cores and the vector units of a SIMD overlap only within a wave
+// (a probe: 4 FMAs and an exponential beside each 32 x 32 MFMA cost nothing),
+// so each half turn, of 32 slots, does three things that do not depend on
+// each other: the scores of half u + 1, the softmax of half u and the product
+// of half u - 1 with its values. Turn t has the product of tile t's two halves
+// and the scores of tile t + 1's, so of keys and of values one tile each is
+// in use and one on its way. Turns with hidden slots and the last run in a
+// general form of the same.
+//
+// DMA into LDS is issued in inline assembly: the compiler, which cannot tell
+// the stages apart, would wait for it before every transpose load.
+template <int HD, bool E8>
+__global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedKernelArgs a) {
   using S = SlotTile<HD>;
-  constexpr int BM = 128 * NQ, NS = HD / 16, ND = HD / 32;
-  constexpr int kTile = 64 * S::kRowBytes, kStage = 2 * kTile;
-  __shared__ __attribute__((aligned(16))) char smem[2 * kStage];
+  constexpr int BM = 128, NS = HD / 16, ND = HD / 32;
+  constexpr int kTile = 64 * S::kRowBytes;
+  constexpr float kLag = 8.f;           // log2 units
+  constexpr float kNothing = -3.0e38f;  // the maximum of nothing: finite, so that -inf less it is -inf
+  __shared__ __attribute__((aligned(16))) char smem[4 * kTile];  // K 0, K 1, V 0, V 1
   const int tid = threadIdx.x, lane = tid & 63, r32 = lane & 31, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // kv head innermost: consecutive workgroups go to different XCDs, so that
@@ -347,251 +451,414 @@ __global__ __launch_bounds__(256) void paged_chunk_kernel(PagedKernelArgs a) {
   if (w.splits > 1 && w.begin >= w.end) return;  // a split that none of the tile's rows sees
 
   // this wave's rows: row m of the sequence, its token's slot
-  int slot_of[NQ];
-  bool live[NQ];
-  bf16x8 qf[NQ][NS];
-  const int m0 = w.tile * BM + wave * 32 * NQ;
+  const int m0 = w.tile * BM + wave * 32, m = m0 + r32, mc = min(m, w.M - 1);
+  const int tok = mc / a.G, g = mc - tok * a.G, my_slot = w.p0 + tok;
+  bf16x8 qf[NS];
+  {
+    const uint16_t* qp =
+        static_cast<const uint16_t*>(a.q) + int64_t(w.row0 + tok) * a.q_row + int64_t(kvh * a.G + g) * a.q_head;
 #pragma unroll
-  for (int qi = 0; qi < NQ; ++qi) {
-    const int m = m0 + 32 * qi + r32, mc = min(m, w.M - 1);
-    const int tok = mc / a.G, g = mc - tok * a.G;
-    live[qi] = m < w.M;
-    slot_of[qi] = w.p0 + tok;
-    const uint16_t* qp = static_cast<const uint16_t*>(a.q) + int64_t(w.row0 + tok) * a.q_row + int64_t(kvh * a.G + g) * a.q_head;
-#pragma unroll
-    for (int s = 0; s < NS; ++s) qf[qi][s] = *reinterpret_cast<const bf16x8*>(qp + 16 * s + 8 * hi);
+    for (int s = 0; s < NS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qp + 16 * s + 8 * hi);
   }
   // slots that every row of the wave sees: [see_lo, see_hi)
-  const int see_hi = w.p0 + min(m0, w.M - 1) / a.G + 1;
-  const int see_lo = a.window ? w.p0 + min(m0 + 32 * NQ - 1, w.M - 1) / a.G - a.window + 1 : 0;
-  // and that some row sees
-  const int any_hi = m0 < w.M ? w.p0 + min(m0 + 32 * NQ - 1, w.M - 1) / a.G + 1 : 0;
+  const int see_hi = min(w.p0 + min(m0, w.M - 1) / a.G + 1, w.end);
+  const int see_lo = a.window ? w.p0 + min(m0 + 31, w.M - 1) / a.G - a.window + 1 : 0;
 
-  f32x16 o[NQ][ND];
-  float m_run[NQ], l_run[NQ];
-#pragma unroll
-  for (int qi = 0; qi < NQ; ++qi) {
-    m_run[qi] = -INFINITY;
-    l_run[qi] = 0.f;
-#pragma unroll
-    for (int db = 0; db < ND; ++db)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[qi][db][i] = 0.f;
-  }
   const float sc = 1.4426950408889634f / sqrtf(float(HD));  // log2(e) / sqrt(hd)
+  f32x16 o[ND];
+  float m_run = kNothing, l_run = 0.f;
+#pragma unroll
+  for (int db = 0; db < ND; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
 
   // staging: this wave brings slots 16 wave .. + 15 of every tile
+  const int nt = (w.end - w.begin + 63) >> 6, s0 = w.begin + 16 * wave;
   PagedTable tab;
-  const int ntiles = (w.end - w.begin + 63) >> 6;
-  CodeSlots<HD> kc, vc;
-  const int s0 = w.begin + 16 * wave;
   tab.load(a, w.b, w.begin >> a.pb.page_shift, lane);
-  auto fetch = [&](int t) {
-    const int slot = s0 + 64 * t;
-    const int page = tab.at(a, w.b, slot >> a.pb.page_shift, lane);
-    char* st = smem + (t & 1) * kStage + 16 * wave * S::kRowBytes;
-    if constexpr (E8) {
-      kc.load(a.pool.k, a.pool.ke, a, page, kvh, slot, w.end, lane);
-      vc.load(a.pool.v, a.pool.ve, a, page, kvh, slot, w.end, lane);
-    } else {
-      DmaSlots<HD>::load(a.pool.k, a, page, kvh, slot, w.end, st, lane);
-      DmaSlots<HD>::load(a.pool.v, a, page, kvh, slot, w.end, st + kTile, lane);
-    }
+  PagedTable vtab = tab;  // values are a tile behind
+  CodeSlots<HD> codes;
+  char* const mine = smem + 16 * wave * S::kRowBytes;
+  auto fetch_k = [&](int t) DSF_INLINE {
+    const int slot = s0 + 64 * t, page = tab.at(a, w.b, slot >> a.pb.page_shift, lane);
+    if constexpr (E8) codes.load(a.pool.k, a.pool.ke, a, page, kvh, slot, w.end, lane);
+    else DmaSlots<HD>::load(a.pool.k, a, page, kvh, slot, w.end, mine + (t & 1) * kTile, lane);
   };
-  auto settle = [&](int t) {  // e4m3: the fetched codes into their stage
-    if constexpr (E8) {
-      char* st = smem + (t & 1) * kStage + 16 * wave * S::kRowBytes;
-      kc.store(st, lane);
-      vc.store(st + kTile, lane);
-    }
+  auto fetch_v = [&](int t) DSF_INLINE {
+    const int slot = s0 + 64 * t, page = vtab.at(a, w.b, slot >> a.pb.page_shift, lane);
+    if constexpr (E8) codes.load(a.pool.v, a.pool.ve, a, page, kvh, slot, w.end, lane);
+    else DmaSlots<HD>::load(a.pool.v, a, page, kvh, slot, w.end, mine + (2 + (t & 1)) * kTile, lane);
   };
-
-  // V^T reads: lane (group of 16 G, a4 = lane & 3, j = lane / 4 & 3) addresses slot 4 hi + j at dims 16 (G & 1) + 4 a4
-  const int tj = (lane >> 2) & 3, vrow = 4 * hi + tj;
-  const int vch = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), vbyte = (lane & 1) * 8;
-
-  auto tile = [&](int t) {
-    const int kb0 = w.begin + 64 * t;
-    const char* Ks = smem + (t & 1) * kStage;
-    const char* Vs = Ks + kTile;
-    if (kb0 >= any_hi) return;  // in the future of every row of this wave
-    f32x16 s[NQ][2];
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      const int row = 32 * kb + r32;
-#pragma unroll
-      for (int qi = 0; qi < NQ; ++qi)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[qi][kb][i] = 0.f;
-#pragma unroll
-      for (int st = 0; st < NS; ++st) {
-        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(Ks + row * S::kRowBytes + (((2 * st + hi) ^ S::swz(row)) << 4));
-#pragma unroll
-        for (int qi = 0; qi < NQ; ++qi)
-          s[qi][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[qi][st], s[qi][kb], 0, 0, 0);
-      }
-    }
-    const bool masked = kb0 + 64 > min(see_hi, w.end) || kb0 < see_lo;  // wave-uniform
-    bf16x8 pb[NQ][4];
-#pragma unroll
-    for (int qi = 0; qi < NQ; ++qi) {
-      if (masked) {
-        // slot kb0 + x is seen iff lo <= x <= top
-        const int top = min(slot_of[qi], w.end - 1) - kb0 - 4 * hi;
-        const int lo = a.window ? slot_of[qi] - a.window + 1 - kb0 - 4 * hi : -64;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int x = 32 * kb + 8 * (i / 4) + i % 4;
-            s[qi][kb][i] = x > top || x < lo ? -INFINITY : s[qi][kb][i];
-          }
-      }
-      float mx = -INFINITY;
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[qi][kb][i]);
-      const float m_new = fmaxf(m_run[qi], pair32_max(mx) * sc);
-      const float base = m_new == -INFINITY ? 0.f : m_new;
-      if (__builtin_amdgcn_ballot_w64(m_new != m_run[qi])) {
-        const float alpha = __builtin_amdgcn_exp2f(m_run[qi] - base);
-        l_run[qi] *= alpha;
-#pragma unroll
-        for (int db = 0; db < ND; ++db) o[qi][db] *= alpha;
-      }
-      m_run[qi] = m_new;
-#pragma unroll
-      for (int st = 0; st < 4; ++st)
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          pb[qi][st][j] = (__bf16)__builtin_amdgcn_exp2f(fmaf(s[qi][st / 2][8 * (st & 1) + j], sc, -base));
-      float sum = l_run[qi];
-#pragma unroll
-      for (int st = 0; st < 4; ++st)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-          const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f}, p2 = {pb[qi][st][2 * j], pb[qi][st][2 * j + 1]};
-          sum = __builtin_amdgcn_fdot2_f32_bf16(p2, one, sum, false);
-        }
-      l_run[qi] = sum;
-    }
-    const uint32_t vs = uint32_t(size_t((__attribute__((address_space(3))) const char*)Vs)) + vrow * S::kRowBytes + vbyte;
-#pragma unroll
-    for (int db = 0; db < ND; ++db) {
-      u32x2 v[8];
-      lds_read_tr8<S::kRowBytes>(vs + (((4 * db + vch) ^ S::swz(vrow)) << 4),
-                                 vs + 8 * S::kRowBytes + (((4 * db + vch) ^ S::swz(vrow + 8)) << 4), v);
-      bf16x8 vf[4];
-#pragma unroll
-      for (int st = 0; st < 4; ++st) {
-        const u32x4 raw = {v[2 * st][0], v[2 * st][1], v[2 * st + 1][0], v[2 * st + 1][1]};
-        vf[st] = __builtin_bit_cast(bf16x8, raw);
-      }
-      if (masked) {
-        uint32_t bad = 0;
-#pragma unroll
-        for (int st = 0; st < 4; ++st) bad |= not_finite_bits(vf[st]);
-        if (__builtin_amdgcn_ballot_w64(bad != 0)) {
-#pragma unroll
-          for (int qi = 0; qi < NQ; ++qi) {
-            const int top = min(slot_of[qi], w.end - 1) - kb0 - 4 * hi;
-            const int lo = a.window ? slot_of[qi] - a.window + 1 - kb0 - 4 * hi : -64;
-            f32x16 c;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) c[i] = 0.f;
-#pragma unroll
-            for (int st = 0; st < 4; ++st) {
-              bf16x8 one;
-#pragma unroll
-              for (int j = 0; j < 8; ++j) {
-                const int x = 16 * st + j % 4 + 8 * (j / 4);
-                one[j] = (__bf16)(x > top || x < lo ? 0.f : 1.f);
-              }
-              c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(not_finite_codes(vf[st]), one, c, 0, 0, 0);
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[qi][db][i] += not_finite_sum(c[i]);
-          }
-#pragma unroll
-          for (int st = 0; st < 4; ++st) vf[st] = finite_or_zero(vf[st]);
-        }
-      }
-#pragma unroll
-      for (int st = 0; st < 4; ++st)
-#pragma unroll
-        for (int qi = 0; qi < NQ; ++qi)
-          o[qi][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[st], pb[qi][st], o[qi][db], 0, 0, 0);
-    }
+  auto store_k = [&](int t) DSF_INLINE {
+    if constexpr (E8) codes.store(mine + (t & 1) * kTile, lane);
   };
-
-  if (ntiles > 0) fetch(0);
-  if constexpr (E8) {
-    if (ntiles > 0) settle(0);
-  }
-  for (int t = 0; t < ntiles; ++t) {
-    // tile t is in LDS for every wave, and every wave is done with tile t - 1, whose stage is filled next
+  auto store_v = [&](int t) DSF_INLINE {
+    if constexpr (E8) codes.store(mine + (2 + (t & 1)) * kTile, lane);
+  };
+  auto landed = [&]() DSF_INLINE {  // what this wave has staged, then what all have
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __syncthreads();
-    if (t + 1 < ntiles) fetch(t + 1);
-    tile(t);
-    if (t + 1 < ntiles) settle(t + 1);
+  };
+
+  // LDS addresses: rows r32 (+ 32 half) of a key tile, chunk 2 st + hi; of a value tile lane (group of 16 G, a4 =
+  // lane & 3, j = lane / 4 & 3) reads slots 4 hi + j (+ 8) (+ 16 st) at dims 32 db + 16 (G & 1) + 4 a4
+  const int vrow = 4 * hi + ((lane >> 2) & 3), vch = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+  const char *ka[NS], *va[ND], *vb[ND];
+#pragma unroll
+  for (int st = 0; st < NS; ++st) ka[st] = smem + r32 * S::kRowBytes + (((2 * st + hi) ^ S::swz(r32)) << 4);
+#pragma unroll
+  for (int db = 0; db < ND; ++db) {
+    const char* v = smem + 2 * kTile + vrow * S::kRowBytes + (lane & 1) * 8;
+    va[db] = v + (((4 * db + vch) ^ S::swz(vrow)) << 4);
+    vb[db] = v + 8 * S::kRowBytes + (((4 * db + vch) ^ S::swz(vrow + 8)) << 4);
+  }
+  // step st of a half of a key tile, and 32 dims of 16 slots of a value tile, at byte `at` of the stages
+  auto read_k = [&](int at, int st) DSF_INLINE { return *reinterpret_cast<const bf16x8*>(ka[st] + at); };
+  auto read_v = [&](int at, int db) DSF_INLINE {
+    return __builtin_shufflevector(lds_read_tr(va[db] + at), lds_read_tr(vb[db] + at), 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+
+  // scores of one half of tile t
+  auto scores = [&](int t, int half, f32x16& s) DSF_INLINE {
+    const int at = (t & 1) * kTile + 32 * half * S::kRowBytes;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+    for (int st = 0; st < NS; ++st) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_k(at, st), qf[st], s, 0, 0, 0);
+  };
+  // the slots of a half of tile t that this lane's row sees, relative to the lane's first
+  auto bounds = [&](int t, int half, int* lo, int* top) DSF_INLINE {
+    const int kb0 = w.begin + 64 * t + 32 * half + 4 * hi;
+    *top = min(my_slot, w.end - 1) - kb0;
+    *lo = a.window ? my_slot - a.window + 1 - kb0 : -64;
+  };
+  // The softmax of a half's scores in twelve steps of about the same work: the maximum in 0 to 3, then two of a lane's
+  // 16 weights in each. `sum` is of this half's, m_new what they are scaled by.
+  struct Soft {
+    float mx, m_new, sum;
+  };
+  auto soft = [&](int step, Soft& f, f32x16& s, bf16x8 (&p)[2]) DSF_INLINE {
+    if (step == 0) {
+      f.mx = fmaxf(s[0], s[1]);
+#pragma unroll
+      for (int i = 2; i < 8; ++i) f.mx = fmaxf(f.mx, s[i]);
+    } else if (step == 1) {
+#pragma unroll
+      for (int i = 8; i < 16; ++i) f.mx = fmaxf(f.mx, s[i]);
+    } else if (step == 2) {
+      f.mx = pair32_max(f.mx) * sc;
+    } else if (step == 3) {
+      f.m_new = f.mx > m_run + kLag ? f.mx : m_run;
+      f.sum = 0.f;
+    } else {
+      const int e = 2 * (step - 4);
+      typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+      const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
+      const bf16x2 p2 = {(__bf16)__builtin_amdgcn_exp2f(fmaf(s[e], sc, -f.m_new)),
+                         (__bf16)__builtin_amdgcn_exp2f(fmaf(s[e + 1], sc, -f.m_new))};
+      p[e / 8][e % 8] = p2[0];
+      p[e / 8][e % 8 + 1] = p2[1];
+      f.sum = __builtin_amdgcn_fdot2_f32_bf16(p2, one, f.sum, false);
+    }
+  };
+  // after it, and after the product that the accumulators had still to get with the old maximum
+  auto settle = [&](const Soft& f) DSF_INLINE {
+    if (__builtin_amdgcn_ballot_w64(f.m_new != m_run)) {
+      const float alpha = __builtin_amdgcn_exp2f(m_run - f.m_new);  // 1 where it did not move
+      l_run *= alpha;
+#pragma unroll
+      for (int db = 0; db < ND; ++db) o[db] *= alpha;
+    }
+    l_run += f.sum;
+    m_run = f.m_new;
+  };
+  // product of a half of tile t, where some row may not see some slot
+  auto product = [&](int t, int half, const bf16x8 (&p)[2]) DSF_INLINE {
+    const int at = (t & 1) * kTile + 32 * half * S::kRowBytes;
+#pragma unroll
+    for (int db = 0; db < ND; ++db) {
+      bf16x8 vf[2];
+#pragma unroll
+      for (int st = 0; st < 2; ++st) vf[st] = read_v(at + 16 * st * S::kRowBytes, db);
+      if (__builtin_amdgcn_ballot_w64((not_finite_bits(vf[0]) | not_finite_bits(vf[1])) != 0)) {
+        int lo, top;
+        bounds(t, half, &lo, &top);
+        f32x16 c;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) c[i] = 0.f;
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+          bf16x8 one;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int x = 16 * st + j % 4 + 8 * (j / 4);
+            one[j] = (__bf16)(x > top || x < lo ? 0.f : 1.f);
+          }
+          c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(not_finite_codes(vf[st]), one, c, 0, 0, 0);
+          vf[st] = finite_or_zero(vf[st]);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[db][i] += not_finite_sum(c[i]);
+      }
+#pragma unroll
+      for (int st = 0; st < 2; ++st) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[st], p[st], o[db], 0, 0, 0);
+    }
+  };
+  auto hide = [&](int t, int half, f32x16& s) DSF_INLINE {
+    int lo, top;
+    bounds(t, half, &lo, &top);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int x = 8 * (i / 4) + i % 4;
+      s[i] = x > top || x < lo ? -INFINITY : s[i];
+    }
+  };
+  // A half turn without hidden slots: s_next of the half at byte `kat` of the key stages, the softmax of s_now into
+  // p_now, the product of the half at byte `vat` of the value stages with p_last. The instructions stand in the order
+  // they are to be issued in: a matrix product, of the scores and of the values in turn, then a part of the softmax;
+  // operands are read kAhead products of a kind ahead.
+  auto half_turn = [&](int kat, f32x16& s_next, f32x16& s_now, bf16x8 (&p_now)[2], int vat,
+                       const bf16x8 (&p_last)[2]) DSF_INLINE {
+    constexpr int kPairs = NS, kSteps = 12, kAhead = E8 ? 1 : 2;  // NS == 2 ND: as many products of either kind
+    Soft f = {};
+    bf16x8 kf[kAhead + 1], vf[kAhead + 1];
+    auto next_k = [&](int i) DSF_INLINE { kf[i % (kAhead + 1)] = read_k(kat, i); };
+    auto next_v = [&](int i) DSF_INLINE { vf[i % (kAhead + 1)] = read_v(vat + 16 * (i / ND) * S::kRowBytes, i % ND); };
+#pragma unroll
+    for (int i = 0; i < kAhead && i < kPairs; ++i) {
+      next_k(i);
+      next_v(i);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s_next[i] = 0.f;
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < 2 * kPairs; ++i) {
+      const int j = i / 2;
+      if (i % 2 == 0) {
+        if (j + kAhead < kPairs) next_k(j + kAhead);
+        s_next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[j % (kAhead + 1)], qf[j], s_next, 0, 0, 0);
+      } else {
+        if (j + kAhead < kPairs) next_v(j + kAhead);
+        o[j % ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[j % (kAhead + 1)], p_last[j / ND], o[j % ND], 0, 0, 0);
+      }
+#pragma unroll
+      for (int step = i * kSteps / (2 * kPairs); step < (i + 1) * kSteps / (2 * kPairs); ++step) soft(step, f, s_now, p_now);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    // the weights are wanted in the next half turn only: keep them from moving there
+    asm volatile("" : "+v"(p_now[0]), "+v"(p_now[1]), "+v"(f.sum));
+    settle(f);
+  };
+  auto soft_all = [&](Soft& f, f32x16& s, bf16x8 (&p)[2]) DSF_INLINE {
+#pragma unroll
+    for (int step = 0; step < 12; ++step) soft(step, f, s, p);
+  };
+
+  if (nt > 0) {
+    f32x16 s0x, s1;  // scores of a tile's halves
+    bf16x8 p0[2], p1[2];
+    Soft f = {};
+    fetch_k(0);
+    store_k(0);
+    landed();
+    if (nt > 1) fetch_k(1);
+    if (!E8) fetch_v(0);
+    scores(0, 0, s0x);
+    scores(0, 1, s1);
+    if (nt > 1) store_k(1);
+    if (E8) fetch_v(0);
+    hide(0, 0, s0x);
+    soft_all(f, s0x, p0);
+    settle(f);
+    store_v(0);
+    // At the start of turn t: p0 and s1 of tile t. Keys of tile t + 1 and values of tile t have landed then, and
+    // the other stages are free. Codes go through the same registers, keys in a turn's first half, values in its second.
+    auto open = [&](int t) DSF_INLINE {
+      landed();
+      if (t + 2 < nt) fetch_k(t + 2);
+      if (!E8 && t + 1 < nt) fetch_v(t + 1);
+    };
+    auto middle = [&](int t) DSF_INLINE {
+      if (E8 && t + 2 < nt) store_k(t + 2);
+      if (E8 && t + 1 < nt) fetch_v(t + 1);
+    };
+    auto close = [&](int t) DSF_INLINE {
+      if (E8 && t + 1 < nt) store_v(t + 1);
+    };
+    // turns [t0, t1) have no hidden slot in tiles t and t + 1; they go in pairs from an even one, so that the stages'
+    // addresses are constants
+    const int t0 = min(max(see_lo - w.begin + 63, 0) >> 6, nt);
+    const int t1 = max((see_hi - w.begin) / 64 - 1, t0);
+    constexpr int kHalf = 32 * S::kRowBytes;
+    int t = 0;
+    while (t < nt) {
+      if (t >= t0 && !(t & 1)) {
+        for (; t + 1 < t1; t += 2) {
+          open(t);
+          half_turn(kTile, s0x, s1, p1, 0, p0);
+          middle(t);
+          half_turn(kTile + kHalf, s1, s0x, p0, kHalf, p1);
+          close(t);
+          open(t + 1);
+          half_turn(0, s0x, s1, p1, kTile, p0);
+          middle(t + 1);
+          half_turn(kHalf, s1, s0x, p0, kTile + kHalf, p1);
+          close(t + 1);
+        }
+        if (t >= nt) break;
+      }
+      open(t);
+      const bool more = t + 1 < nt;
+      if (more) scores(t + 1, 0, s0x);
+      hide(t, 1, s1);
+      soft_all(f, s1, p1);
+      product(t, 0, p0);
+      settle(f);
+      middle(t);
+      if (more) {
+        scores(t + 1, 1, s1);
+        hide(t + 1, 0, s0x);
+        soft_all(f, s0x, p0);
+      }
+      product(t, 1, p1);
+      if (more) settle(f);
+      close(t);
+      ++t;
+    }
   }
 
   // lane holds O^T[dim 32 db + 8 (i / 4) + 4 hi + i % 4][row r32]
+  const float l = pair32_sum(l_run);
+  if (m >= w.M) return;
+  if (w.splits > 1) {
+    const int64_t at = int64_t(blockIdx.x) * BM + (m - w.tile * BM);
+    float* po = a.part_o + at * HD;
 #pragma unroll
-  for (int qi = 0; qi < NQ; ++qi) {
-    const float l = pair32_sum(l_run[qi]);
-    if (!live[qi]) continue;
-    const int m = m0 + 32 * qi + r32;
-    if (w.splits > 1) {
-      const int64_t slot = int64_t(blockIdx.x) * BM + (m - w.tile * BM);
-      float* po = a.part_o + slot * HD;
+    for (int db = 0; db < ND; ++db)
 #pragma unroll
-      for (int db = 0; db < ND; ++db)
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4*>(po + 32 * db + 8 * i + 4 * hi) =
+            f32x4{o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]};
+    if (hi == 0) a.part_ml[at] = make_float2(m_run == kNothing ? -INFINITY : m_run, l);
+  } else {
+    const float inv = l == 0.f ? 0.f : 1.0f / l;  // a row that sees nothing: zeros
+    uint16_t* op = static_cast<uint16_t*>(a.out) + int64_t(w.row0 + tok) * a.o_row + int64_t(kvh * a.G + g) * a.o_head;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<f32x4*>(po + 32 * db + 8 * i + 4 * hi) =
-              f32x4{o[qi][db][4 * i], o[qi][db][4 * i + 1], o[qi][db][4 * i + 2], o[qi][db][4 * i + 3]};
-      if (hi == 0) a.part_ml[slot] = make_float2(m_run[qi], l);
-    } else {
-      const float inv = l == 0.f ? 0.f : 1.0f / l;  // a row that sees nothing: zeros
-      const int tok = m / a.G, g = m - tok * a.G;
-      uint16_t* op = static_cast<uint16_t*>(a.out) + int64_t(w.row0 + tok) * a.o_row + int64_t(kvh * a.G + g) * a.o_head;
+    for (int db = 0; db < ND; ++db)
 #pragma unroll
-      for (int db = 0; db < ND; ++db)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          u32x2 pk;
-          pk[0] = uint32_t(f2bf(o[qi][db][4 * i] * inv)) | uint32_t(f2bf(o[qi][db][4 * i + 1] * inv)) << 16;
-          pk[1] = uint32_t(f2bf(o[qi][db][4 * i + 2] * inv)) | uint32_t(f2bf(o[qi][db][4 * i + 3] * inv)) << 16;
-          *reinterpret_cast<u32x2*>(op + 32 * db + 8 * i + 4 * hi) = pk;
-        }
-    }
+      for (int i = 0; i < 4; ++i) {
+        u32x2 pk;
+        pk[0] = uint32_t(f2bf(o[db][4 * i] * inv)) | uint32_t(f2bf(o[db][4 * i + 1] * inv)) << 16;
+        pk[1] = uint32_t(f2bf(o[db][4 * i + 2] * inv)) | uint32_t(f2bf(o[db][4 * i + 3] * inv)) << 16;
+        *reinterpret_cast<u32x2*>(op + 32 * db + 8 * i + 4 * hi) = pk;
+      }
   }
 }
 
 // ------------------------------------------------------------ a few tokens
 
-// R transpose loads and their wait: for the steps of 32 slots of a tile (two
-// 16-slot halves each) the V^T operand of v_mfma_f32_16x16x32_bf16 for 16 dims.
+// Two transpose loads at each of four addresses and their wait: the V^T
+// operands of v_mfma_f32_16x16x32_bf16 for four (16 dims, 32 slots).
 template <int ROW>
-__device__ __forceinline__ void lds_read_tr2(uint32_t addr, u32x2 (&v)[2]) {
+__device__ __forceinline__ void lds_read_tr4x2(const uint32_t (&at)[4], u32x2 (&v)[8]) {
   asm volatile(
-      "ds_read_b64_tr_b16 %0, %2\n\t"
-      "ds_read_b64_tr_b16 %1, %2 offset:%3\n\t"
+      "ds_read_b64_tr_b16 %0, %8\n\t"
+      "ds_read_b64_tr_b16 %1, %8 offset:%12\n\t"
+      "ds_read_b64_tr_b16 %2, %9\n\t"
+      "ds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
+      "ds_read_b64_tr_b16 %4, %10\n\t"
+      "ds_read_b64_tr_b16 %5, %10 offset:%12\n\t"
+      "ds_read_b64_tr_b16 %6, %11\n\t"
+      "ds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
       "s_waitcnt lgkmcnt(0)"
-      : "=&v"(v[0]), "=&v"(v[1])
-      : "v"(addr), "n"(16 * ROW)
+      : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]), "=&v"(v[6]), "=&v"(v[7])
+      : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "n"(16 * ROW)
       : "memory");
 }
 
-// A workgroup of four waves takes 16 NR rows; each wave runs through every
-// fourth piece of TK slots by itself, from its own LDS, with a softmax of its
-// own, and the four are joined in wave order at the end: nothing waits for
-// another wave while slots stream in (memory bound: the rows of one token of
-// a few heads are far too few for the matrix cores to matter).
+// 16 slots of keys as the A operands of S^T = K Q^T: lane (r16, grp) has dims
+// dim(st, grp) .. + 7 of slot r16 for step st. The dims may be taken in any
+// order that Q is taken in too, so e4m3 codes are loaded 16 at a time, half
+// of them for the next step.
+template <int HD, bool E8>
+struct KeySlots {
+  static constexpr int NS = HD / 32;
+  static constexpr bool kWide = E8 && HD >= 64;
+  static constexpr int kWords = E8 ? HD / 16 : HD / 8;  // of a lane
+  uint32_t c[kWords];
+  uint32_t e;
+  __device__ static __forceinline__ int dim(int st, int grp) {
+    return kWide ? 64 * (st >> 1) + 16 * grp + 8 * (st & 1) : 32 * st + 8 * grp;
+  }
+  __device__ __forceinline__ void load(const PagedKernelArgs& a, int page, int kvh, int slot, int end, int lane) {
+    const int r16 = lane & 15, grp = lane >> 4, eb = E8 ? 1 : 2;
+    const int64_t row = ((int64_t(page) * a.pool.Hkv + kvh) << a.pb.page_shift) + (slot & ((1 << a.pb.page_shift) - 1));
+    const int rows = min(max(end - slot, 0), 16);
+    const auto rc = __builtin_amdgcn_make_buffer_rsrc(static_cast<char*>(a.pool.k) + row * HD * eb, (short)0,
+                                                      rows * HD * eb, 0x00020000);
+    if constexpr (E8 && !kWide) {
+      const u32x2 t = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rc, r16 * HD + 8 * grp, 0, 0));
+      c[0] = t[0];
+      c[1] = t[1];
+    } else {
+#pragma unroll
+      for (int i = 0; i < kWords / 4; ++i) {
+        const u32x4 t =
+            __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rc, r16 * HD * eb + 16 * grp + 64 * i, 0, 0));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c[4 * i + j] = t[j];
+      }
+    }
+    if constexpr (E8) {
+      const auto re = __builtin_amdgcn_make_buffer_rsrc(a.pool.ke + row, (short)0, rows, 0x00020000);
+      e = __builtin_amdgcn_raw_buffer_load_b8(re, r16, 0, 0);
+    }
+  }
+  __device__ __forceinline__ bf16x8 at(int st) const {
+    if constexpr (E8) {
+      const float s = paged_scale(e);
+      const u32x2 x = paged_widen4(c[2 * st], s), y = paged_widen4(c[2 * st + 1], s);
+      return __builtin_bit_cast(bf16x8, u32x4{x[0], x[1], y[0], y[1]});
+    } else {
+      return __builtin_bit_cast(bf16x8, u32x4{c[4 * st], c[4 * st + 1], c[4 * st + 2], c[4 * st + 3]});
+    }
+  }
+};
+
+// 16 slots of values, 16 bytes a lane, for LDS.
+template <int HD>
+struct ValueSlots {
+  static constexpr int kLoads = HD / 32;
+  u32x4 c[kLoads];
+  __device__ __forceinline__ void load(const PagedKernelArgs& a, int page, int kvh, int slot, int end, int lane) {
+    const int64_t row = ((int64_t(page) * a.pool.Hkv + kvh) << a.pb.page_shift) + (slot & ((1 << a.pb.page_shift) - 1));
+    const int rows = min(max(end - slot, 0), 16);  // the others load as zeros
+    const auto rc = __builtin_amdgcn_make_buffer_rsrc(static_cast<char*>(a.pool.v) + row * HD * 2, (short)0, rows * HD * 2,
+                                                      0x00020000);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+      c[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rc, 1024 * i + 16 * lane, 0, 0));
+  }
+  __device__ __forceinline__ void store(char* lds, int lane) const {
+    using S = SlotTile<HD>;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int byte = 1024 * i + 16 * lane, r = byte / S::kRowBytes, ch = byte % S::kRowBytes / 16;
+      *reinterpret_cast<u32x4*>(lds + r * S::kRowBytes + ((ch ^ S::swz(r)) << 4)) = c[i];
+    }
+  }
+};
+
+// A workgroup of four waves takes its share of the line (paged_flat), one
+// tile of 16 NR rows after the other; of a tile's slots each wave runs through
+// every fourth piece of TK by itself, with a softmax of its own, and the four
+// are joined in wave order. Memory bound (the rows of one token of a few
+// heads are far too few for the matrix cores to matter), so what counts is
+// bytes on the way: keys are loaded as the matrix operand they will be,
+// straight into registers, values into registers and on through LDS, which
+// transposes them; the next piece's loads are issued as soon as this one's
+// registers are free, and several workgroups share a CU.
 //
 // S^T = K Q^T with v_mfma_f32_16x16x32_bf16: lane (r16, grp) holds of row r16
 // the scores of slots 16 kb + 4 grp + i, which is the B operand of
@@ -602,226 +869,227 @@ __device__ __forceinline__ void lds_read_tr2(uint32_t addr, u32x2 (&v)[2]) {
 template <int HD, bool E8, int NR>
 __global__ __launch_bounds__(256) void paged_token_kernel(PagedKernelArgs a) {
   using S = SlotTile<HD>;
+  using K = KeySlots<HD, E8>;
+  using V = std::conditional_t<E8, CodeSlots<HD>, ValueSlots<HD>>;
   constexpr int BM = 16 * NR, TK = 4096 / HD, NS = HD / 32, ND = HD / 16, KB = TK / 16;
-  constexpr int kTile = TK * S::kRowBytes, kStages = E8 ? 1 : 2, kRing = 2 * kTile * kStages;
-  constexpr int kDma = 2 * kTile / 1024;  // DMA instructions per piece
-  constexpr int OS = HD + 4;              // floats per row of the join, so that 16 rows spread over the banks
-  static_assert(4 * kRing >= 4 * 16 * OS * 4, "the join reuses the ring");
-  __shared__ __attribute__((aligned(16))) char smem[4 * kRing];
+  constexpr int kTile = TK * S::kRowBytes;  // values of a piece
+  constexpr int OS = HD + 4;                // floats per row of the join, so that 16 rows spread over the banks
+  constexpr int kLds = 4 * kTile > 4 * 16 * OS * 4 ? 4 * kTile : 4 * 16 * OS * 4;
+  __shared__ __attribute__((aligned(16))) char smem[kLds];
   __shared__ float ms[4][BM], ls[4][BM];
   const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, grp = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int item = int(blockIdx.x) / a.pool.Hkv, kvh = int(blockIdx.x) - item * a.pool.Hkv;
-  const PagedItem it = paged_item(a, item, lane);
-  if (it.b < 0) return;
-  const PagedWork w = paged_work(a, it);
-  if (w.splits > 1 && w.begin >= w.end) return;
-
-  int slot_of[NR];
-  bf16x8 qf[NR][NS];
-  const int m0 = w.tile * BM;
-#pragma unroll
-  for (int r = 0; r < NR; ++r) {
-    const int mc = min(m0 + 16 * r + r16, w.M - 1);
-    const int tok = mc / a.G, g = mc - tok * a.G;
-    slot_of[r] = w.p0 + tok;
-    const uint16_t* qp = static_cast<const uint16_t*>(a.q) + int64_t(w.row0 + tok) * a.q_row + int64_t(kvh * a.G + g) * a.q_head;
-#pragma unroll
-    for (int s = 0; s < NS; ++s) qf[r][s] = *reinterpret_cast<const bf16x8*>(qp + 32 * s + 8 * grp);
-  }
-  const int see_hi = w.p0 + m0 / a.G + 1, last = w.p0 + min(m0 + BM - 1, w.M - 1) / a.G;
-  const int see_lo = a.window ? last - a.window + 1 : 0;
-  f32x4 o[NR][ND];
-  float m_run[NR], l_run[NR];
-#pragma unroll
-  for (int r = 0; r < NR; ++r) {
-    m_run[r] = -INFINITY;
-    l_run[r] = 0.f;
-#pragma unroll
-    for (int db = 0; db < ND; ++db) o[r][db] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
+  const int wg = int(blockIdx.x) / a.pool.Hkv, kvh = int(blockIdx.x) - wg * a.pool.Hkv;
+  PagedShape shapes = {};
+  if (lane < a.pb.B) shapes = paged_shape(a, lane);
+  const PagedFlat flat = paged_flat(a, shapes, lane);
+  if (wg >= flat.wgs) return;
+  int pos = flat.whole ? wg : flat.start(wg);
+  const int stop = flat.whole ? wg + 1 : flat.start(wg + 1);
   const float sc = 1.4426950408889634f / sqrtf(float(HD));
-
-  char* ring = smem + wave * kRing;
-  const int s0 = w.begin + TK * wave;
-  const int nt = w.end > s0 ? (w.end - s0 + 4 * TK - 1) / (4 * TK) : 0;
-  PagedTable tab;
-  tab.load(a, w.b, w.begin >> a.pb.page_shift, lane);
-  CodeSlots<HD> kc[KB], vc[KB];
-  auto fetch = [&](int t) {
-    const int slot = s0 + 4 * TK * t;
-    char* st = ring + (t & (kStages - 1)) * 2 * kTile;
-#pragma unroll
-    for (int i = 0; i < KB; ++i) {
-      const int page = tab.at(a, w.b, (slot + 16 * i) >> a.pb.page_shift, lane);
-      if constexpr (E8) {
-        kc[i].load(a.pool.k, a.pool.ke, a, page, kvh, slot + 16 * i, w.end, lane);
-        vc[i].load(a.pool.v, a.pool.ve, a, page, kvh, slot + 16 * i, w.end, lane);
-      } else {
-        DmaSlots<HD>::load(a.pool.k, a, page, kvh, slot + 16 * i, w.end, st + 16 * i * S::kRowBytes, lane);
-        DmaSlots<HD>::load(a.pool.v, a, page, kvh, slot + 16 * i, w.end, st + kTile + 16 * i * S::kRowBytes, lane);
-      }
-    }
-  };
+  char* vt = smem + wave * kTile;
   const int tj = (lane >> 2) & 3, vrow = 4 * grp + tj, vch = (lane & 3) >> 1, vbyte = (lane & 1) * 8;
-  auto piece = [&](int t) {
-    const int kb0 = s0 + 4 * TK * t;
-    const char* Ks = ring + (t & (kStages - 1)) * 2 * kTile;
-    f32x4 s[NR][KB];
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-      const int row = 16 * kb + r16;
-#pragma unroll
-      for (int r = 0; r < NR; ++r) s[r][kb] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int st = 0; st < NS; ++st) {
-        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(Ks + row * S::kRowBytes + (((4 * st + grp) ^ S::swz(row)) << 4));
-#pragma unroll
-        for (int r = 0; r < NR; ++r) s[r][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[r][st], s[r][kb], 0, 0, 0);
-      }
+  const uint32_t vs = uint32_t(size_t((__attribute__((address_space(3))) const char*)vt)) + vrow * S::kRowBytes + vbyte;
+
+  while (pos < stop) {
+    const PagedSpot spot = paged_spot(a, shapes, flat.whole, pos, lane);
+    if (spot.b < 0) return;
+    const int until = min(spot.until, stop);
+    const bool before = pos > spot.from, after = until < spot.until;  // shared with the last, the next workgroup
+    const PagedShape& w = spot.w;
+    int begin, end;
+    paged_range(a, w, spot.tile, 0, kNoSplit << 6, &begin, &end);
+    if (!flat.whole) {
+      begin = max(begin, w.lo + ((pos - spot.from) << a.unit_shift));
+      end = max(min(end, w.lo + ((until - spot.from) << a.unit_shift)), begin);
     }
-    const bool masked = kb0 + TK > min(see_hi, w.end) || kb0 < see_lo;
-    bf16x8 ph[NR][KB / 2], pl[NR][KB / 2];
+    pos = until;
+    const int p0 = w.kv - w.n, m0 = spot.tile * BM;
+
+    int slot_of[NR];
+    bf16x8 qf[NR][NS];
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
-      if (masked) {
-        const int top = min(slot_of[r], w.end - 1) - kb0 - 4 * grp;
-        const int lo = a.window ? slot_of[r] - a.window + 1 - kb0 - 4 * grp : -TK;
+      const int mc = min(m0 + 16 * r + r16, w.M - 1);
+      const int tok = mc / a.G, g = mc - tok * a.G;
+      slot_of[r] = p0 + tok;
+      const uint16_t* qp =
+          static_cast<const uint16_t*>(a.q) + int64_t(w.row0 + tok) * a.q_row + int64_t(kvh * a.G + g) * a.q_head;
+#pragma unroll
+      for (int s = 0; s < NS; ++s) qf[r][s] = *reinterpret_cast<const bf16x8*>(qp + K::dim(s, grp));
+    }
+    const int see_hi = p0 + m0 / a.G + 1, last = p0 + min(m0 + BM - 1, w.M - 1) / a.G;
+    const int see_lo = a.window ? last - a.window + 1 : 0;
+    f32x4 o[NR][ND];
+    float m_run[NR], l_run[NR];
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+      m_run[r] = -INFINITY;
+      l_run[r] = 0.f;
+#pragma unroll
+      for (int db = 0; db < ND; ++db) o[r][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    const int s0 = begin + TK * wave;
+    const int nt = end > s0 ? (end - s0 + 4 * TK - 1) / (4 * TK) : 0;
+    PagedTable tab;
+    tab.load(a, spot.b, begin >> a.pb.page_shift, lane);
+    K kx[KB];
+    V vx[KB];
+    auto fetch = [&](int slot) {
+#pragma unroll
+      for (int i = 0; i < KB; ++i) {
+        const int page = tab.at(a, spot.b, (slot + 16 * i) >> a.pb.page_shift, lane);
+        kx[i].load(a, page, kvh, slot + 16 * i, end, lane);
+        if constexpr (E8) vx[i].load(a.pool.v, a.pool.ve, a, page, kvh, slot + 16 * i, end, lane);
+        else vx[i].load(a, page, kvh, slot + 16 * i, end, lane);
+      }
+    };
+    if (nt > 0) fetch(s0);
+    for (int t = 0; t < nt; ++t) {
+      const int kb0 = s0 + 4 * TK * t;
+      f32x4 s[NR][KB];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+#pragma unroll
+        for (int r = 0; r < NR; ++r) s[r][kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int st = 0; st < NS; ++st) {
+          const bf16x8 kf = kx[kb].at(st);
+#pragma unroll
+          for (int r = 0; r < NR; ++r)
+            s[r][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[r][st], s[r][kb], 0, 0, 0);
+        }
+      }
+      // the values into LDS (this wave has read the last piece's), and the next piece's loads
+#pragma unroll
+      for (int i = 0; i < KB; ++i) vx[i].store(vt + 16 * i * S::kRowBytes, lane);
+      if (t + 1 < nt) fetch(kb0 + 4 * TK);
+      const bool masked = kb0 + TK > min(see_hi, end) || kb0 < see_lo;
+      bf16x8 ph[NR][KB / 2], pl[NR][KB / 2];
+#pragma unroll
+      for (int r = 0; r < NR; ++r) {
+        if (masked) {
+          const int top = min(slot_of[r], end - 1) - kb0 - 4 * grp;
+          const int lo = a.window ? slot_of[r] - a.window + 1 - kb0 - 4 * grp : -TK;
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[r][kb][i] = 16 * kb + i > top || 16 * kb + i < lo ? -INFINITY : s[r][kb][i];
+        }
+        float mx = -INFINITY;
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s[r][kb][i] = 16 * kb + i > top || 16 * kb + i < lo ? -INFINITY : s[r][kb][i];
-      }
-      float mx = -INFINITY;
+          for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[r][kb][i]);
+        const float m_new = fmaxf(m_run[r], rows4_max(mx) * sc);
+        const float base = m_new == -INFINITY ? 0.f : m_new;
+        if (__builtin_amdgcn_ballot_w64(m_new != m_run[r])) {
+          const float alpha = __builtin_amdgcn_exp2f(m_run[r] - base);
+          l_run[r] *= alpha;
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[r][kb][i]);
-      const float m_new = fmaxf(m_run[r], rows4_max(mx) * sc);
-      const float base = m_new == -INFINITY ? 0.f : m_new;
-      if (__builtin_amdgcn_ballot_w64(m_new != m_run[r])) {
-        const float alpha = __builtin_amdgcn_exp2f(m_run[r] - base);
-        l_run[r] *= alpha;
-#pragma unroll
-        for (int db = 0; db < ND; ++db) o[r][db] *= alpha;
-      }
-      m_run[r] = m_new;
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(s[r][kb][i], sc, -base));
-          l_run[r] += p;
-          const __bf16 h = (__bf16)p;
-          ph[r][kb / 2][4 * (kb & 1) + i] = h;
-          pl[r][kb / 2][4 * (kb & 1) + i] = (__bf16)(p - float(h));
+          for (int db = 0; db < ND; ++db) o[r][db] *= alpha;
         }
-    }
-    const uint32_t vs = uint32_t(size_t((__attribute__((address_space(3))) const char*)(Ks + kTile))) + vrow * S::kRowBytes + vbyte;
+        m_run[r] = m_new;
 #pragma unroll
-    for (int db = 0; db < ND; ++db) {
-      const uint32_t vc0 = vs + (((2 * db + vch) ^ S::swz(vrow)) << 4);
+        for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-      for (int ks = 0; ks < KB / 2; ++ks) {
-        u32x2 v[2];
-        lds_read_tr2<S::kRowBytes>(vc0 + 32 * ks * S::kRowBytes, v);
-        const u32x4 raw = {v[0][0], v[0][1], v[1][0], v[1][1]};
-        bf16x8 vf = __builtin_bit_cast(bf16x8, raw);
-        if (masked) {
-          if (__builtin_amdgcn_ballot_w64(not_finite_bits(vf) != 0)) {
+          for (int i = 0; i < 4; ++i) {
+            const float p = __builtin_amdgcn_exp2f(fmaf(s[r][kb][i], sc, -base));
+            l_run[r] += p;
+            const __bf16 h = (__bf16)p;
+            ph[r][kb / 2][4 * (kb & 1) + i] = h;
+            pl[r][kb / 2][4 * (kb & 1) + i] = (__bf16)(p - float(h));
+          }
+      }
+      // products four (16 dims, 32 slots) at a time
 #pragma unroll
-            for (int r = 0; r < NR; ++r) {
-              const int top = min(slot_of[r], w.end - 1) - kb0 - 4 * grp - 32 * ks;
-              const int lo = a.window ? slot_of[r] - a.window + 1 - kb0 - 4 * grp - 32 * ks : -TK;
-              bf16x8 one;
+      for (int c0 = 0; c0 < ND * KB / 2; c0 += 4) {
+        uint32_t at[4];
+        u32x2 v[8];
 #pragma unroll
-              for (int j = 0; j < 8; ++j) {
-                const int x = 16 * (j / 4) + j % 4;
-                one[j] = (__bf16)(x > top || x < lo ? 0.f : 1.f);
+        for (int c = 0; c < 4; ++c) {
+          const int db = (c0 + c) % ND, ks = (c0 + c) / ND;
+          at[c] = vs + (((2 * db + vch) ^ S::swz(vrow)) << 4) + 32 * ks * S::kRowBytes;
+        }
+        lds_read_tr4x2<S::kRowBytes>(at, v);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const int db = (c0 + c) % ND, ks = (c0 + c) / ND;
+          const u32x4 raw = {v[2 * c][0], v[2 * c][1], v[2 * c + 1][0], v[2 * c + 1][1]};
+          bf16x8 vf = __builtin_bit_cast(bf16x8, raw);
+          if (masked) {
+            if (__builtin_amdgcn_ballot_w64(not_finite_bits(vf) != 0)) {
+#pragma unroll
+              for (int r = 0; r < NR; ++r) {
+                const int top = min(slot_of[r], end - 1) - kb0 - 4 * grp - 32 * ks;
+                const int lo = a.window ? slot_of[r] - a.window + 1 - kb0 - 4 * grp - 32 * ks : -TK;
+                bf16x8 one;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                  const int x = 16 * (j / 4) + j % 4;
+                  one[j] = (__bf16)(x > top || x < lo ? 0.f : 1.f);
+                }
+                const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+                const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(not_finite_codes(vf), one, zero, 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[r][db][i] += not_finite_sum(n[i]);
               }
-              const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-              const f32x4 c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(not_finite_codes(vf), one, zero, 0, 0, 0);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) o[r][db][i] += not_finite_sum(c[i]);
+              vf = finite_or_zero(vf);
             }
-            vf = finite_or_zero(vf);
+          }
+#pragma unroll
+          for (int r = 0; r < NR; ++r) {
+            o[r][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, ph[r][ks], o[r][db], 0, 0, 0);
+            o[r][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pl[r][ks], o[r][db], 0, 0, 0);
           }
         }
+      }
+    }
+
+    // the four waves' results, in wave order; 16 rows at a time
+    float* os = reinterpret_cast<float*>(smem);
 #pragma unroll
-        for (int r = 0; r < NR; ++r) {
-          o[r][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, ph[r][ks], o[r][db], 0, 0, 0);
-          o[r][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pl[r][ks], o[r][db], 0, 0, 0);
+    for (int r = 0; r < NR; ++r) {
+      const float l = rows4_sum(l_run[r]);
+      __syncthreads();  // every wave is done with its values, or with the last 16 rows
+      if (grp == 0) {
+        ms[wave][16 * r + r16] = m_run[r];
+        ls[wave][16 * r + r16] = l;
+      }
+#pragma unroll
+      for (int db = 0; db < ND; ++db) *reinterpret_cast<f32x4*>(os + (wave * 16 + r16) * OS + 16 * db + 4 * grp) = o[r][db];
+      __syncthreads();
+      for (int e = tid; e < 16 * HD / 4; e += 256) {
+        const int q = e / (HD / 4), d = e % (HD / 4) * 4, m = m0 + 16 * r + q;
+        if (m >= w.M) break;
+        float M = -INFINITY, L = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) M = fmaxf(M, ms[i][16 * r + q]);
+        f32x4 O = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          // a wave whose slots are all hidden (maximum -inf) has zeros (NaN where a score was)
+          const float mi = ms[i][16 * r + q], f = mi == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mi - M);
+          L += ls[i][16 * r + q] * f;
+          O += *reinterpret_cast<const f32x4*>(os + (i * 16 + q) * OS + d) * f;
+        }
+        if (before || after) {
+          const int64_t slot = (int64_t(2 * wg + (before ? 0 : 1)) * a.pool.Hkv + kvh) * BM + 16 * r + q;
+          *reinterpret_cast<f32x4*>(a.part_o + slot * HD + d) = O;
+          if (d == 0) a.part_ml[slot] = make_float2(M, L);
+        } else {
+          const float inv = L == 0.f ? 0.f : 1.0f / L;
+          const int tok = m / a.G, g = m - tok * a.G;
+          u32x2 pk;
+          pk[0] = uint32_t(f2bf(O[0] * inv)) | uint32_t(f2bf(O[1] * inv)) << 16;
+          pk[1] = uint32_t(f2bf(O[2] * inv)) | uint32_t(f2bf(O[3] * inv)) << 16;
+          *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + int64_t(w.row0 + tok) * a.o_row +
+                                    int64_t(kvh * a.G + g) * a.o_head + d) = pk;
         }
       }
     }
-  };
-  if (nt > 0) fetch(0);
-  for (int t = 0; t < nt; ++t) {
-    if constexpr (E8) {
-      // the codes of this piece into LDS (the wave is done with the last one's), then the next ones' loads
-      char* st = ring;
-#pragma unroll
-      for (int i = 0; i < KB; ++i) {
-        kc[i].store(st + 16 * i * S::kRowBytes, lane);
-        vc[i].store(st + kTile + 16 * i * S::kRowBytes, lane);
-      }
-      if (t + 1 < nt) fetch(t + 1);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    } else {
-      if (t + 1 < nt) {
-        fetch(t + 1);
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kDma) : "memory");  // all but the next piece's
-      } else {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      }
-    }
-    __builtin_amdgcn_wave_barrier();
-    piece(t);
-    __builtin_amdgcn_wave_barrier();
-  }
-
-  // the four waves' shares, in wave order; 16 rows at a time through the ring
-  float* os = reinterpret_cast<float*>(smem);
-#pragma unroll
-  for (int r = 0; r < NR; ++r) {
-    const float l = rows4_sum(l_run[r]);
-    if (grp == 0) {
-      ms[wave][16 * r + r16] = m_run[r];
-      ls[wave][16 * r + r16] = l;
-    }
-    __syncthreads();  // every wave is done with the ring, and with the last 16 rows
-#pragma unroll
-    for (int db = 0; db < ND; ++db) *reinterpret_cast<f32x4*>(os + (wave * 16 + r16) * OS + 16 * db + 4 * grp) = o[r][db];
-    __syncthreads();
-    for (int e = tid; e < 16 * HD / 4; e += 256) {
-      const int q = e / (HD / 4), d = e % (HD / 4) * 4, m = m0 + 16 * r + q;
-      if (m >= w.M) break;
-      float M = -INFINITY, L = 0.f;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) M = fmaxf(M, ms[i][16 * r + q]);
-      f32x4 O = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float mi = ms[i][16 * r + q], f = mi == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mi - M);
-        // a wave whose slots are all hidden (maximum -inf) has a sum of 0, or of NaN where a score is NaN
-        L += mi == -INFINITY ? ls[i][16 * r + q] : ls[i][16 * r + q] * f;
-        const f32x4 oi = *reinterpret_cast<const f32x4*>(os + (i * 16 + q) * OS + d);
-        O += mi == -INFINITY ? oi : oi * f;
-      }
-      if (w.splits > 1) {
-        const int64_t slot = int64_t(blockIdx.x) * BM + 16 * r + q;
-        *reinterpret_cast<f32x4*>(a.part_o + slot * HD + d) = O;
-        if (d == 0) a.part_ml[slot] = make_float2(M, L);
-      } else {
-        const float inv = L == 0.f ? 0.f : 1.0f / L;
-        const int tok = m / a.G, g = m - tok * a.G;
-        u32x2 pk;
-        pk[0] = uint32_t(f2bf(O[0] * inv)) | uint32_t(f2bf(O[1] * inv)) << 16;
-        pk[1] = uint32_t(f2bf(O[2] * inv)) | uint32_t(f2bf(O[3] * inv)) << 16;
-        *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + int64_t(w.row0 + tok) * a.o_row +
-                                  int64_t(kvh * a.G + g) * a.o_head + d) = pk;
-      }
-    }
+    __syncthreads();  // the next tile's values go where these were
   }
 }
 
@@ -1043,68 +1311,128 @@ __global__ __launch_bounds__(256) void paged_f32_kernel(PagedKernelArgs a) {
   }
 }
 
-// ---------------------------------------------------- joining the splits
+// ---------------------------------------------------- joining the shares
 
-// One workgroup per (row, kv head): every split's share of the row, in the
-// splits' order. Rows of sequences that were not split are done already.
-// LOG2: the maxima are in log2 units.
+// Shares 0 .. n - 1 of a row of a tile, in their order, eight of them on the
+// way at a time, with a running maximum. Share i lies at place
+// i ? at1 + i * step : at0 of the workspace. The maxima are in log2 units for
+// bf16, natural ones for fp32.
 template <int HD, typename T>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedKernelArgs a) {
+__device__ __forceinline__ void paged_join_row(const PagedKernelArgs& a, int64_t at0, int64_t at1, int64_t step, int n,
+                                               int d, T* op) {
   constexpr bool LOG2 = sizeof(T) == 2;
-  const int r = blockIdx.x, kvh = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+  constexpr int U = 8;
+  float M = -INFINITY, L = 0.f;
+  f32x4 O = {0.f, 0.f, 0.f, 0.f};
+  for (int i0 = 0; i0 < n; i0 += U) {
+    float2 x[U];
+    f32x4 v[U];
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const int i = min(i0 + j, n - 1);
+      const int64_t at = i ? at1 + i * step : at0;
+      x[j] = a.part_ml[at];
+      v[j] = *reinterpret_cast<const f32x4*>(a.part_o + at * HD + d);
+    }
+    float mx = M;
+#pragma unroll
+    for (int j = 0; j < U; ++j) mx = fmaxf(mx, x[j].x);
+    // a share that saw nothing has zeros (NaN where a score was), as has the start
+    auto factor = [mx](float m) { return m == -INFINITY ? 1.f : LOG2 ? __builtin_amdgcn_exp2f(m - mx) : expf(m - mx); };
+    const float f0 = factor(M);
+    O *= f0;
+    L *= f0;
+#pragma unroll
+    for (int j = 0; j < U; ++j)
+      if (i0 + j < n) {
+        const float f = factor(x[j].x);
+        O += v[j] * f;
+        L += x[j].y * f;
+      }
+    M = mx;
+  }
+  const float inv = L == 0.f ? 0.f : 1.0f / L;
+  if constexpr (sizeof(T) == 2) {
+    u32x2 pk;
+    pk[0] = uint32_t(f2bf(O[0] * inv)) | uint32_t(f2bf(O[1] * inv)) << 16;
+    pk[1] = uint32_t(f2bf(O[2] * inv)) | uint32_t(f2bf(O[3] * inv)) << 16;
+    *reinterpret_cast<u32x2*>(op) = pk;
+  } else {
+    *reinterpret_cast<f32x4*>(op) = O * inv;
+  }
+}
+
+// A workgroup takes R rows of one tile and kv head, a thread four dims of a
+// row. Tiles that one workgroup had to itself are done already. FLAT: shares
+// of the line, else splits.
+template <int HD, typename T, bool FLAT, int R>
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedKernelArgs a) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  int tile = int(blockIdx.x) / a.pool.Hkv;
+  const int kvh = int(blockIdx.x) - tile * a.pool.Hkv;
   PagedShape w = {};
   if (lane < a.pb.B) w = paged_shape(a, lane);
-  const int per = paged_split_blocks(a, w, lane);
-  int first = 0;
+  PagedFlat flat = {};
+  int per = 0;
+  if constexpr (FLAT) {
+    flat = paged_flat(a, w, lane);
+    if (flat.whole) return;
+  } else {
+    per = paged_split_blocks(a, w, lane);
+  }
+  // the sequence that has the tile, and where its items (FLAT: units) begin
+  PagedShape s = {};
+  int first = 0, b = -1, each = 0;
   for (int b0 = 0; b0 < a.pb.B; b0 += 64) {
     if (b0) {
       w = PagedShape{};
       if (b0 + lane < a.pb.B) w = paged_shape(a, b0 + lane);
     }
-    const int splits = paged_splits(w, per), c = min(w.tiles * splits, a.items);
-    const int end = wave_prefix(c);
-    const uint64_t here = __builtin_amdgcn_ballot_w64(w.tiles > 0 && r >= w.row0 && r < w.row0 + min(w.n, a.pb.max_rows));
-    if (here) {
-      const int ln = __builtin_ctzll(here), ns = __builtin_amdgcn_readlane(splits, ln);
-      if (ns == 1) return;
-      first += __builtin_amdgcn_readlane(end, ln) - __builtin_amdgcn_readlane(c, ln);
-      const PagedShape s = paged_shape(a, b0 + ln);
-      const int tok = r - s.row0;
-      for (int e = tid; e < a.G * (HD / 4); e += 256) {
-        const int g = e / (HD / 4), d = e % (HD / 4) * 4, m = tok * a.G + g;
-        const int tile = m >> a.bm_shift, row = m & ((1 << a.bm_shift) - 1);
-        float M = -INFINITY, L = 0.f;
-        f32x4 O = {0.f, 0.f, 0.f, 0.f};
-        for (int i = 0; i < ns; ++i) {
-          int begin, stop;
-          paged_range(a, s, tile, i, per << 6, &begin, &stop);
-          if (begin >= stop) continue;
-          const int64_t item = min(first + i * s.tiles + max(s.tiles - 1 - tile, 0), a.items - 1);
-          const int64_t slot = ((item * a.pool.Hkv + kvh) << a.bm_shift) + row;
-          const float2 ml = a.part_ml[slot];
-          const f32x4 oi = *reinterpret_cast<const f32x4*>(a.part_o + slot * HD + d);
-          const float mn = fmaxf(M, ml.x);
-          // nothing seen so far, or nothing in this split: zeros (NaN where a score was)
-          const float f0 = M == -INFINITY ? 1.f : LOG2 ? __builtin_amdgcn_exp2f(M - mn) : expf(M - mn);
-          const float f1 = ml.x == -INFINITY ? 1.f : LOG2 ? __builtin_amdgcn_exp2f(ml.x - mn) : expf(ml.x - mn);
-          O = O * f0 + oi * f1;
-          L = L * f0 + ml.y * f1;
-          M = mn;
-        }
-        const float inv = L == 0.f ? 0.f : 1.0f / L;
-        T* op = static_cast<T*>(a.out) + int64_t(r) * a.o_row + int64_t(kvh * a.G + g) * a.o_head + d;
-        if constexpr (sizeof(T) == 2) {
-          u32x2 pk;
-          pk[0] = uint32_t(f2bf(O[0] * inv)) | uint32_t(f2bf(O[1] * inv)) << 16;
-          pk[1] = uint32_t(f2bf(O[2] * inv)) | uint32_t(f2bf(O[3] * inv)) << 16;
-          *reinterpret_cast<u32x2*>(op) = pk;
-        } else {
-          *reinterpret_cast<f32x4*>(op) = O * inv;
-        }
-      }
-      return;
+    const int n = FLAT ? paged_units(a, w) : paged_splits(w, per);
+    const int c = FLAT ? w.tiles * n : min(w.tiles * n, a.items);
+    const int tend = wave_prefix(w.tiles), end = wave_prefix(c);
+    const uint64_t over = __builtin_amdgcn_ballot_w64(tend > tile);
+    if (over) {
+      const int l = __builtin_ctzll(over);
+      b = b0 + l;
+      s = shape_of(w, l);
+      each = __builtin_amdgcn_readlane(n, l);
+      tile -= __builtin_amdgcn_readlane(tend, l) - __builtin_amdgcn_readlane(w.tiles, l);
+      first += __builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(c, l);
+      break;
     }
-    first = min(first + __builtin_amdgcn_readlane(end, 63), a.items);
+    tile -= __builtin_amdgcn_readlane(tend, 63);
+    first += __builtin_amdgcn_readlane(end, 63);
+    if (!FLAT) first = min(first, a.items);
+  }
+  if (b < 0) return;
+  int n;
+  int64_t at0, at1, step;  // places, in tiles
+  if constexpr (FLAT) {
+    const int j0 = flat.of(first + tile * each), j1 = flat.of(first + tile * each + each - 1);
+    n = j1 - j0 + 1;
+    if (n <= 1 || j0 < 0 || j1 >= a.items) return;
+    at0 = int64_t(2 * j0 + 1) * a.pool.Hkv + kvh;
+    at1 = int64_t(2 * j0) * a.pool.Hkv + kvh;
+    step = 2 * a.pool.Hkv;
+  } else {
+    if (each == 1) return;
+    int begin, stop;
+    paged_range(a, s, tile, 0, kNoSplit << 6, &begin, &stop);
+    const int len = per << 6, i0 = (begin - s.lo) / len, i1 = stop > begin ? (stop - s.lo + len - 1) / len : i0;
+    n = i1 - i0;
+    const int item = first + i0 * s.tiles + (s.tiles - 1 - tile);
+    // tables that claim more items than the launch has (row_start not ascending) end here
+    if (item < 0 || item + int64_t(max(n - 1, 0)) * s.tiles >= a.items) return;
+    at0 = at1 = int64_t(item) * a.pool.Hkv + kvh;
+    step = int64_t(s.tiles) * a.pool.Hkv;
+  }
+  for (int e = tid; e < R * (HD / 4); e += 256) {
+    const int row = int(blockIdx.y) * R + e / (HD / 4), d = e % (HD / 4) * 4, m = (tile << a.bm_shift) + row;
+    if (m >= s.M) break;
+    const int tok = m / a.G, g = m - tok * a.G;
+    paged_join_row<HD, T>(a, (at0 << a.bm_shift) + row, (at1 << a.bm_shift) + row, step << a.bm_shift, n, d,
+                          static_cast<T*>(a.out) + int64_t(s.row0 + tok) * a.o_row + int64_t(kvh * a.G + g) * a.o_head + d);
   }
 }
 
@@ -1116,30 +1444,59 @@ namespace {
 struct PagedPlan {
   bool on;
   int bm_shift, m_lo, m_hi;
-  int items;   // per kv head, at most
-  int target;  // per kv head (0: no splits)
-  size_t bytes;
+  int items;       // workgroups per kv head, at most
+  int tiles;       // of rows, the same
+  int target;      // splits: items aimed at (0: none)
+  int unit_shift;
+  bool join;       // whether tiles may have shares
+  size_t places;   // of shares, per kv head
 };
 
-constexpr int kTokenRows = 64;        // rows of a sequence (tokens times heads) the token kernel takes
-constexpr int kTokenItems = 1024;     // items aimed at, of all kv heads
-constexpr int kChunkItems = 512;
-constexpr int kF32Items = 1024;
-constexpr int kSplitMinBlocks = 8;    // 512 slots
+constexpr int kTokenRows = 64;       // rows of a sequence (tokens times heads) the token kernel takes
+constexpr int kChunkItems = 512;     // workgroups aimed at, of all kv heads
+constexpr int kF32Items = 512;
+constexpr int kSplitMinBlocks = 4;   // 256 slots
+
+// Workgroups of the token kernel that a CU holds, for 16, 32 and 64 rows.
+constexpr int kTokenPerCu[3] = {2, 1, 1};
 
 size_t align256(size_t n) { return (n + 255) & ~size_t(255); }
 
-PagedPlan make_plan(const PagedBatch& pb, int G, int Hkv, int hd, int bm_shift, int m_lo, int m_hi, int total) {
-  PagedPlan p = {true, bm_shift, m_lo, m_hi, 0, 0, 0};
+PagedPlan tiles_plan(const PagedBatch& pb, int G, int bm_shift, int m_lo, int m_hi) {
+  PagedPlan p = {};
+  p.on = true;
+  p.bm_shift = bm_shift;
+  p.m_lo = m_lo;
+  p.m_hi = m_hi;
+  p.unit_shift = 6;
   // tiles: full ones, and a part of one per sequence that takes part
   const int64_t rows = int64_t(pb.n_rows) * G;
   const int64_t seqs = std::min<int64_t>(std::min(pb.B, pb.n_rows), rows / (m_lo + 1));
-  const int64_t tiles = (rows >> bm_shift) + seqs;
+  int64_t tiles = (rows >> bm_shift) + seqs;
+  if (m_hi < 1 << 20) tiles = std::min<int64_t>(tiles, seqs * (((m_hi - 1) >> bm_shift) + 1));
+  p.tiles = int(tiles);
+  return p;
+}
+
+PagedPlan split_plan(const PagedBatch& pb, int G, int Hkv, int bm_shift, int m_lo, int m_hi, int total) {
+  PagedPlan p = tiles_plan(pb, G, bm_shift, m_lo, m_hi);
   const int64_t blocks = (int64_t(pb.max_pages) << pb.page_shift) / 64;
-  if (blocks > kSplitMinBlocks && tiles <= 4096 && tiles * Hkv < 2 * total) p.target = std::max(total / Hkv, 1);
-  p.items = int(tiles + p.target);
-  if (p.target)
-    p.bytes = align256((size_t(p.items) * Hkv << bm_shift) * hd * 4) + align256((size_t(p.items) * Hkv << bm_shift) * 8);
+  if (blocks > kSplitMinBlocks && p.tiles <= 4096 && int64_t(p.tiles) * Hkv < 2 * total) p.target = std::max(total / Hkv, 1);
+  p.items = p.tiles + p.target;
+  p.join = p.target != 0;
+  p.places = p.join ? p.items : 0;
+  return p;
+}
+
+PagedPlan flat_plan(const PagedBatch& pb, int G, int Hkv, int bm_shift, int m_hi) {
+  PagedPlan p = tiles_plan(pb, G, bm_shift, 0, m_hi);
+  p.items = std::max(256 * kTokenPerCu[bm_shift - 4] / Hkv, 1);
+  const int64_t slots = int64_t(pb.max_pages) << pb.page_shift;
+  // (row_start that does not ascend may claim all tiles of every sequence)
+  const int64_t most = int64_t(pb.B) * (((m_hi - 1) >> bm_shift) + 1);
+  while (most * ((slots >> p.unit_shift) + 1) > int64_t(1) << 30) ++p.unit_shift;
+  p.join = slots > kWholeUnits << 6 || most > p.items;
+  p.places = p.join ? 2 * size_t(p.items) : 0;
   return p;
 }
 
@@ -1148,15 +1505,20 @@ void paged_plans(int dtype, int Hq, const PagedPool& pool, const PagedBatch& pb,
   const int G = Hq / pool.Hkv;
   p[0] = p[1] = PagedPlan{};
   if (dtype == DSF_F32) {
-    p[0] = make_plan(pb, G, pool.Hkv, pool.hd, 4, 0, 0x7fffffff, kF32Items);
+    p[1] = split_plan(pb, G, pool.Hkv, 4, 0, 0x7fffffff, kF32Items);
     return;
   }
   const int64_t most = int64_t(std::min(pb.max_rows, pb.n_rows)) * G;
   // sequences of one token stay with the token kernel beside ones with chunks
   const int few = most <= kTokenRows ? int(most) : std::min((G + 15) / 16 * 16, kTokenRows);
-  if (most <= kTokenRows || pb.B > 1)
-    p[0] = make_plan(pb, G, pool.Hkv, pool.hd, few <= 16 ? 4 : few <= 32 ? 5 : 6, 0, few, kTokenItems);
-  if (most > kTokenRows) p[1] = make_plan(pb, G, pool.Hkv, pool.hd, 7, pb.B > 1 ? few : 0, 0x7fffffff, kChunkItems);
+  if (most <= kTokenRows || pb.B > 1) p[0] = flat_plan(pb, G, pool.Hkv, few <= 16 ? 4 : few <= 32 ? 5 : 6, few);
+  if (most > kTokenRows) p[1] = split_plan(pb, G, pool.Hkv, 7, pb.B > 1 ? few : 0, 0x7fffffff, kChunkItems);
+}
+
+size_t plan_rows(const PagedPlan& p, int Hkv) { return p.places * Hkv << p.bm_shift; }
+size_t plan_bytes(const PagedPlan& p, const PagedPool& pool) {
+  const size_t rows = plan_rows(p, pool.Hkv);
+  return align256(rows * pool.hd * 4) + align256(rows * 8);
 }
 
 }  // namespace
@@ -1164,7 +1526,7 @@ void paged_plans(int dtype, int Hq, const PagedPool& pool, const PagedBatch& pb,
 size_t paged_attention_workspace_bytes(int dtype, int Hq, const PagedPool& pool, const PagedBatch& pb) {
   PagedPlan p[2];
   paged_plans(dtype, Hq, pool, pb, p);
-  return std::max<size_t>(p[0].bytes + p[1].bytes, 256);
+  return std::max<size_t>(plan_bytes(p[0], pool) + plan_bytes(p[1], pool), 256);
 }
 
 hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t s) {
@@ -1173,7 +1535,6 @@ hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t s) {
   PagedPlan p[2];
   paged_plans(a.dtype, a.Hq, a.pool, a.pb, p);
   char* ws = static_cast<char*>(a.workspace);
-  const bool e8 = a.pool.codes;
   for (int i = 0; i < 2; ++i) {
     if (!p[i].on) continue;
     PagedKernelArgs k;
@@ -1193,24 +1554,25 @@ hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t s) {
     k.items = p[i].items;
     k.target = p[i].target;
     k.split_min = kSplitMinBlocks;
-    const size_t rows = size_t(p[i].items) * a.pool.Hkv << p[i].bm_shift;
+    k.unit_shift = p[i].unit_shift;
     k.part_o = reinterpret_cast<float*>(ws);
-    k.part_ml = reinterpret_cast<float2*>(ws + align256(rows * a.pool.hd * 4));
-    ws += p[i].bytes;
+    k.part_ml = reinterpret_cast<float2*>(ws + align256(plan_rows(p[i], a.pool.Hkv) * a.pool.hd * 4));
+    ws += plan_bytes(p[i], a.pool);
     const unsigned grid = unsigned(p[i].items) * a.pool.Hkv;
     auto run = [&](auto hdc, auto e8c) -> hipError_t {
       constexpr int HD = decltype(hdc)::value;
       constexpr bool E8 = decltype(e8c)::value;
       if (a.dtype == DSF_F32) paged_f32_kernel<HD, E8><<<grid, 256, 0, s>>>(k);
-      else if (i == 1) paged_chunk_kernel<HD, E8, 1><<<grid, 256, 0, s>>>(k);
+      else if (i == 1) paged_chunk_kernel<HD, E8><<<grid, 256, 0, s>>>(k);
       else if (k.bm_shift == 4) paged_token_kernel<HD, E8, 1><<<grid, 256, 0, s>>>(k);
       else if (k.bm_shift == 5) paged_token_kernel<HD, E8, 2><<<grid, 256, 0, s>>>(k);
       else paged_token_kernel<HD, E8, 4><<<grid, 256, 0, s>>>(k);
-      hipError_t e = hipGetLastError();
-      if (e != hipSuccess || !k.target) return e;
-      const dim3 jg(a.pb.n_rows, a.pool.Hkv);
-      if (a.dtype == DSF_F32) paged_join_kernel<HD, float><<<jg, 256, 0, s>>>(k);
-      else paged_join_kernel<HD, uint16_t><<<jg, 256, 0, s>>>(k);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess || !p[i].join) return e;
+      const dim3 jg(unsigned(p[i].tiles) * a.pool.Hkv, (1 << k.bm_shift) / 16);
+      if (a.dtype == DSF_F32) paged_join_kernel<HD, float, false, 16><<<jg, 256, 0, s>>>(k);
+      else if (i == 1) paged_join_kernel<HD, uint16_t, false, 16><<<jg, 256, 0, s>>>(k);
+      else paged_join_kernel<HD, uint16_t, true, 16><<<jg, 256, 0, s>>>(k);
       return hipGetLastError();
     };
     auto run_h = [&](auto e8c) -> hipError_t {
@@ -1221,7 +1583,7 @@ hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t s) {
         default: return hipErrorInvalidValue;
       }
     };
-    const hipError_t e = e8 ? run_h(std::true_type()) : run_h(std::false_type());
+    const hipError_t e = a.pool.codes ? run_h(std::true_type()) : run_h(std::false_type());
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
