@@ -447,6 +447,7 @@ class PagedCache:
                                  "None for others")
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
         self.device = _one_device(*(t for t in (k, v, k_exp, v_exp) if t is not None))
+        self.index = k.get_device()  # -1: not on a GPU
         n_pages, heads, page, hd = k.shape
         self.n_kv_heads, self.head_dim = heads, hd
         self._struct = _PagedCacheStruct(_ptr(k), _ptr(v), _ptr(k_exp), _ptr(v_exp), types[k.dtype], n_pages, heads, page,
@@ -477,6 +478,7 @@ class PagedBatch:
             raise ValueError("row_start [B + 1], kv_len [B], pages [B, max_pages]")
         self.row_start, self.kv_len, self.pages, self.n_rows = row_start, kv_len, pages, n_rows
         self.device = _one_device(row_start, kv_len, pages)
+        self.index = kv_len.get_device()
         self._struct = _PagedBatchStruct(_ptr(row_start), _ptr(kv_len), _ptr(pages), B, pages.shape[1], n_rows, max_rows)
         self._addr = ctypes.addressof(self._struct)
 
@@ -494,8 +496,8 @@ def _paged_rows(name: str, t, cache: PagedCache, batch: PagedBatch, heads: Optio
     if len(shape) != 3 or shape[0] != batch.n_rows or shape[2] != cache.head_dim or (heads is not None and shape[1] != heads):
         raise ValueError(f"{name}: [n_rows, heads, head_dim] = [{batch.n_rows}, {heads or 'heads'}, {cache.head_dim}] "
                          f"expected, got {list(shape)}")
-    if t.device != cache.device or t.device != batch.device:
-        raise ValueError(f"{name} lies on {t.device}, the cache on {cache.device}, the batch on {batch.device}")
+    if t.get_device() != cache.index:
+        raise ValueError(f"{name} lies on {t.device}, the cache on {cache.device}")
     row, head, last = t.stride()
     if last != 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
@@ -503,34 +505,41 @@ def _paged_rows(name: str, t, cache: PagedCache, batch: PagedBatch, heads: Optio
     return t.data_ptr(), row if shape[0] > 1 else 0, head if shape[1] > 1 else 0
 
 
-def _on_device(device, stream, call):
-    """call(stream handle) with `device` current; the stream is the given one or that device's current one."""
-    if device.type != "cuda":
-        raise ValueError(f"the tensors lie on {device}, not on a GPU")
-    if stream is not None and stream.device != device:
-        raise ValueError(f"the stream belongs to {stream.device}, the tensors to {device}")
-    if device.index == torch.cuda.current_device():
-        return call(_stream(stream))
-    with torch.cuda.device(device):
-        return call(_stream(stream))
+def _paged_call(name: str, cache: PagedCache, batch: PagedBatch, stream, *args):
+    """The C entry point `name` with the caches' device current, on the given stream or that device's current one."""
+    index = cache.index
+    if index < 0:
+        raise ValueError(f"the tensors lie on {cache.device}, not on a GPU")
+    if batch.index != index:
+        raise ValueError(f"the batch lies on {batch.device}, the cache on {cache.device}")
+    if stream is not None and stream.device.index != index:
+        raise ValueError(f"the stream belongs to {stream.device}, the tensors to {cache.device}")
+    fn = getattr(_lib or lib(), name)
+    if index == torch.cuda.current_device():
+        rc = fn(cache._addr, batch._addr, *args, _stream(stream))
+    else:
+        with torch.cuda.device(index):
+            rc = fn(cache._addr, batch._addr, *args, _stream(stream))
+    if rc:
+        _check(name, rc)
 
 
 def paged_cache_write(cache: PagedCache, batch: PagedBatch, k, v, stream=None):
     """k, v [n_rows, n_kv_heads, head_dim] (views of wider rows, too) into the slots of the batch's rows."""
-    kp, vp = _paged_rows("k", k, cache, batch, cache.n_kv_heads), _paged_rows("v", v, cache, batch, cache.n_kv_heads)
+    heads = cache.n_kv_heads
     if v.dtype != k.dtype:
         raise ValueError("k and v have different dtypes")
-    _check("dsf_paged_cache_write", _on_device(cache.device, stream, lambda s: lib().dsf_paged_cache_write(
-        cache._addr, batch._addr, _dtype_code(k), *kp, *vp, s)))
+    _paged_call("dsf_paged_cache_write", cache, batch, stream, _dtype_code(k), *_paged_rows("k", k, cache, batch, heads),
+                *_paged_rows("v", v, cache, batch, heads))
 
 
 def paged_cache_read(cache: PagedCache, batch: PagedBatch, k, v, stream=None):
     """The slots of the batch's rows into k, v [n_rows, n_kv_heads, head_dim]; other rows stay as they are."""
-    kp, vp = _paged_rows("k", k, cache, batch, cache.n_kv_heads), _paged_rows("v", v, cache, batch, cache.n_kv_heads)
+    heads = cache.n_kv_heads
     if v.dtype != k.dtype:
         raise ValueError("k and v have different dtypes")
-    _check("dsf_paged_cache_read", _on_device(cache.device, stream, lambda s: lib().dsf_paged_cache_read(
-        cache._addr, batch._addr, _dtype_code(k), *kp, *vp, s)))
+    _paged_call("dsf_paged_cache_read", cache, batch, stream, _dtype_code(k), *_paged_rows("k", k, cache, batch, heads),
+                *_paged_rows("v", v, cache, batch, heads))
 
 
 def paged_attention_workspace_size(cache: PagedCache, batch: PagedBatch, dtype: int, n_heads: int) -> int:
@@ -539,19 +548,22 @@ def paged_attention_workspace_size(cache: PagedCache, batch: PagedBatch, dtype: 
 
 def paged_attention(cache: PagedCache, batch: PagedBatch, q, out, window: int = 0, workspace=None, stream=None):
     """q [n_rows, n_heads, head_dim] over the pages; out the same shape. Rows of no sequence stay as they are."""
-    qp, op = _paged_rows("q", q, cache, batch), _paged_rows("out", out, cache, batch, q.shape[1])
+    qp, heads = _paged_rows("q", q, cache, batch), q.shape[1]
+    op = _paged_rows("out", out, cache, batch, heads)
     if out.dtype != q.dtype:
         raise ValueError("q and out have different dtypes")
     dtype = _dtype_code(q)
     if workspace is None:
-        need = max(paged_attention_workspace_size(cache, batch, dtype, q.shape[1]), 256)
+        need = max(paged_attention_workspace_size(cache, batch, dtype, heads), 256)
         # on the stream that uses it, so that its memory is not handed on before that
         with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
             workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-    elif workspace.device != cache.device:
+    elif workspace.get_device() != cache.index:
         raise ValueError(f"workspace lies on {workspace.device}, the cache on {cache.device}")
-    _check("dsf_paged_attention", _on_device(cache.device, stream, lambda s: lib().dsf_paged_attention(
-        cache._addr, batch._addr, dtype, q.shape[1], *qp, window, *op, _ptr(workspace), workspace.nbytes, s)))
+    elif not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous")
+    _paged_call("dsf_paged_attention", cache, batch, stream, dtype, heads, *qp, window, *op, workspace.data_ptr(),
+                workspace.nbytes)
 
 
 def timing_enable(max_records: int, kinds: Optional[Sequence[str]] = None):

@@ -82,22 +82,32 @@ struct PagedItem {
   int splits;  // of the sequence
 };
 constexpr int kNoSplit = 1 << 19;  // blocks: more slots than a sequence may have
-// Blocks of 64 slots per split: all the work (tiles times blocks) over the
-// number of items aimed at, so that items are alike whatever the sequences'
-// lengths. Sequences in lanes: b = lane of the first 64 in w.
+__device__ __forceinline__ int paged_splits(const PagedShape& w, int per) { return max((w.blocks + per - 1) / per, 1); }
+// Blocks of 64 slots per split. All the work (tiles times blocks) over the
+// number of items aimed at: a longer item would outlast the others. Where
+// there are fewer tiles than that, so many longer that the items are no more:
+// one round of workgroups, and a few in a second would double the time.
+// w: shapes of the first 64 sequences, in lanes.
 __device__ __forceinline__ int paged_split_blocks(const PagedKernelArgs& a, const PagedShape& w, int lane) {
   if (a.target == 0) return kNoSplit;
-  int sum = w.tiles * w.blocks;
-  for (int b0 = 64; b0 < a.pb.B; b0 += 64) {
-    if (b0 + lane < a.pb.B) {
-      const PagedShape x = paged_shape(a, b0 + lane);
-      sum += x.tiles * x.blocks;
+  // sum over the sequences of what f says of them
+  auto total = [&](auto f) {
+    int n = f(w);
+    for (int b0 = 64; b0 < a.pb.B; b0 += 64)
+      if (b0 + lane < a.pb.B) n += f(paged_shape(a, b0 + lane));
+    return __builtin_amdgcn_readlane(wave_prefix(n), 63);
+  };
+  const int sum = total([](const PagedShape& x) { return x.tiles * x.blocks; });
+  int per = max((sum + a.target - 1) / a.target, a.split_min);
+  if (a.pb.B <= 64 && total([](const PagedShape& x) { return x.tiles; }) < a.target) {
+    for (int i = 0; i < 4; ++i) {
+      const int items = total([per](const PagedShape& x) { return x.tiles * paged_splits(x, per); });
+      if (items <= a.target) break;
+      per = int((unsigned(per) * unsigned(items) + a.target - 1) / unsigned(a.target));
     }
   }
-  sum = __builtin_amdgcn_readlane(wave_prefix(sum), 63);
-  return max((sum + a.target - 1) / a.target, a.split_min);
+  return per;
 }
-__device__ __forceinline__ int paged_splits(const PagedShape& w, int per) { return max((w.blocks + per - 1) / per, 1); }
 
 // The sequence that item `item` (of one kv head) belongs to.
 __device__ __forceinline__ PagedItem paged_item(const PagedKernelArgs& a, int item, int lane) {
@@ -432,19 +442,20 @@ __device__ __forceinline__ float not_finite_sum(float c) {
 //
 // DMA into LDS is issued in inline assembly: the compiler, which cannot tell
 // the stages apart, would wait for it before every transpose load.
+template <int HD>
+constexpr int kChunkLds = 4 * 64 * SlotTile<HD>::kRowBytes;  // two tiles of keys, two of values
 template <int HD, bool E8>
-__global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedKernelArgs a) {
+__device__ __forceinline__ void paged_chunk(const PagedKernelArgs& a, int block, char* smem) {
   using S = SlotTile<HD>;
   constexpr int BM = 128, NS = HD / 16, ND = HD / 32;
   constexpr int kTile = 64 * S::kRowBytes;
   constexpr float kLag = 8.f;           // log2 units
   constexpr float kNothing = -3.0e38f;  // the maximum of nothing: finite, so that -inf less it is -inf
-  __shared__ __attribute__((aligned(16))) char smem[4 * kTile];  // K 0, K 1, V 0, V 1
   const int tid = threadIdx.x, lane = tid & 63, r32 = lane & 31, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // kv head innermost: consecutive workgroups go to different XCDs, so that
   // (with 8 heads or a divisor of 8) an XCD's L2 sees the slots of few heads
-  const int item = int(blockIdx.x) / a.pool.Hkv, kvh = int(blockIdx.x) - item * a.pool.Hkv;
+  const int item = block / a.pool.Hkv, kvh = block - item * a.pool.Hkv;
   const PagedItem it = paged_item(a, item, lane);
   if (it.b < 0) return;
   const PagedWork w = paged_work(a, it);
@@ -463,6 +474,10 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedKernelArgs a) 
   // slots that every row of the wave sees: [see_lo, see_hi)
   const int see_hi = min(w.p0 + min(m0, w.M - 1) / a.G + 1, w.end);
   const int see_lo = a.window ? w.p0 + min(m0 + 31, w.M - 1) / a.G - a.window + 1 : 0;
+
+  // tiles up to the last one that some row sees
+  const int any_hi = m0 < w.M ? w.p0 + min(m0 + 31, w.M - 1) / a.G + 1 : 0;
+  const int my_nt = max(min(any_hi, w.end) - w.begin + 63, 0) >> 6;
 
   const float sc = 1.4426950408889634f / sqrtf(float(HD));  // log2(e) / sqrt(hd)
   f32x16 o[ND];
@@ -692,7 +707,7 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedKernelArgs a) 
     const int t1 = max((see_hi - w.begin) / 64 - 1, t0);
     constexpr int kHalf = 32 * S::kRowBytes;
     int t = 0;
-    while (t < nt) {
+    while (t < my_nt) {
       if (t >= t0 && !(t & 1)) {
         for (; t + 1 < t1; t += 2) {
           open(t);
@@ -706,10 +721,10 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedKernelArgs a) 
           half_turn(kHalf, s1, s0x, p0, kTile + kHalf, p1);
           close(t + 1);
         }
-        if (t >= nt) break;
+        if (t >= my_nt) break;
       }
       open(t);
-      const bool more = t + 1 < nt;
+      const bool more = t + 1 < my_nt;
       if (more) scores(t + 1, 0, s0x);
       hide(t, 1, s1);
       soft_all(f, s1, p1);
@@ -726,13 +741,18 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedKernelArgs a) 
       close(t);
       ++t;
     }
+    for (; t < nt; ++t) {  // for the other waves
+      open(t);
+      middle(t);
+      close(t);
+    }
   }
 
   // lane holds O^T[dim 32 db + 8 (i / 4) + 4 hi + i % 4][row r32]
   const float l = pair32_sum(l_run);
   if (m >= w.M) return;
   if (w.splits > 1) {
-    const int64_t at = int64_t(blockIdx.x) * BM + (m - w.tile * BM);
+    const int64_t at = int64_t(block) * BM + (m - w.tile * BM);
     float* po = a.part_o + at * HD;
 #pragma unroll
     for (int db = 0; db < ND; ++db)
@@ -866,20 +886,26 @@ struct ValueSlots {
 // A probability goes into that product as two bf16 numbers (its rounding and
 // what that leaves), so it counts with 16 bits: the second product costs
 // nothing here.
+// LDS: the waves' values, or 16 rows of all four waves (rows HD + 4 floats
+// apart, so that they spread over the banks); then maxima and sums.
+template <int HD>
+constexpr int kTokenShare = 4 * 8192 > 4 * 16 * (HD + 4) * 4 ? 4 * 8192 : 4 * 16 * (HD + 4) * 4;
+template <int HD, int NR>
+constexpr int kTokenLds = kTokenShare<HD> + 2 * 4 * 16 * NR * 4;
 template <int HD, bool E8, int NR>
-__global__ __launch_bounds__(256) void paged_token_kernel(PagedKernelArgs a) {
+__device__ __forceinline__ void paged_token(const PagedKernelArgs& a, int block, char* smem) {
   using S = SlotTile<HD>;
   using K = KeySlots<HD, E8>;
   using V = std::conditional_t<E8, CodeSlots<HD>, ValueSlots<HD>>;
   constexpr int BM = 16 * NR, TK = 4096 / HD, NS = HD / 32, ND = HD / 16, KB = TK / 16;
   constexpr int kTile = TK * S::kRowBytes;  // values of a piece
-  constexpr int OS = HD + 4;                // floats per row of the join, so that 16 rows spread over the banks
-  constexpr int kLds = 4 * kTile > 4 * 16 * OS * 4 ? 4 * kTile : 4 * 16 * OS * 4;
-  __shared__ __attribute__((aligned(16))) char smem[kLds];
-  __shared__ float ms[4][BM], ls[4][BM];
+  constexpr int OS = HD + 4;                // floats per row of the join
+  static_assert(kTile == 8192, "values of a piece");
+  auto ms = reinterpret_cast<float(*)[BM]>(smem + kTokenShare<HD>);  // [4][BM]
+  auto ls = ms + 4;
   const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, grp = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wg = int(blockIdx.x) / a.pool.Hkv, kvh = int(blockIdx.x) - wg * a.pool.Hkv;
+  const int wg = block / a.pool.Hkv, kvh = block - wg * a.pool.Hkv;
   PagedShape shapes = {};
   if (lane < a.pb.B) shapes = paged_shape(a, lane);
   const PagedFlat flat = paged_flat(a, shapes, lane);
@@ -1093,6 +1119,30 @@ __global__ __launch_bounds__(256) void paged_token_kernel(PagedKernelArgs a) {
   }
 }
 
+// --------------------------------------------------------------- kernels
+
+template <int HD, bool E8>
+__global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedKernelArgs a) {
+  __shared__ __attribute__((aligned(16))) char smem[kChunkLds<HD>];
+  paged_chunk<HD, E8>(a, blockIdx.x, smem);
+}
+template <int HD, bool E8, int NR>
+__global__ __launch_bounds__(256) void paged_token_kernel(PagedKernelArgs a) {
+  __shared__ __attribute__((aligned(16))) char smem[kTokenLds<HD, NR>];
+  paged_token<HD, E8, NR>(a, blockIdx.x, smem);
+}
+// Both, for batches that may have either: the chunks' workgroups first (their
+// work is longer), the tokens' beside them. One after the other they took 60
+// us where 24 sequences, six of them with chunks, take 49 this way.
+template <int HD, bool E8>
+__global__ __launch_bounds__(256, 2) void paged_mixed_kernel(PagedKernelArgs chunks, PagedKernelArgs tokens) {
+  constexpr int kLds = kChunkLds<HD> > kTokenLds<HD, 1> ? kChunkLds<HD> : kTokenLds<HD, 1>;
+  __shared__ __attribute__((aligned(16))) char smem[kLds];
+  const int first = chunks.items * chunks.pool.Hkv;
+  if (int(blockIdx.x) < first) paged_chunk<HD, E8>(chunks, blockIdx.x, smem);
+  else paged_token<HD, E8, 1>(tokens, int(blockIdx.x) - first, smem);
+}
+
 // -------------------------------------------------------------------- fp32
 
 // fp32 on the fp32 matrix cores: a workgroup takes 16 rows, its four waves
@@ -1162,7 +1212,7 @@ __global__ __launch_bounds__(256) void paged_f32_kernel(PagedKernelArgs a) {
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
         const int64_t vr = row + 4 * s + grp;
-        float* v = vf[4 * kb + s];
+        float v[DPL];
         if constexpr (E8) {
           const float sv = paged_scale(a.pool.ve[vr]);
           const uint8_t* vp = static_cast<const uint8_t*>(a.pool.v) + vr * HD + DPL * r16;
@@ -1194,10 +1244,9 @@ __global__ __launch_bounds__(256) void paged_f32_kernel(PagedKernelArgs a) {
           }
         }
         // whatever lies behind the sequence's last slot is none of its values
-        if (key0 + 16 * kb + 4 * s + grp >= w.end) {
+        const bool mine = key0 + 16 * kb + 4 * s + grp < w.end;
 #pragma unroll
-          for (int e = 0; e < DPL; ++e) v[e] = 0.f;
-        }
+        for (int e = 0; e < DPL; ++e) vf[4 * kb + s][e] = mine ? v[e] : 0.f;
       }
     }
     float sc[2][4];
@@ -1362,78 +1411,97 @@ __device__ __forceinline__ void paged_join_row(const PagedKernelArgs& a, int64_t
   }
 }
 
-// A workgroup takes R rows of one tile and kv head, a thread four dims of a
-// row. Tiles that one workgroup had to itself are done already. FLAT: shares
-// of the line, else splits.
-template <int HD, typename T, bool FLAT, int R>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedKernelArgs a) {
+// A workgroup takes kJoinRows rows of one tile and kv head at a time, a
+// thread four dims of a row, and goes on to every blocks-th such part. Tiles
+// that one workgroup had to itself are done already. FLAT: shares of the
+// line, else splits.
+constexpr int kJoinRows = 16;
+constexpr int kJoinBlocks = 1024;
+template <int HD, typename T, bool FLAT>
+__device__ __forceinline__ void paged_join(const PagedKernelArgs& a, int block, int blocks) {
   const int tid = threadIdx.x, lane = tid & 63;
-  int tile = int(blockIdx.x) / a.pool.Hkv;
-  const int kvh = int(blockIdx.x) - tile * a.pool.Hkv;
-  PagedShape w = {};
-  if (lane < a.pb.B) w = paged_shape(a, lane);
+  PagedShape w0 = {};
+  if (lane < a.pb.B) w0 = paged_shape(a, lane);
   PagedFlat flat = {};
   int per = 0;
   if constexpr (FLAT) {
-    flat = paged_flat(a, w, lane);
+    flat = paged_flat(a, w0, lane);
     if (flat.whole) return;
   } else {
-    per = paged_split_blocks(a, w, lane);
+    per = paged_split_blocks(a, w0, lane);
+    // no sequence is split
+    if (a.pb.B <= 64 && !__builtin_amdgcn_ballot_w64(w0.tiles > 0 && paged_splits(w0, per) > 1)) return;
   }
-  // the sequence that has the tile, and where its items (FLAT: units) begin
-  PagedShape s = {};
-  int first = 0, b = -1, each = 0;
-  for (int b0 = 0; b0 < a.pb.B; b0 += 64) {
-    if (b0) {
-      w = PagedShape{};
-      if (b0 + lane < a.pb.B) w = paged_shape(a, b0 + lane);
+  const int parts = (1 << a.bm_shift) / kJoinRows;
+  for (int unit = block;; unit += blocks) {
+    int tile = unit / parts / a.pool.Hkv;
+    const int part = unit % parts, kvh = unit / parts - tile * a.pool.Hkv;
+    // the sequence that has the tile, and where its items (FLAT: units) begin
+    PagedShape w = w0, s = {};
+    int first = 0, b = -1, each = 0;
+    for (int b0 = 0; b0 < a.pb.B; b0 += 64) {
+      if (b0) {
+        w = PagedShape{};
+        if (b0 + lane < a.pb.B) w = paged_shape(a, b0 + lane);
+      }
+      const int n = FLAT ? paged_units(a, w) : paged_splits(w, per);
+      const int c = FLAT ? w.tiles * n : min(w.tiles * n, a.items);
+      const int tend = wave_prefix(w.tiles), end = wave_prefix(c);
+      const uint64_t over = __builtin_amdgcn_ballot_w64(tend > tile);
+      if (over) {
+        const int l = __builtin_ctzll(over);
+        b = b0 + l;
+        s = shape_of(w, l);
+        each = __builtin_amdgcn_readlane(n, l);
+        tile -= __builtin_amdgcn_readlane(tend, l) - __builtin_amdgcn_readlane(w.tiles, l);
+        first += __builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(c, l);
+        break;
+      }
+      tile -= __builtin_amdgcn_readlane(tend, 63);
+      first += __builtin_amdgcn_readlane(end, 63);
+      if (!FLAT) first = min(first, a.items);
     }
-    const int n = FLAT ? paged_units(a, w) : paged_splits(w, per);
-    const int c = FLAT ? w.tiles * n : min(w.tiles * n, a.items);
-    const int tend = wave_prefix(w.tiles), end = wave_prefix(c);
-    const uint64_t over = __builtin_amdgcn_ballot_w64(tend > tile);
-    if (over) {
-      const int l = __builtin_ctzll(over);
-      b = b0 + l;
-      s = shape_of(w, l);
-      each = __builtin_amdgcn_readlane(n, l);
-      tile -= __builtin_amdgcn_readlane(tend, l) - __builtin_amdgcn_readlane(w.tiles, l);
-      first += __builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(c, l);
-      break;
+    if (b < 0) return;  // past the last tile
+    int n;
+    int64_t at0, at1, step;  // places, in tiles
+    if constexpr (FLAT) {
+      const int j0 = flat.of(first + tile * each), j1 = flat.of(first + tile * each + each - 1);
+      n = j1 - j0 + 1;
+      if (n <= 1 || j0 < 0 || j1 >= a.items) continue;
+      at0 = int64_t(2 * j0 + 1) * a.pool.Hkv + kvh;
+      at1 = int64_t(2 * j0) * a.pool.Hkv + kvh;
+      step = 2 * a.pool.Hkv;
+    } else {
+      if (each == 1) continue;
+      int begin, stop;
+      paged_range(a, s, tile, 0, kNoSplit << 6, &begin, &stop);
+      const int len = per << 6, i0 = (begin - s.lo) / len, i1 = stop > begin ? (stop - s.lo + len - 1) / len : i0;
+      n = i1 - i0;
+      const int item = first + i0 * s.tiles + (s.tiles - 1 - tile);
+      // tables that claim more items than the launch has (row_start not ascending) end here
+      if (item < 0 || item + int64_t(max(n - 1, 0)) * s.tiles >= a.items) continue;
+      at0 = at1 = int64_t(item) * a.pool.Hkv + kvh;
+      step = int64_t(s.tiles) * a.pool.Hkv;
     }
-    tile -= __builtin_amdgcn_readlane(tend, 63);
-    first += __builtin_amdgcn_readlane(end, 63);
-    if (!FLAT) first = min(first, a.items);
+    for (int e = tid; e < kJoinRows * (HD / 4); e += 256) {
+      const int row = part * kJoinRows + e / (HD / 4), d = e % (HD / 4) * 4, m = (tile << a.bm_shift) + row;
+      if (m >= s.M) break;
+      const int tok = m / a.G, g = m - tok * a.G;
+      paged_join_row<HD, T>(a, (at0 << a.bm_shift) + row, (at1 << a.bm_shift) + row, step << a.bm_shift, n, d,
+                            static_cast<T*>(a.out) + int64_t(s.row0 + tok) * a.o_row + int64_t(kvh * a.G + g) * a.o_head + d);
+    }
   }
-  if (b < 0) return;
-  int n;
-  int64_t at0, at1, step;  // places, in tiles
-  if constexpr (FLAT) {
-    const int j0 = flat.of(first + tile * each), j1 = flat.of(first + tile * each + each - 1);
-    n = j1 - j0 + 1;
-    if (n <= 1 || j0 < 0 || j1 >= a.items) return;
-    at0 = int64_t(2 * j0 + 1) * a.pool.Hkv + kvh;
-    at1 = int64_t(2 * j0) * a.pool.Hkv + kvh;
-    step = 2 * a.pool.Hkv;
-  } else {
-    if (each == 1) return;
-    int begin, stop;
-    paged_range(a, s, tile, 0, kNoSplit << 6, &begin, &stop);
-    const int len = per << 6, i0 = (begin - s.lo) / len, i1 = stop > begin ? (stop - s.lo + len - 1) / len : i0;
-    n = i1 - i0;
-    const int item = first + i0 * s.tiles + (s.tiles - 1 - tile);
-    // tables that claim more items than the launch has (row_start not ascending) end here
-    if (item < 0 || item + int64_t(max(n - 1, 0)) * s.tiles >= a.items) return;
-    at0 = at1 = int64_t(item) * a.pool.Hkv + kvh;
-    step = int64_t(s.tiles) * a.pool.Hkv;
-  }
-  for (int e = tid; e < R * (HD / 4); e += 256) {
-    const int row = int(blockIdx.y) * R + e / (HD / 4), d = e % (HD / 4) * 4, m = (tile << a.bm_shift) + row;
-    if (m >= s.M) break;
-    const int tok = m / a.G, g = m - tok * a.G;
-    paged_join_row<HD, T>(a, (at0 << a.bm_shift) + row, (at1 << a.bm_shift) + row, step << a.bm_shift, n, d,
-                          static_cast<T*>(a.out) + int64_t(s.row0 + tok) * a.o_row + int64_t(kvh * a.G + g) * a.o_head + d);
-  }
+}
+
+template <int HD, typename T, bool FLAT>
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedKernelArgs a) {
+  paged_join<HD, T, FLAT>(a, blockIdx.x, gridDim.x);
+}
+// The chunks' tiles by `first` workgroups, the tokens' by the others.
+template <int HD>
+__global__ __launch_bounds__(256) void paged_mixed_join_kernel(PagedKernelArgs chunks, PagedKernelArgs tokens, int first) {
+  if (int(blockIdx.x) < first) paged_join<HD, uint16_t, false>(chunks, blockIdx.x, first);
+  else paged_join<HD, uint16_t, true>(tokens, int(blockIdx.x) - first, int(gridDim.x) - first);
 }
 
 // ------------------------------------------------------------------ launch
@@ -1454,7 +1522,7 @@ struct PagedPlan {
 
 constexpr int kTokenRows = 64;       // rows of a sequence (tokens times heads) the token kernel takes
 constexpr int kChunkItems = 512;     // workgroups aimed at, of all kv heads
-constexpr int kF32Items = 512;
+constexpr int kF32Items = 768;
 constexpr int kSplitMinBlocks = 4;   // 256 slots
 
 // Workgroups of the token kernel that a CU holds, for 16, 32 and 64 rows.
@@ -1535,58 +1603,68 @@ hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t s) {
   PagedPlan p[2];
   paged_plans(a.dtype, a.Hq, a.pool, a.pb, p);
   char* ws = static_cast<char*>(a.workspace);
+  PagedKernelArgs k[2];
+  unsigned grid[2] = {}, joins[2] = {};
   for (int i = 0; i < 2; ++i) {
     if (!p[i].on) continue;
-    PagedKernelArgs k;
-    k.pool = a.pool;
-    k.pb = a.pb;
-    k.q = a.q;
-    k.q_row = a.q_row;
-    k.q_head = a.q_head;
-    k.out = a.out;
-    k.o_row = a.o_row;
-    k.o_head = a.o_head;
-    k.G = a.Hq / a.pool.Hkv;
-    k.window = a.window;
-    k.bm_shift = p[i].bm_shift;
-    k.m_lo = p[i].m_lo;
-    k.m_hi = p[i].m_hi;
-    k.items = p[i].items;
-    k.target = p[i].target;
-    k.split_min = kSplitMinBlocks;
-    k.unit_shift = p[i].unit_shift;
-    k.part_o = reinterpret_cast<float*>(ws);
-    k.part_ml = reinterpret_cast<float2*>(ws + align256(plan_rows(p[i], a.pool.Hkv) * a.pool.hd * 4));
+    k[i].pool = a.pool;
+    k[i].pb = a.pb;
+    k[i].q = a.q;
+    k[i].q_row = a.q_row;
+    k[i].q_head = a.q_head;
+    k[i].out = a.out;
+    k[i].o_row = a.o_row;
+    k[i].o_head = a.o_head;
+    k[i].G = a.Hq / a.pool.Hkv;
+    k[i].window = a.window;
+    k[i].bm_shift = p[i].bm_shift;
+    k[i].m_lo = p[i].m_lo;
+    k[i].m_hi = p[i].m_hi;
+    k[i].items = p[i].items;
+    k[i].target = p[i].target;
+    k[i].split_min = kSplitMinBlocks;
+    k[i].unit_shift = p[i].unit_shift;
+    k[i].part_o = reinterpret_cast<float*>(ws);
+    k[i].part_ml = reinterpret_cast<float2*>(ws + align256(plan_rows(p[i], a.pool.Hkv) * a.pool.hd * 4));
     ws += plan_bytes(p[i], a.pool);
-    const unsigned grid = unsigned(p[i].items) * a.pool.Hkv;
-    auto run = [&](auto hdc, auto e8c) -> hipError_t {
-      constexpr int HD = decltype(hdc)::value;
-      constexpr bool E8 = decltype(e8c)::value;
-      if (a.dtype == DSF_F32) paged_f32_kernel<HD, E8><<<grid, 256, 0, s>>>(k);
-      else if (i == 1) paged_chunk_kernel<HD, E8><<<grid, 256, 0, s>>>(k);
-      else if (k.bm_shift == 4) paged_token_kernel<HD, E8, 1><<<grid, 256, 0, s>>>(k);
-      else if (k.bm_shift == 5) paged_token_kernel<HD, E8, 2><<<grid, 256, 0, s>>>(k);
-      else paged_token_kernel<HD, E8, 4><<<grid, 256, 0, s>>>(k);
-      const hipError_t e = hipGetLastError();
-      if (e != hipSuccess || !p[i].join) return e;
-      const dim3 jg(unsigned(p[i].tiles) * a.pool.Hkv, (1 << k.bm_shift) / 16);
-      if (a.dtype == DSF_F32) paged_join_kernel<HD, float, false, 16><<<jg, 256, 0, s>>>(k);
-      else if (i == 1) paged_join_kernel<HD, uint16_t, false, 16><<<jg, 256, 0, s>>>(k);
-      else paged_join_kernel<HD, uint16_t, true, 16><<<jg, 256, 0, s>>>(k);
-      return hipGetLastError();
-    };
-    auto run_h = [&](auto e8c) -> hipError_t {
-      switch (a.pool.hd) {
-        case 32: return run(std::integral_constant<int, 32>(), e8c);
-        case 64: return run(std::integral_constant<int, 64>(), e8c);
-        case 128: return run(std::integral_constant<int, 128>(), e8c);
-        default: return hipErrorInvalidValue;
-      }
-    };
-    const hipError_t e = a.pool.codes ? run_h(std::true_type()) : run_h(std::false_type());
-    if (e != hipSuccess) return e;
+    grid[i] = unsigned(p[i].items) * a.pool.Hkv;
+    const int64_t parts = int64_t(p[i].tiles) * a.pool.Hkv * ((1 << p[i].bm_shift) / kJoinRows);
+    joins[i] = p[i].join ? unsigned(std::min<int64_t>(parts, kJoinBlocks)) : 0;
   }
-  return hipSuccess;
+  auto run = [&](auto hdc, auto e8c) -> hipError_t {
+    constexpr int HD = decltype(hdc)::value;
+    constexpr bool E8 = decltype(e8c)::value;
+    if (a.dtype == DSF_F32) {
+      paged_f32_kernel<HD, E8><<<grid[1], 256, 0, s>>>(k[1]);
+      if (joins[1]) paged_join_kernel<HD, float, false><<<joins[1], 256, 0, s>>>(k[1]);
+      return hipGetLastError();
+    }
+    if (p[0].on && p[1].on && p[0].bm_shift == 4) {
+      paged_mixed_kernel<HD, E8><<<grid[0] + grid[1], 256, 0, s>>>(k[1], k[0]);
+      if (joins[0] + joins[1]) paged_mixed_join_kernel<HD><<<joins[0] + joins[1], 256, 0, s>>>(k[1], k[0], int(joins[1]));
+      return hipGetLastError();
+    }
+    if (p[1].on) {
+      paged_chunk_kernel<HD, E8><<<grid[1], 256, 0, s>>>(k[1]);
+      if (joins[1]) paged_join_kernel<HD, uint16_t, false><<<joins[1], 256, 0, s>>>(k[1]);
+    }
+    if (p[0].on) {
+      if (p[0].bm_shift == 4) paged_token_kernel<HD, E8, 1><<<grid[0], 256, 0, s>>>(k[0]);
+      else if (p[0].bm_shift == 5) paged_token_kernel<HD, E8, 2><<<grid[0], 256, 0, s>>>(k[0]);
+      else paged_token_kernel<HD, E8, 4><<<grid[0], 256, 0, s>>>(k[0]);
+      if (joins[0]) paged_join_kernel<HD, uint16_t, true><<<joins[0], 256, 0, s>>>(k[0]);
+    }
+    return hipGetLastError();
+  };
+  auto run_h = [&](auto e8c) -> hipError_t {
+    switch (a.pool.hd) {
+      case 32: return run(std::integral_constant<int, 32>(), e8c);
+      case 64: return run(std::integral_constant<int, 64>(), e8c);
+      case 128: return run(std::integral_constant<int, 128>(), e8c);
+      default: return hipErrorInvalidValue;
+    }
+  };
+  return a.pool.codes ? run_h(std::true_type()) : run_h(std::false_type());
 }
 
 }  // namespace dsf
