@@ -48,8 +48,8 @@ __device__ __forceinline__ int wave_prefix(int v) {
   return v;
 }
 
-// How sequence b's work is cut: `tiles` tiles of BM rows, slots from `lo` (a
-// multiple of 64) to kv in splits of `len`.
+// A sequence's work: `tiles` tiles of BM rows, slots from `lo` (a multiple of
+// 64) to kv, of which a tile sees no more than `blocks` blocks of 64.
 struct PagedShape {
   int n, row0, kv;  // rows, first row, slots
   int M;            // rows * G that take part
@@ -66,6 +66,7 @@ __device__ __forceinline__ PagedShape paged_shape(const PagedKernelArgs& a, int 
   w.tiles = w.M > a.m_lo && w.M <= a.m_hi ? min((w.M + (1 << a.bm_shift) - 1) >> a.bm_shift, a.items) : 0;
   w.lo = a.window ? max(s.kv - s.n - a.window + 1, 0) & ~63 : 0;
   w.blocks = (max(s.kv - w.lo, 0) + 63) >> 6;
+  if (a.window) w.blocks = min(w.blocks, (min(a.window, w.kv) + ((1 << a.bm_shift) - 1) / a.G + 64 + 63) >> 6);
   return w;
 }
 // Lane l's shape, in every lane.
@@ -78,12 +79,12 @@ struct PagedItem {
   int b;       // -1: none
   int first;   // the sequence's first item
   int local;   // this one's number among them
-  int len;     // slots per split
-  int splits;  // of the sequence
+  int splits;  // of each of the sequence's tiles
 };
 constexpr int kNoSplit = 1 << 19;  // blocks: more slots than a sequence may have
+// A tile's blocks go to its splits evenly, so that they end at the same time.
 __device__ __forceinline__ int paged_splits(const PagedShape& w, int per) { return max((w.blocks + per - 1) / per, 1); }
-// Blocks of 64 slots per split. All the work (tiles times blocks) over the
+// Blocks of 64 slots per split, at most. All the work (tiles times blocks) over the
 // number of items aimed at: a longer item would outlast the others. Where
 // there are fewer tiles than that, so many longer that the items are no more:
 // one round of workgroups, and a few in a second would double the time.
@@ -130,7 +131,6 @@ __device__ __forceinline__ PagedItem paged_item(const PagedKernelArgs& a, int it
       it.b = b0 + l;
       it.first = first + __builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(c, l);
       it.local = item - it.first;
-      it.len = per << 6;
       it.splits = __builtin_amdgcn_readlane(splits, l);
       it.w = shape_of(w, l);
       return it;
@@ -159,10 +159,17 @@ struct PagedFlat {
 __device__ __forceinline__ int paged_units(const PagedKernelArgs& a, const PagedShape& w) {  // of a tile
   return max((max(w.kv - w.lo, 0) + (1 << a.unit_shift) - 1) >> a.unit_shift, 1);
 }
+// Largest of the wave's numbers (none negative), in every lane.
 __device__ __forceinline__ int wave_most(int v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = max(v, __shfl_xor(v, o, 64));
-  return v;
+#define DSF_SCAN(ctrl, rows) v = max(v, __builtin_amdgcn_update_dpp(0, v, ctrl, rows, 0xf, false))
+  DSF_SCAN(0x111, 0xf);
+  DSF_SCAN(0x112, 0xf);
+  DSF_SCAN(0x114, 0xf);
+  DSF_SCAN(0x118, 0xf);
+  DSF_SCAN(0x142, 0xa);
+  DSF_SCAN(0x143, 0xc);
+#undef DSF_SCAN
+  return __builtin_amdgcn_readlane(v, 63);
 }
 __device__ __forceinline__ PagedFlat paged_flat(const PagedKernelArgs& a, const PagedShape& w, int lane) {
   int units = w.tiles ? w.tiles * paged_units(a, w) : 0, tiles = w.tiles, most = w.tiles ? paged_units(a, w) : 0;
@@ -179,7 +186,7 @@ __device__ __forceinline__ PagedFlat paged_flat(const PagedKernelArgs& a, const 
   }
   units = __builtin_amdgcn_readlane(wave_prefix(units), 63);
   tiles = __builtin_amdgcn_readlane(wave_prefix(tiles), 63);
-  most = __builtin_amdgcn_readfirstlane(wave_most(most));
+  most = wave_most(most);
   PagedFlat f;
   f.whole = most << a.unit_shift <= kWholeUnits << 6 && tiles <= a.items;
   f.wgs = f.whole ? tiles : min(max(units / kLeastUnits, 1), a.items);
@@ -215,25 +222,27 @@ __device__ __forceinline__ PagedSpot paged_spot(const PagedKernelArgs& a, PagedS
   return PagedSpot{PagedShape{}, -1, 0, 0, 0};
 }
 
-// One item's tile and slots. Splits outermost: the tiles of one split read
+// One item's tile and slots. Splits outermost: neighbouring tiles read about
 // the same slots at the same time; within a split the last tile, which sees
 // the most, is the first.
 struct PagedWork {
-  int b, n, row0, kv, M, lo;
+  int b, n, row0, kv, M;
   int tile;            // of BM rows
   int p0;              // slot of the sequence's first row (may be negative)
   int begin, end;      // slots of this item that some row of the tile sees
   int splits;
 };
-__device__ __forceinline__ void paged_range(const PagedKernelArgs& a, const PagedShape& w, int tile, int split, int len,
-                                            int* begin, int* end) {
+// Slots that some row of the tile sees: from a multiple of 64.
+__device__ __forceinline__ void paged_range(const PagedKernelArgs& a, const PagedShape& w, int tile, int* begin, int* end) {
   const int p0 = w.kv - w.n;
   const int m0 = tile << a.bm_shift, m1 = min(m0 + (1 << a.bm_shift), w.M) - 1;
-  int e = p0 + m1 / a.G + 1, s = a.window ? max(p0 + m0 / a.G - a.window + 1, 0) : 0;
-  s = max(s & ~63, w.lo + split * len);
-  e = min(e, min(w.kv, w.lo + (split + 1) * len));
+  const int s = a.window ? max(p0 + m0 / a.G - a.window + 1, 0) & ~63 : 0;
   *begin = s;
-  *end = max(e, s);
+  *end = max(min(p0 + m1 / a.G + 1, w.kv), s);
+}
+// Slots per split of such a range (0: there are none).
+__device__ __forceinline__ int paged_split_len(int begin, int end, int splits) {
+  return (((end - begin + 63) >> 6) + splits - 1) / splits << 6;
 }
 __device__ __forceinline__ PagedWork paged_work(const PagedKernelArgs& a, const PagedItem& it) {
   PagedWork k;
@@ -243,12 +252,14 @@ __device__ __forceinline__ PagedWork paged_work(const PagedKernelArgs& a, const 
   k.row0 = w.row0;
   k.kv = w.kv;
   k.M = w.M;
-  k.lo = w.lo;
   k.p0 = w.kv - w.n;
   const int split = it.local / w.tiles;
   k.tile = w.tiles - 1 - (it.local - split * w.tiles);
   k.splits = it.splits;
-  paged_range(a, w, k.tile, split, it.len, &k.begin, &k.end);
+  paged_range(a, w, k.tile, &k.begin, &k.end);
+  const int len = paged_split_len(k.begin, k.end, it.splits);
+  k.begin = min(k.begin + split * len, k.end);
+  k.end = min(k.begin + len, k.end);
   return k;
 }
 
@@ -305,6 +316,27 @@ struct SlotTile {
 
 #define DSF_INLINE __attribute__((always_inline))  // for lambdas over register arrays
 
+// N DMA instructions of a wave: lane l of the e-th brings the 16 bytes at
+// offset(e) of `src` to lds + 1024 e + 16 l, zeros for those past `bytes`.
+template <int N, typename F>
+__device__ __forceinline__ void lds_dma(const char* src, int bytes, char* lds, F offset) {
+  auto uniform = [](uint32_t x) { return uint32_t(__builtin_amdgcn_readfirstlane(int(x))); };
+  const uint64_t base = reinterpret_cast<uint64_t>(src);
+  // buffer resource: base, no stride, size, raw 32-bit format
+  const u32x4 rsrc = {uniform(uint32_t(base)), uniform(uint32_t(base >> 32) & 0xffffu), uniform(uint32_t(bytes)),
+                      0x00020000u};
+  const uint32_t at = uniform(uint32_t(size_t((__attribute__((address_space(3))) char*)lds)));
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+    asm volatile(
+        "s_mov_b32 m0, %0\n\t"
+        "s_nop 0\n\t"
+        "buffer_load_dwordx4 %1, %2, 0 offen lds"
+        :
+        : "s"(at + 1024 * e), "v"(offset(e)), "s"(rsrc)
+        : "memory");
+}
+
 // 16 slots from `slot` on of one kv head to LDS at `lds` (a tile's row 16 i):
 // bf16 by DMA, each lane 16 bytes at a time; slots at or past `end` become
 // zeros. All 16 lie in one page.
@@ -313,31 +345,27 @@ struct DmaSlots {
   __device__ static __forceinline__ void load(const void* pool, const PagedKernelArgs& a, int page, int kvh, int slot,
                                               int end, char* lds, int lane) {
     using S = SlotTile<HD>;
-    const int mask = (1 << a.pb.page_shift) - 1;
-    const int64_t row = ((int64_t(page) * a.pool.Hkv + kvh) << a.pb.page_shift) + (slot & mask);
-    const uint64_t base = reinterpret_cast<uint64_t>(pool) + row * S::kRowBytes;
-    // buffer resource: base, no stride, the bytes of the slots that count, raw 32-bit format
-    auto uniform = [](uint32_t x) { return uint32_t(__builtin_amdgcn_readfirstlane(int(x))); };
-    const u32x4 rsrc = {uniform(uint32_t(base)), uniform(uint32_t(base >> 32) & 0xffffu),
-                        uniform(uint32_t(min(max(end - slot, 0), 16) * S::kRowBytes)), 0x00020000u};
-    const uint32_t at = uniform(uint32_t(size_t((__attribute__((address_space(3))) char*)lds)));
-#pragma unroll
-    for (int e = 0; e < 16 * S::kRowBytes / 1024; ++e) {
-      const int byte = 1024 * e + 16 * lane;
-      const int r = byte / S::kRowBytes, c = byte % S::kRowBytes / 16;
-      asm volatile(
-          "s_mov_b32 m0, %0\n\t"
-          "s_nop 0\n\t"
-          "buffer_load_dwordx4 %1, %2, 0 offen lds"
-          :
-          : "s"(at + 1024 * e), "v"(r * S::kRowBytes + ((c ^ S::swz(r)) << 4)), "s"(rsrc)
-          : "memory");
-    }
+    const int64_t row = ((int64_t(page) * a.pool.Hkv + kvh) << a.pb.page_shift) + (slot & ((1 << a.pb.page_shift) - 1));
+    lds_dma<16 * S::kRowBytes / 1024>(static_cast<const char*>(pool) + row * S::kRowBytes,
+                                      min(max(end - slot, 0), 16) * S::kRowBytes, lds, [lane](int e) {
+                                        const int byte = 1024 * e + 16 * lane;
+                                        const int r = byte / S::kRowBytes, c = byte % S::kRowBytes / 16;
+                                        return r * S::kRowBytes + ((c ^ S::swz(r)) << 4);
+                                      });
   }
 };
 
-// The same of e4m3 codes: loaded into registers, 16 codes of a slot at a
-// time, and later widened into the tile.
+// 16 slots of e4m3 codes as they are, to `lds` (at least 1 KB).
+template <int HD>
+__device__ __forceinline__ void codes16_dma(const void* pool, const PagedKernelArgs& a, int page, int kvh, int slot, int end,
+                                            char* lds, int lane) {
+  const int64_t row = ((int64_t(page) * a.pool.Hkv + kvh) << a.pb.page_shift) + (slot & ((1 << a.pb.page_shift) - 1));
+  lds_dma<(16 * HD + 1023) / 1024>(static_cast<const char*>(pool) + row * HD, min(max(end - slot, 0), 16) * HD, lds,
+                                   [lane](int e) { return 1024 * e + 16 * lane; });
+}
+
+// e4m3 codes in registers, 16 of a slot at a time, and their widening into
+// the tile.
 template <int HD>
 struct CodeSlots {
   static constexpr int kCpr = HD / 16;                       // 16-byte loads per slot
@@ -357,6 +385,12 @@ struct CodeSlots {
     for (int i = 0; i < kLoads; ++i)
       c[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rc, 1024 * i + 16 * lane, 0, 0));
     e = __builtin_amdgcn_raw_buffer_load_b8(re, lane & 15, 0, 0);
+  }
+  // what codes16_dma brought; `exps`: the exponent byte of slot lane & 15
+  __device__ __forceinline__ void read(const char* lds, uint32_t exps, int lane) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) c[i] = *reinterpret_cast<const u32x4*>(lds + 1024 * i + 16 * lane);
+    e = exps;
   }
   __device__ __forceinline__ void store(char* lds, int lane) const {
     using S = SlotTile<HD>;
@@ -442,8 +476,11 @@ __device__ __forceinline__ float not_finite_sum(float c) {
 //
 // DMA into LDS is issued in inline assembly: the compiler, which cannot tell
 // the stages apart, would wait for it before every transpose load.
+// LDS: two tiles of keys, two of values; e4m3: each wave's codes of a tile of either.
 template <int HD>
-constexpr int kChunkLds = 4 * 64 * SlotTile<HD>::kRowBytes;  // two tiles of keys, two of values
+constexpr int kCodeBytes = 16 * HD > 1024 ? 16 * HD : 1024;
+template <int HD, bool E8>
+constexpr int kChunkLds = 4 * 64 * SlotTile<HD>::kRowBytes + (E8 ? 8 * kCodeBytes<HD> : 0);
 template <int HD, bool E8>
 __device__ __forceinline__ void paged_chunk(const PagedKernelArgs& a, int block, char* smem) {
   using S = SlotTile<HD>;
@@ -492,27 +529,46 @@ __device__ __forceinline__ void paged_chunk(const PagedKernelArgs& a, int block,
   PagedTable tab;
   tab.load(a, w.b, w.begin >> a.pb.page_shift, lane);
   PagedTable vtab = tab;  // values are a tile behind
-  CodeSlots<HD> codes;
   char* const mine = smem + 16 * wave * S::kRowBytes;
+  char* const raw = smem + 4 * kTile + 2 * wave * kCodeBytes<HD>;  // keys' codes, then values'
+  uint32_t ke = 0, ve = 0;  // exponent bytes of the codes there, of slot lane & 15
+  auto exponents = [&](const uint8_t* exps, int page, int slot) DSF_INLINE {
+    const int64_t row = ((int64_t(page) * a.pool.Hkv + kvh) << a.pb.page_shift) + (slot & ((1 << a.pb.page_shift) - 1));
+    return uint32_t(slot + (lane & 15) < w.end ? exps[row + (lane & 15)] : 0);
+  };
   auto fetch_k = [&](int t) DSF_INLINE {
     const int slot = s0 + 64 * t, page = tab.at(a, w.b, slot >> a.pb.page_shift, lane);
-    if constexpr (E8) codes.load(a.pool.k, a.pool.ke, a, page, kvh, slot, w.end, lane);
-    else DmaSlots<HD>::load(a.pool.k, a, page, kvh, slot, w.end, mine + (t & 1) * kTile, lane);
+    if constexpr (E8) {
+      ke = exponents(a.pool.ke, page, slot);
+      codes16_dma<HD>(a.pool.k, a, page, kvh, slot, w.end, raw, lane);
+    } else {
+      DmaSlots<HD>::load(a.pool.k, a, page, kvh, slot, w.end, mine + (t & 1) * kTile, lane);
+    }
   };
   auto fetch_v = [&](int t) DSF_INLINE {
     const int slot = s0 + 64 * t, page = vtab.at(a, w.b, slot >> a.pb.page_shift, lane);
-    if constexpr (E8) codes.load(a.pool.v, a.pool.ve, a, page, kvh, slot, w.end, lane);
-    else DmaSlots<HD>::load(a.pool.v, a, page, kvh, slot, w.end, mine + (2 + (t & 1)) * kTile, lane);
+    if constexpr (E8) {
+      ve = exponents(a.pool.ve, page, slot);
+      codes16_dma<HD>(a.pool.v, a, page, kvh, slot, w.end, raw + kCodeBytes<HD>, lane);
+    } else {
+      DmaSlots<HD>::load(a.pool.v, a, page, kvh, slot, w.end, mine + (2 + (t & 1)) * kTile, lane);
+    }
   };
-  auto store_k = [&](int t) DSF_INLINE {
-    if constexpr (E8) codes.store(mine + (t & 1) * kTile, lane);
+  // e4m3: the codes fetched last, widened into tile t's stage
+  auto widen = [&](int t, bool values) DSF_INLINE {
+    CodeSlots<HD> x;
+    x.read(raw + (values ? kCodeBytes<HD> : 0), values ? ve : ke, lane);
+    x.store(mine + ((values ? 2 : 0) + (t & 1)) * kTile, lane);
   };
-  auto store_v = [&](int t) DSF_INLINE {
-    if constexpr (E8) codes.store(mine + (2 + (t & 1)) * kTile, lane);
+  constexpr int kTileDma = 16 * S::kRowBytes / 1024;  // DMA instructions of fetch_k, of fetch_v (bf16)
+  auto meet = [&]() DSF_INLINE {                      // what every wave has written to LDS is there for all
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
   };
-  auto landed = [&]() DSF_INLINE {  // what this wave has staged, then what all have
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    __syncthreads();
+  auto landed = [&]() DSF_INLINE {  // and what every wave has fetched
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    meet();
   };
 
   // LDS addresses: rows r32 (+ 32 half) of a key tile, chunk 2 st + hi; of a value tile lane (group of 16 G, a4 =
@@ -634,7 +690,7 @@ __device__ __forceinline__ void paged_chunk(const PagedKernelArgs& a, int block,
   // operands are read kAhead products of a kind ahead.
   auto half_turn = [&](int kat, f32x16& s_next, f32x16& s_now, bf16x8 (&p_now)[2], int vat,
                        const bf16x8 (&p_last)[2]) DSF_INLINE {
-    constexpr int kPairs = NS, kSteps = 12, kAhead = E8 ? 1 : 2;  // NS == 2 ND: as many products of either kind
+    constexpr int kPairs = NS, kSteps = 12, kAhead = 2;  // NS == 2 ND: as many products of either kind
     Soft f = {};
     bf16x8 kf[kAhead + 1], vf[kAhead + 1];
     auto next_k = [&](int i) DSF_INLINE { kf[i % (kAhead + 1)] = read_k(kat, i); };
@@ -675,31 +731,46 @@ __device__ __forceinline__ void paged_chunk(const PagedKernelArgs& a, int block,
     bf16x8 p0[2], p1[2];
     Soft f = {};
     fetch_k(0);
-    store_k(0);
-    landed();
-    if (nt > 1) fetch_k(1);
-    if (!E8) fetch_v(0);
+    if constexpr (E8) {
+      fetch_v(0);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      widen(0, false);
+      widen(0, true);
+      if (nt > 1) {
+        fetch_k(1);
+        fetch_v(1);
+      }
+    } else {
+      fetch_v(0);
+      if (nt > 1) fetch_k(1);
+      // the first keys
+      if (nt > 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kTileDma) : "memory");
+      else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kTileDma) : "memory");
+    }
+    meet();
     scores(0, 0, s0x);
     scores(0, 1, s1);
-    if (nt > 1) store_k(1);
-    if (E8) fetch_v(0);
     hide(0, 0, s0x);
     soft_all(f, s0x, p0);
     settle(f);
-    store_v(0);
-    // At the start of turn t: p0 and s1 of tile t. Keys of tile t + 1 and values of tile t have landed then, and
-    // the other stages are free. Codes go through the same registers, keys in a turn's first half, values in its second.
+    if constexpr (E8) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      if (nt > 1) widen(1, false);
+      if (nt > 2) fetch_k(2);
+    }
+    // At the start of turn t: p0 and s1 of tile t. Keys of tile t + 1 and values of tile t are in LDS then, and the
+    // other stages are free: for what comes by DMA in this turn, or (e4m3) for the codes that came in the last one.
     auto open = [&](int t) DSF_INLINE {
       landed();
-      if (t + 2 < nt) fetch_k(t + 2);
-      if (!E8 && t + 1 < nt) fetch_v(t + 1);
-    };
-    auto middle = [&](int t) DSF_INLINE {
-      if (E8 && t + 2 < nt) store_k(t + 2);
-      if (E8 && t + 1 < nt) fetch_v(t + 1);
-    };
-    auto close = [&](int t) DSF_INLINE {
-      if (E8 && t + 1 < nt) store_v(t + 1);
+      if constexpr (E8) {
+        if (t + 2 < nt) widen(t + 2, false);
+        if (t + 1 < nt) widen(t + 1, true);
+        if (t + 3 < nt) fetch_k(t + 3);
+        if (t + 2 < nt) fetch_v(t + 2);
+      } else {
+        if (t + 2 < nt) fetch_k(t + 2);
+        if (t + 1 < nt) fetch_v(t + 1);
+      }
     };
     // turns [t0, t1) have no hidden slot in tiles t and t + 1; they go in pairs from an even one, so that the stages'
     // addresses are constants
@@ -712,14 +783,10 @@ __device__ __forceinline__ void paged_chunk(const PagedKernelArgs& a, int block,
         for (; t + 1 < t1; t += 2) {
           open(t);
           half_turn(kTile, s0x, s1, p1, 0, p0);
-          middle(t);
           half_turn(kTile + kHalf, s1, s0x, p0, kHalf, p1);
-          close(t);
           open(t + 1);
           half_turn(0, s0x, s1, p1, kTile, p0);
-          middle(t + 1);
           half_turn(kHalf, s1, s0x, p0, kTile + kHalf, p1);
-          close(t + 1);
         }
         if (t >= my_nt) break;
       }
@@ -730,7 +797,6 @@ __device__ __forceinline__ void paged_chunk(const PagedKernelArgs& a, int block,
       soft_all(f, s1, p1);
       product(t, 0, p0);
       settle(f);
-      middle(t);
       if (more) {
         scores(t + 1, 1, s1);
         hide(t + 1, 0, s0x);
@@ -738,14 +804,9 @@ __device__ __forceinline__ void paged_chunk(const PagedKernelArgs& a, int block,
       }
       product(t, 1, p1);
       if (more) settle(f);
-      close(t);
       ++t;
     }
-    for (; t < nt; ++t) {  // for the other waves
-      open(t);
-      middle(t);
-      close(t);
-    }
+    for (; t < nt; ++t) open(t);  // for the other waves
   }
 
   // lane holds O^T[dim 32 db + 8 (i / 4) + 4 hi + i % 4][row r32]
@@ -924,7 +985,7 @@ __device__ __forceinline__ void paged_token(const PagedKernelArgs& a, int block,
     const bool before = pos > spot.from, after = until < spot.until;  // shared with the last, the next workgroup
     const PagedShape& w = spot.w;
     int begin, end;
-    paged_range(a, w, spot.tile, 0, kNoSplit << 6, &begin, &end);
+    paged_range(a, w, spot.tile, &begin, &end);
     if (!flat.whole) {
       begin = max(begin, w.lo + ((pos - spot.from) << a.unit_shift));
       end = max(min(end, w.lo + ((until - spot.from) << a.unit_shift)), begin);
@@ -1123,7 +1184,7 @@ __device__ __forceinline__ void paged_token(const PagedKernelArgs& a, int block,
 
 template <int HD, bool E8>
 __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedKernelArgs a) {
-  __shared__ __attribute__((aligned(16))) char smem[kChunkLds<HD>];
+  __shared__ __attribute__((aligned(16))) char smem[kChunkLds<HD, E8>];
   paged_chunk<HD, E8>(a, blockIdx.x, smem);
 }
 template <int HD, bool E8, int NR>
@@ -1136,7 +1197,7 @@ __global__ __launch_bounds__(256) void paged_token_kernel(PagedKernelArgs a) {
 // us where 24 sequences, six of them with chunks, take 49 this way.
 template <int HD, bool E8>
 __global__ __launch_bounds__(256, 2) void paged_mixed_kernel(PagedKernelArgs chunks, PagedKernelArgs tokens) {
-  constexpr int kLds = kChunkLds<HD> > kTokenLds<HD, 1> ? kChunkLds<HD> : kTokenLds<HD, 1>;
+  constexpr int kLds = kChunkLds<HD, E8> > kTokenLds<HD, 1> ? kChunkLds<HD, E8> : kTokenLds<HD, 1>;
   __shared__ __attribute__((aligned(16))) char smem[kLds];
   const int first = chunks.items * chunks.pool.Hkv;
   if (int(blockIdx.x) < first) paged_chunk<HD, E8>(chunks, blockIdx.x, smem);
@@ -1474,10 +1535,10 @@ __device__ __forceinline__ void paged_join(const PagedKernelArgs& a, int block, 
     } else {
       if (each == 1) continue;
       int begin, stop;
-      paged_range(a, s, tile, 0, kNoSplit << 6, &begin, &stop);
-      const int len = per << 6, i0 = (begin - s.lo) / len, i1 = stop > begin ? (stop - s.lo + len - 1) / len : i0;
-      n = i1 - i0;
-      const int item = first + i0 * s.tiles + (s.tiles - 1 - tile);
+      paged_range(a, s, tile, &begin, &stop);
+      const int len = paged_split_len(begin, stop, each);
+      n = len ? (stop - begin + len - 1) / len : 0;
+      const int item = first + (s.tiles - 1 - tile);
       // tables that claim more items than the launch has (row_start not ascending) end here
       if (item < 0 || item + int64_t(max(n - 1, 0)) * s.tiles >= a.items) continue;
       at0 = at1 = int64_t(item) * a.pool.Hkv + kvh;
