@@ -1370,9 +1370,10 @@ __global__ __launch_bounds__(256) void paged_f32_kernel(PagedKernelArgs a) {
                                                     0, 0);
     }
     if (fix) {
+#pragma unroll 1
+      for (int g = 0; g < 4; ++g)
 #pragma unroll
-      for (int s = 0; s < KV / 4; ++s)
-        for (int g = 0; g < 4; ++g) {
+        for (int s = 0; s < KV / 4; ++s) {
           const int key = key0 + 4 * s + g;
 #pragma unroll
           for (int e = 0; e < DPL; ++e) {
