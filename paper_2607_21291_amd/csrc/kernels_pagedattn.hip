@@ -28,6 +28,7 @@ struct PagedKernelArgs {
   int items;       // per kv head: the grid's, and no more than that have a place in part_o
   int target;      // of them to cut the work into (0: no splits)
   int split_min;   // least blocks of 64 slots per split
+  int split_gain;  // least blocks that the longest tile has to be cut by
   int unit_shift;  // paged_flat: log2 of the slots per unit
   float* part_o;   // [item][kv head][BM][HD]
   float2* part_ml; // [item][kv head][BM]: maximum (log2 units), sum
@@ -46,6 +47,19 @@ __device__ __forceinline__ int wave_prefix(int v) {
   DSF_SCAN(0x143, 0xc);  // lane 31 to rows 2 and 3
 #undef DSF_SCAN
   return v;
+}
+
+// Largest of the wave's numbers (none negative), in every lane.
+__device__ __forceinline__ int wave_most(int v) {
+#define DSF_SCAN(ctrl, rows) v = max(v, __builtin_amdgcn_update_dpp(0, v, ctrl, rows, 0xf, false))
+  DSF_SCAN(0x111, 0xf);
+  DSF_SCAN(0x112, 0xf);
+  DSF_SCAN(0x114, 0xf);
+  DSF_SCAN(0x118, 0xf);
+  DSF_SCAN(0x142, 0xa);
+  DSF_SCAN(0x143, 0xc);
+#undef DSF_SCAN
+  return __builtin_amdgcn_readlane(v, 63);
 }
 
 // A sequence's work: `tiles` tiles of BM rows, slots from `lo` (a multiple of
@@ -106,6 +120,7 @@ __device__ __forceinline__ int paged_split_blocks(const PagedKernelArgs& a, cons
       if (items <= a.target) break;
       per = int((unsigned(per) * unsigned(items) + a.target - 1) / unsigned(a.target));
     }
+    if (wave_most(w.tiles ? w.blocks : 0) <= per + a.split_gain) per = kNoSplit;
   }
   return per;
 }
@@ -158,18 +173,6 @@ struct PagedFlat {
 };
 __device__ __forceinline__ int paged_units(const PagedKernelArgs& a, const PagedShape& w) {  // of a tile
   return max((max(w.kv - w.lo, 0) + (1 << a.unit_shift) - 1) >> a.unit_shift, 1);
-}
-// Largest of the wave's numbers (none negative), in every lane.
-__device__ __forceinline__ int wave_most(int v) {
-#define DSF_SCAN(ctrl, rows) v = max(v, __builtin_amdgcn_update_dpp(0, v, ctrl, rows, 0xf, false))
-  DSF_SCAN(0x111, 0xf);
-  DSF_SCAN(0x112, 0xf);
-  DSF_SCAN(0x114, 0xf);
-  DSF_SCAN(0x118, 0xf);
-  DSF_SCAN(0x142, 0xa);
-  DSF_SCAN(0x143, 0xc);
-#undef DSF_SCAN
-  return __builtin_amdgcn_readlane(v, 63);
 }
 __device__ __forceinline__ PagedFlat paged_flat(const PagedKernelArgs& a, const PagedShape& w, int lane) {
   int units = w.tiles ? w.tiles * paged_units(a, w) : 0, tiles = w.tiles, most = w.tiles ? paged_units(a, w) : 0;
@@ -1586,6 +1589,7 @@ constexpr int kTokenRows = 64;       // rows of a sequence (tokens times heads) 
 constexpr int kChunkItems = 512;     // workgroups aimed at, of all kv heads
 constexpr int kF32Items = 768;
 constexpr int kSplitMinBlocks = 4;   // 256 slots
+constexpr int kSplitGain = 8;        // a chunk's turns that the splits' way through memory and their join cost
 
 // Workgroups of the token kernel that a CU holds, for 16, 32 and 64 rows.
 constexpr int kTokenPerCu[3] = {2, 1, 1};
@@ -1685,6 +1689,7 @@ hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t s) {
     k[i].items = p[i].items;
     k[i].target = p[i].target;
     k[i].split_min = kSplitMinBlocks;
+    k[i].split_gain = a.dtype == DSF_F32 ? 0 : kSplitGain;
     k[i].unit_shift = p[i].unit_shift;
     k[i].part_o = reinterpret_cast<float*>(ws);
     k[i].part_ml = reinterpret_cast<float2*>(ws + align256(plan_rows(p[i], a.pool.Hkv) * a.pool.hd * 4));
