@@ -14,13 +14,15 @@ namespace dsf {
 struct PagedSeq {
   int row0, n, kv;
 };
-__device__ __forceinline__ PagedSeq paged_seq(const PagedBatch& pb, int b) {
+__device__ __forceinline__ PagedSeq paged_seq(const PagedBatch& pb, int r0, int r1, int kv) {
   PagedSeq s;
-  const int r0 = pb.row_start[b], r1 = pb.row_start[b + 1], kv = pb.kv_len[b];
   s.row0 = min(max(r0, 0), pb.n_rows);
   s.n = min(max(r1, s.row0), pb.n_rows) - s.row0;
   s.kv = min(max(kv, 0), pb.max_pages << pb.page_shift);
   return s;
+}
+__device__ __forceinline__ PagedSeq paged_seq(const PagedBatch& pb, int b) {
+  return paged_seq(pb, pb.row_start[b], pb.row_start[b + 1], pb.kv_len[b]);
 }
 // Page that holds page index i (>= 0) of sequence b.
 __device__ __forceinline__ int paged_page(const PagedBatch& pb, int b, int i, int n_pages) {
