@@ -476,6 +476,8 @@ class PagedBatch:
             raise ValueError("row_start, kv_len and pages must be int32")
         if kv_len.dim() != 1 or row_start.shape != (B + 1,) or pages.dim() != 2 or pages.shape[0] != B:
             raise ValueError("row_start [B + 1], kv_len [B], pages [B, max_pages]")
+        if not (0 <= n_rows < 2**31 and 0 <= max_rows < 2**31):
+            raise ValueError("n_rows and max_rows must be from 0 to 2^31 - 1")
         self.row_start, self.kv_len, self.pages, self.n_rows = row_start, kv_len, pages, n_rows
         self.device = _one_device(row_start, kv_len, pages)
         self.index = kv_len.get_device()
@@ -552,6 +554,8 @@ def paged_attention(cache: PagedCache, batch: PagedBatch, q, out, window: int = 
     op = _paged_rows("out", out, cache, batch, heads)
     if out.dtype != q.dtype:
         raise ValueError("q and out have different dtypes")
+    if not 0 <= window < 2**31:
+        raise ValueError("window must be from 0 to 2^31 - 1")
     dtype = _dtype_code(q)
     if workspace is None:
         need = max(paged_attention_workspace_size(cache, batch, dtype, heads), 256)

@@ -1374,7 +1374,7 @@ static int check_paged_rows(const char* name, const void* p, int64_t row, int64_
   DSF_CHECK(row >= 0 && head >= 0 && row % 8 == 0 && head % 8 == 0, DSF_EINVAL,
             "%s: strides must be non-negative multiples of 8 elements", name);
   const int64_t most = int64_t(1) << 40;
-  DSF_CHECK(row <= most && head <= most && row * (n_rows - 1) <= most && head * (heads - 1) <= most, DSF_EINVAL,
+  DSF_CHECK(row <= most / std::max(n_rows - 1, 1) && head <= most / std::max(heads - 1, 1), DSF_EINVAL,
             "%s: strides too large", name);
   return DSF_OK;
 }

@@ -118,7 +118,8 @@ __device__ __forceinline__ int paged_split_blocks(const PagedKernelArgs& a, cons
     for (int i = 0; i < 4; ++i) {
       const int items = total([per](const PagedShape& x) { return x.tiles * paged_splits(x, per); });
       if (items <= a.target) break;
-      per = int((unsigned(per) * unsigned(items) + a.target - 1) / unsigned(a.target));
+      // (a row_start that does not ascend may claim any number of items)
+      per = int(min((unsigned(per) * unsigned(min(items, 4096)) + a.target - 1) / unsigned(a.target), unsigned(kNoSplit)));
     }
     if (wave_most(w.tiles ? w.blocks : 0) <= per + a.split_gain) per = kNoSplit;
   }

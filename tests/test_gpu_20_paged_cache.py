@@ -89,6 +89,32 @@ def test_read(dev, dtype, cache, hd, name):
         assert torch.equal(got.cpu().double().nan_to_num(nan=1e30), want.nan_to_num(nan=1e30))
 
 
+@pytest.mark.parametrize("dtype,cache", KINDS)
+def test_more_rows_than_a_pass_of_the_grid(dev, dtype, cache):
+    """Every workgroup comes round again, with rows of several sequences, rows of none and rows without a slot."""
+    s = Setup([(2500, 2600), (0, 5), (2500, 2000), (1699, 1699)], hkv=5, hd=128, page=128, dtype=dtype, cache=cache,
+              pad=200)
+    announce(f"paged copies {dtype} {cache} of many rows")
+    c, batch = s.device(dev)
+    new_k, new_v = s.rows(5, seed=4), s.rows(5, seed=5)
+    outs = [torch.full(new_k.shape, 7.0, dtype=DT[dtype], device=dev) for _ in range(2)]
+    P.paged_cache_write(c, batch, new_k.to(dev), new_v.to(dev))
+    P.paged_cache_read(c, batch, *outs)
+    torch.cuda.synchronize()
+    want = _expect(s, new_k, new_v)
+    for got, bits in zip((c.k, c.k_exp, c.v, c.v_exp), want):
+        if bits is not None:
+            assert torch.equal(_bits(got), _bits(bits))
+    for got, pool, exps in ((outs[0], want[0], want[1]), (outs[1], want[2], want[3])):
+        back = torch.full(new_k.shape, 7.0, dtype=torch.float64)
+        for b in range(len(s.seqs)):
+            parts = (pool.numpy(), exps.numpy()) if exps is not None else (pool.double().numpy(), None)
+            x = torch.from_numpy(G.sequence(*parts, s.pages[b], s.kv_len[b], s.page))
+            for r, p in G.rows_of(s.row_start, s.kv_len, b, s.max_rows):
+                back[r] = x[p] if p >= 0 else 0.0
+        assert torch.equal(got.cpu().double(), back)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_every_code_and_odd_values(dev, dtype):
     """Rows around every border of the format: zeros, the least numbers, infinities, NaN, ties, each code times a power

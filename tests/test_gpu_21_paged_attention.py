@@ -113,6 +113,28 @@ def test_long_sequences_are_split(dev, dtype, cache, hd):
         _check(s, q, out, window=1500)
 
 
+@pytest.mark.parametrize("dtype,cache", KINDS)
+@pytest.mark.parametrize("hd", [32, 64, 128])
+def test_chunks_that_end_around_a_turn(dev, dtype, cache, hd):
+    """Tiles of 1 to 7 turns of 64 slots, the last one whole, a slot short of it and a slot more."""
+    seqs = [(70, 64 * k + d) for k in range(2, 8) for d in (-1, 0, 1)] + [(70, 70), (70, 64), (70, 63)]
+    s = Setup(seqs, hkv=1, hd=hd, page=32, dtype=dtype, cache=cache)
+    announce(f"paged attention {dtype} {cache} hd={hd} turns")
+    q, out = _run(dev, s, 2)
+    _check(s, q, out)
+
+
+@pytest.mark.parametrize("dtype,cache", KINDS)
+@pytest.mark.parametrize("window", [500, 1100, 2500])
+def test_splits_of_a_window(dev, dtype, cache, window):
+    """A tile's splits share what its own rows see: windows that begin at any slot, beside a chunk that is its own
+    whole context and one whose rows are more than its slots."""
+    s = Setup([(150, 5000), (90, 2777), (200, 200), (100, 40)], hkv=1, hd=64, page=64, dtype=dtype, cache=cache)
+    announce(f"paged attention {dtype} {cache} splits of a window {window}")
+    q, out = _run(dev, s, 3, window=window)
+    _check(s, q, out, window=window)
+
+
 @pytest.mark.parametrize("dtype,cache", [("bf16", "bf16"), ("f32", "f32"), ("bf16", "e4m3")])
 @pytest.mark.parametrize("count", [63, 64, 65, 130])
 def test_many_sequences(dev, dtype, cache, count):

@@ -208,6 +208,28 @@ def test_binding_refuses_what_does_not_fit():
             P.paged_attention(c, b, qq, out)
 
 
+def test_strides_whose_extent_passes_64_bits_are_refused():
+    """2^40 elements times 2^24 rows is 0 in 64 bits."""
+    many = _batch(n_rows=(1 << 24) + 1)
+    for fn in ("dsf_paged_cache_write", "dsf_paged_cache_read"):
+        assert _copy(fn, batch=many, k_row=1 << 40) == 1
+        assert _copy(fn, batch=many, v_row=1 << 40) == 1
+    assert _attend(batch=many, q_row=1 << 40) == 1
+    assert _attend(batch=many, o_row=1 << 40) == 1
+
+
+def test_binding_refuses_numbers_past_32_bits():
+    """The C structures would take their lower halves."""
+    b = _cpu_batch()
+    for n_rows, max_rows in ((5, 1 << 32), (1 << 32, 3), (-1, 3), (5, -1)):
+        with pytest.raises(ValueError, match="2\\^31"):
+            P.PagedBatch(b.row_start, b.kv_len, b.pages, n_rows, max_rows)
+    q = torch.zeros(5, 4, 64, dtype=torch.bfloat16)
+    for window in (-1, 1 << 31, (1 << 32) + 5):
+        with pytest.raises(ValueError, match="window"):
+            P.paged_attention(_cpu_pool(), b, q, q.clone(), window=window)
+
+
 def test_binding_refuses_tensors_off_the_gpu():
     c, b = _cpu_pool(), _cpu_batch()
     rows, q = torch.zeros(5, 2, 64, dtype=torch.bfloat16), torch.zeros(5, 4, 64, dtype=torch.bfloat16)
