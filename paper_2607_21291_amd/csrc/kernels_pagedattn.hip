@@ -6,10 +6,15 @@
 // maximum and sum of the softmax of a tile's rows in fp32. Where there are
 // too few tiles for the chip the slots are divided too, by rules that every
 // workgroup works out for itself from the sequences' lengths on the device
-// (the host knows only bounds): chunks of tokens and fp32 in splits of equal
-// length (paged_item), sequences of few rows in equal shares of all the slots
-// (paged_flat). The shares of a tile go to the workspace and
+// (the host knows only bounds): chunks of tokens and fp32 in even splits of
+// each tile (paged_item), sequences of few rows in equal shares of all the
+// slots (paged_flat). The shares of a tile go to the workspace and
 // paged_join_kernel adds them up in their order.
+//
+// Times in this file are of whole calls with their join, in turn over three
+// sets of inputs, unless a kernel's is meant. A call of few tokens is a chain
+// of waits: 2.4 us until a workgroup knows its share (lengths, a scan), 1.5 to
+// its pages and queries, then 2.2 per turn of a wave.
 #include <algorithm>
 #include <type_traits>
 
@@ -98,11 +103,15 @@ struct PagedItem {
 constexpr int kNoSplit = 1 << 19;  // blocks: more slots than a sequence may have
 // A tile's blocks go to its splits evenly, so that they end at the same time.
 __device__ __forceinline__ int paged_splits(const PagedShape& w, int per) { return max((w.blocks + per - 1) / per, 1); }
-// Blocks of 64 slots per split, at most. All the work (tiles times blocks) over the
-// number of items aimed at: a longer item would outlast the others. Where
-// there are fewer tiles than that, so many longer that the items are no more:
-// one round of workgroups, and a few in a second would double the time.
+// Blocks of 64 slots per split, at most. All the work (tiles times blocks)
+// over the number of items aimed at: a longer item would outlast the others.
+// Where there are fewer tiles than that, so many longer that the items are no
+// more: one round of workgroups, and a few in a second would double the time.
+// No splits where they would shorten the longest tile by a.split_gain or less.
 // w: shapes of the first 64 sequences, in lanes.
+// (Even splits of what a tile sees, not of its sequence: 24 sequences with six
+// chunks 60.2 -> 57.1 us, chunks with a window 56.7 -> 55.5. Splits of one
+// place kept on one XCD, for its L2: 2 to 15 % slower, the XCDs' loads differ.)
 __device__ __forceinline__ int paged_split_blocks(const PagedKernelArgs& a, const PagedShape& w, int lane) {
   if (a.target == 0) return kNoSplit;
   // sum over the sequences of what f says of them
@@ -163,6 +172,10 @@ __device__ __forceinline__ PagedItem paged_item(const PagedKernelArgs& a, int it
 // share of a tile that began before it at place 2 j, of one that goes on
 // behind it at place 2 j + 1. Short work is not cut up: with tiles for
 // everybody, none longer than kWholeUnits, each workgroup has whole tiles.
+// kWholeUnits: whole, 900 slots of one sequence take 11.1 us, cut up 11.4, and
+// 513 slots 9.2 and 10.5; but 2000 slots of four sequences 18.4 and 10.4.
+// kLeastUnits: 2000 slots of four sequences take 10.5 us; with 2, for more
+// shares to join, 11.3, with 8, for fewer workgroups, 11.9.
 constexpr int kWholeUnits = 16;  // 1024 slots
 constexpr int kLeastUnits = 4;   // of a share
 struct PagedFlat {
@@ -479,8 +492,23 @@ __device__ __forceinline__ float not_finite_sum(float c) {
 // general form of the same.
 //
 // DMA into LDS is issued in inline assembly: the compiler, which cannot tell
-// the stages apart, would wait for it before every transpose load.
-// LDS: two tiles of keys, two of values; e4m3: each wave's codes of a tile of either.
+// the stages apart, would wait for it before every transpose load. e4m3 codes
+// come as they are and are widened on their way to the stage a turn later.
+//
+// Bound by LDS reads at head dim 128: 32 keys and 32 values of 128 are 16 KB
+// for a wave and half turn, 128 bytes a clock and CU for keys and (transpose
+// loads) half that for values, 3072 of the 3800 clocks that two workgroups
+// take for a turn each. Two chunks of some 4000 tokens over 12000 to 20000
+// slots (28 heads over 4, 1.48 TFLOP): 1400 us, 1.06 PFLOP/s (a large library
+// product of the same type: 1.61). Slower there: 64 rows a wave, for half the
+// reads, 1595 us (one wave to a SIMD issues a vector instruction every 7
+// clocks); eight waves with 256 rows and four stages 1430; LDS addresses that
+// move with the turn instead of constant ones 1412 against 1377.
+// One chunk of 512 over 8192 slots (12 heads over 2): 45 us, the kernel 37: 5
+// us to the first scores, 13 turns of 1.8 us, 6 us for 29 MB of shares.
+// LDS: two tiles of keys, two of values; e4m3: each wave's codes of a tile of
+// either. Four stages at head dim 64 gained nothing (mixed batch below: 51 us
+// either way).
 template <int HD>
 constexpr int kCodeBytes = 16 * HD > 1024 ? 16 * HD : 1024;
 template <int HD, bool E8>
@@ -951,6 +979,13 @@ struct ValueSlots {
 // A probability goes into that product as two bf16 numbers (its rounding and
 // what that leaves), so it counts with 16 bits: the second product costs
 // nothing here.
+//
+// 64 tokens over 60 to 8100 slots each (28 heads over 4 of 128, bf16, 516 MB):
+// 100 us, the kernel 95.5, 5.4 TB/s (a large copy: 5.4). 9 tokens over 20000
+// to 33000 slots, e4m3 (235 MB): 55 us, the kernel 49.9, 4.7 TB/s. One token
+// over 513 slots, 14 heads over 2 of 64: 9.1 us, all of it waits. Two pieces
+// on their way instead of one: 105 us in place of 100, for registers.
+//
 // LDS: the waves' values, or 16 rows of all four waves (rows HD + 4 floats
 // apart, so that they spread over the banks); then maxima and sums.
 template <int HD>
@@ -1197,8 +1232,11 @@ __global__ __launch_bounds__(256) void paged_token_kernel(PagedKernelArgs a) {
   paged_token<HD, E8, NR>(a, blockIdx.x, smem);
 }
 // Both, for batches that may have either: the chunks' workgroups first (their
-// work is longer), the tokens' beside them. One after the other they took 60
-// us where 24 sequences, six of them with chunks, take 49 this way.
+// work is longer), the tokens' beside them. 24 sequences, six of them with
+// chunks of 158 to 616 tokens (14 heads over 2 of 64, e4m3): 57.7 us, as two
+// launches 72.2; five chunks with a window 55.5 and 58.6; two long chunks 1380
+// either way. What bounds the first is its longest items (26 turns of 64 slots
+// at 1.5 us, the average is 18) after 5.5 us to the first scores.
 template <int HD, bool E8>
 __global__ __launch_bounds__(256, 2) void paged_mixed_kernel(PagedKernelArgs chunks, PagedKernelArgs tokens) {
   constexpr int kLds = kChunkLds<HD, E8> > kTokenLds<HD, 1> ? kChunkLds<HD, E8> : kTokenLds<HD, 1>;
@@ -1216,7 +1254,10 @@ __global__ __launch_bounds__(256, 2) void paged_mixed_kernel(PagedKernelArgs chu
 // bytes of a row per lane, element e of the vectors forming one 4-deep
 // product; the probabilities go through a per-wave LDS tile into the A
 // operand of P V, whose B operand is HD / 16 neighbouring dims of slot
-// 4 s + grp as they come from memory.
+// 4 s + grp as they come from memory. Loads of the next piece during this
+// one's product cost more in registers than they hid (21.0 -> 24.1 us): other
+// waves hide them. Two chunks of 77 to 200 tokens over 350 to 1000 slots, 12
+// heads of 64 (0.39 GFLOP): 21 us, the kernel 16.5; at head dim 128 47 us.
 template <int HD, bool E8>
 __global__ __launch_bounds__(256) void paged_f32_kernel(PagedKernelArgs a) {
   constexpr int NK = HD / 16, DPL = HD / 16, KV = 32;
@@ -1480,7 +1521,10 @@ __device__ __forceinline__ void paged_join_row(const PagedKernelArgs& a, int64_t
 // A workgroup takes kJoinRows rows of one tile and kv head at a time, a
 // thread four dims of a row, and goes on to every blocks-th such part. Tiles
 // that one workgroup had to itself are done already. FLAT: shares of the
-// line, else splits.
+// line, else splits. Four to ten us, half of it until the first share is there
+// (four or sixteen of them on the way instead of eight: within 1 us); 1024
+// workgroups: two chunks of 900 tokens 35.4 us, with 512 38.3, with 4096 35.7,
+// but then the mixed batch 59.7 for 56.9, by workgroups without work.
 constexpr int kJoinRows = 16;
 constexpr int kJoinBlocks = 1024;
 template <int HD, typename T, bool FLAT>
@@ -1586,13 +1630,32 @@ struct PagedPlan {
   size_t places;   // of shares, per kv head
 };
 
-constexpr int kTokenRows = 64;       // rows of a sequence (tokens times heads) the token kernel takes
-constexpr int kChunkItems = 512;     // workgroups aimed at, of all kv heads
+// Rows of a sequence (tokens times heads of a kv head) up to which the token
+// kernel takes it, with weights of 16 bits. A choice for what a decoding step
+// answers, not for time: 16 sequences of 49 rows over 500 to 6000 slots take
+// 42.3 us, as chunks 33.1; 64 of 28 rows 116.5 and 114.8; one of 28 rows 23.6
+// and 23.1.
+constexpr int kTokenRows = 64;
+// Workgroups aimed at with splits, of all kv heads: two to a CU. A chunk of
+// 512 over 8192 slots takes 45.5 us (256: 46.6, 1024: 60.2), the mixed batch
+// 57 (59.2, 58.5), a window 55.5 (55.5, 78.5).
+constexpr int kChunkItems = 512;
+// fp32: three to a CU. Short chunks 20.9 us (512: 22.1, 1536: 20.9), 500 to
+// 900 tokens over 2000 to 4000 slots 314.5 (314.1, 317.4).
 constexpr int kF32Items = 768;
-constexpr int kSplitMinBlocks = 4;   // 256 slots
-constexpr int kSplitGain = 8;        // a chunk's turns that the splits' way through memory and their join cost
+// 256 slots. A chunk of 256 over 2048 slots takes 20.9 us (128 slots: 24.3,
+// 512: 23.7), short ones in fp32 20.9 (22.4, 22.2).
+constexpr int kSplitMinBlocks = 4;
+// What a split's way through memory and the join cost, in a chunk's turns: two
+// chunks of 900 tokens on their own context take 27.9 us, with 4 (so that they
+// are split) 35.7; two of 300 over 1000 slots 24.1, with 12 (so that they are
+// not) 29.9. fp32 turns are longer: short chunks 20.9 with 0, 26.6 with 8.
+constexpr int kSplitGain = 8;
 
 // Workgroups of the token kernel that a CU holds, for 16, 32 and 64 rows.
+// One of 16 rows: 9 long e4m3 sequences 75.1 us for 55.6; 3, 2 and 2: 68.8
+// (a second round), 64 bf16 sequences 110.3 for 100, 16 of 49 rows 58.7 for
+// 42.4.
 constexpr int kTokenPerCu[3] = {2, 1, 1};
 
 size_t align256(size_t n) { return (n + 255) & ~size_t(255); }
@@ -1616,6 +1679,8 @@ PagedPlan tiles_plan(const PagedBatch& pb, int G, int bm_shift, int m_lo, int m_
 PagedPlan split_plan(const PagedBatch& pb, int G, int Hkv, int bm_shift, int m_lo, int m_hi, int total) {
   PagedPlan p = tiles_plan(pb, G, bm_shift, m_lo, m_hi);
   const int64_t blocks = (int64_t(pb.max_pages) << pb.page_shift) / 64;
+  // (with two rounds of tiles and more nothing is split: the last round is a small part then, and 4 chunks of 500 to 900
+  // tokens over 3000 to 9000 slots, 1.1 rounds, are split and take 104 us)
   if (blocks > kSplitMinBlocks && p.tiles <= 4096 && int64_t(p.tiles) * Hkv < 2 * total) p.target = std::max(total / Hkv, 1);
   p.items = p.tiles + p.target;
   p.join = p.target != 0;
