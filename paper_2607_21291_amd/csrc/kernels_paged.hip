@@ -79,7 +79,7 @@ __device__ __forceinline__ Raw8<T> paged_get(const void* pool, const uint8_t* ex
 }
 
 template <typename T, bool E8, int HD, bool WRITE>
-__global__ __launch_bounds__(256) void paged_copy_kernel(PagedPool pool, PagedBatch pb, T* __restrict__ k,
+__global__ __launch_bounds__(256) void paged_copy_kernel(PagedPool pool, PagedBatch pb, Divisor by_Hkv, T* __restrict__ k,
                                                          int64_t k_row, int64_t k_head, T* __restrict__ v,
                                                          int64_t v_row, int64_t v_head) {
   constexpr int L = HD / 8, RPB = 256 / L;  // lanes per (row, head), and those per workgroup
@@ -92,10 +92,10 @@ __global__ __launch_bounds__(256) void paged_copy_kernel(PagedPool pool, PagedBa
     __syncthreads();
   }
   const int part = tid % L;
-  const int64_t pairs = int64_t(pb.n_rows) * pool.Hkv, stride = int64_t(gridDim.x) * RPB;
+  const int pairs = pb.n_rows * pool.Hkv, stride = gridDim.x * RPB;  // (pairs: below 2^31)
   // The slot's row in the pool that (row, head) p has; -1 before the first slot, -2 if it is no sequence's row.
-  auto locate = [&](int64_t p) -> int64_t {
-    const int r = int(p / pool.Hkv), h = int(p - int64_t(r) * pool.Hkv);
+  auto locate = [&](int p) -> int64_t {
+    const int r = p / by_Hkv, h = p - r * pool.Hkv;
     int lo = 0, hi = pb.B;  // the last b with row_start[b] <= r
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
@@ -110,11 +110,11 @@ __global__ __launch_bounds__(256) void paged_copy_kernel(PagedPool pool, PagedBa
     return ((int64_t(page) * pool.Hkv + h) << pb.page_shift) + (slot & ((1 << pb.page_shift) - 1));
   };
   // every lane of a (row, head) goes the same way, so the maximum over them is whole
-  int64_t p = int64_t(blockIdx.x) * RPB + tid / L;
+  int p = blockIdx.x * RPB + tid / L;
   if (p >= pairs) return;
   int64_t at = locate(p);
   while (true) {
-    const int r = int(p / pool.Hkv), h = int(p - int64_t(r) * pool.Hkv);
+    const int r = p / by_Hkv, h = p - r * pool.Hkv;
     T* kp = k + r * k_row + h * k_head + 8 * part;
     T* vp = v + r * v_row + h * v_head + 8 * part;
     Raw8<T> kx = {}, vx = {};
@@ -128,8 +128,8 @@ __global__ __launch_bounds__(256) void paged_copy_kernel(PagedPool pool, PagedBa
       }
     }
     const int64_t here = at;
-    p += stride;
-    if (p < pairs) at = locate(p);  // while the loads are on their way
+    const bool more = p < pairs - stride;
+    if (more) at = locate(p += stride);  // while the loads are on their way
     if constexpr (WRITE) {
       if (here >= 0) {
         paged_put<T, E8, HD>(kx, pool.k, pool.ke, here, part);
@@ -142,7 +142,7 @@ __global__ __launch_bounds__(256) void paged_copy_kernel(PagedPool pool, PagedBa
         reinterpret_cast<u32x4*>(vp)[j] = vx.v[j];
       }
     }
-    if (p >= pairs) return;
+    if (!more) return;
   }
 }
 
@@ -156,7 +156,7 @@ hipError_t launch_paged_copy(int dtype, bool write, const PagedPool& pool, const
     const int64_t pairs = int64_t(pb.n_rows) * pool.Hkv;
     const int grid = int(std::min<int64_t>((pairs + RPB - 1) / RPB, kPagedCopyBlocks));
     paged_copy_kernel<T, decltype(e8c)::value, HD, decltype(wc)::value>
-        <<<grid, 256, 0, s>>>(pool, pb, (T*)k, k_row, k_head, (T*)v, v_row, v_head);
+        <<<grid, 256, 0, s>>>(pool, pb, divisor(pool.Hkv), (T*)k, k_row, k_head, (T*)v, v_row, v_head);
     return hipGetLastError();
   };
   auto run_w = [&](auto tag, auto e8c, auto hdc) {

@@ -28,6 +28,7 @@ struct PagedKernelArgs {
   const void* q; int64_t q_row, q_head;
   void* out; int64_t o_row, o_head;
   int G, window;
+  Divisor by_G, by_Hkv;
   int bm_shift;    // log2 of the rows per tile
   int m_lo, m_hi;  // sequences with m_lo < rows * G <= m_hi take part
   int items;       // per kv head: the grid's, and no more than that have a place in part_o
@@ -85,7 +86,7 @@ __device__ __forceinline__ PagedShape paged_shape(const PagedKernelArgs& a, int 
   w.tiles = w.M > a.m_lo && w.M <= a.m_hi ? min((w.M + (1 << a.bm_shift) - 1) >> a.bm_shift, a.items) : 0;
   w.lo = a.window ? max(s.kv - s.n - a.window + 1, 0) & ~63 : 0;
   w.blocks = (max(s.kv - w.lo, 0) + 63) >> 6;
-  if (a.window) w.blocks = min(w.blocks, (min(a.window, w.kv) + ((1 << a.bm_shift) - 1) / a.G + 64 + 63) >> 6);
+  if (a.window) w.blocks = min(w.blocks, (min(a.window, w.kv) + ((1 << a.bm_shift) - 1) / a.by_G + 64 + 63) >> 6);
   return w;
 }
 // Lane l's shape, in every lane.
@@ -253,9 +254,9 @@ struct PagedWork {
 __device__ __forceinline__ void paged_range(const PagedKernelArgs& a, const PagedShape& w, int tile, int* begin, int* end) {
   const int p0 = w.kv - w.n;
   const int m0 = tile << a.bm_shift, m1 = min(m0 + (1 << a.bm_shift), w.M) - 1;
-  const int s = a.window ? max(p0 + m0 / a.G - a.window + 1, 0) & ~63 : 0;
+  const int s = a.window ? max(p0 + m0 / a.by_G - a.window + 1, 0) & ~63 : 0;
   *begin = s;
-  *end = max(min(p0 + m1 / a.G + 1, w.kv), s);
+  *end = max(min(p0 + m1 / a.by_G + 1, w.kv), s);
 }
 // Slots per split of such a range (0: there are none).
 __device__ __forceinline__ int paged_split_len(int begin, int end, int splits) {
@@ -524,7 +525,7 @@ __device__ __forceinline__ void paged_chunk(const PagedKernelArgs& a, int block,
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // kv head innermost: consecutive workgroups go to different XCDs, so that
   // (with 8 heads or a divisor of 8) an XCD's L2 sees the slots of few heads
-  const int item = block / a.pool.Hkv, kvh = block - item * a.pool.Hkv;
+  const int item = block / a.by_Hkv, kvh = block - item * a.pool.Hkv;
   const PagedItem it = paged_item(a, item, lane);
   if (it.b < 0) return;
   const PagedWork w = paged_work(a, it);
@@ -532,7 +533,7 @@ __device__ __forceinline__ void paged_chunk(const PagedKernelArgs& a, int block,
 
   // this wave's rows: row m of the sequence, its token's slot
   const int m0 = w.tile * BM + wave * 32, m = m0 + r32, mc = min(m, w.M - 1);
-  const int tok = mc / a.G, g = mc - tok * a.G, my_slot = w.p0 + tok;
+  const int tok = mc / a.by_G, g = mc - tok * a.G, my_slot = w.p0 + tok;
   bf16x8 qf[NS];
   {
     const uint16_t* qp =
@@ -541,11 +542,11 @@ __device__ __forceinline__ void paged_chunk(const PagedKernelArgs& a, int block,
     for (int s = 0; s < NS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qp + 16 * s + 8 * hi);
   }
   // slots that every row of the wave sees: [see_lo, see_hi)
-  const int see_hi = min(w.p0 + min(m0, w.M - 1) / a.G + 1, w.end);
-  const int see_lo = a.window ? w.p0 + min(m0 + 31, w.M - 1) / a.G - a.window + 1 : 0;
+  const int see_hi = min(w.p0 + min(m0, w.M - 1) / a.by_G + 1, w.end);
+  const int see_lo = a.window ? w.p0 + min(m0 + 31, w.M - 1) / a.by_G - a.window + 1 : 0;
 
   // tiles up to the last one that some row sees
-  const int any_hi = m0 < w.M ? w.p0 + min(m0 + 31, w.M - 1) / a.G + 1 : 0;
+  const int any_hi = m0 < w.M ? w.p0 + min(m0 + 31, w.M - 1) / a.by_G + 1 : 0;
   const int my_nt = max(min(any_hi, w.end) - w.begin + 63, 0) >> 6;
 
   const float sc = 1.4426950408889634f / sqrtf(float(HD));  // log2(e) / sqrt(hd)
@@ -1005,7 +1006,7 @@ __device__ __forceinline__ void paged_token(const PagedKernelArgs& a, int block,
   auto ls = ms + 4;
   const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, grp = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wg = block / a.pool.Hkv, kvh = block - wg * a.pool.Hkv;
+  const int wg = block / a.by_Hkv, kvh = block - wg * a.pool.Hkv;
   PagedShape shapes = {};
   if (lane < a.pb.B) shapes = paged_shape(a, lane);
   const PagedFlat flat = paged_flat(a, shapes, lane);
@@ -1037,14 +1038,14 @@ __device__ __forceinline__ void paged_token(const PagedKernelArgs& a, int block,
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
       const int mc = min(m0 + 16 * r + r16, w.M - 1);
-      const int tok = mc / a.G, g = mc - tok * a.G;
+      const int tok = mc / a.by_G, g = mc - tok * a.G;
       slot_of[r] = p0 + tok;
       const uint16_t* qp =
           static_cast<const uint16_t*>(a.q) + int64_t(w.row0 + tok) * a.q_row + int64_t(kvh * a.G + g) * a.q_head;
 #pragma unroll
       for (int s = 0; s < NS; ++s) qf[r][s] = *reinterpret_cast<const bf16x8*>(qp + K::dim(s, grp));
     }
-    const int see_hi = p0 + m0 / a.G + 1, last = p0 + min(m0 + BM - 1, w.M - 1) / a.G;
+    const int see_hi = p0 + m0 / a.by_G + 1, last = p0 + min(m0 + BM - 1, w.M - 1) / a.by_G;
     const int see_lo = a.window ? last - a.window + 1 : 0;
     f32x4 o[NR][ND];
     float m_run[NR], l_run[NR];
@@ -1206,7 +1207,7 @@ __device__ __forceinline__ void paged_token(const PagedKernelArgs& a, int block,
           if (d == 0) a.part_ml[slot] = make_float2(M, L);
         } else {
           const float inv = L == 0.f ? 0.f : 1.0f / L;
-          const int tok = m / a.G, g = m - tok * a.G;
+          const int tok = m / a.by_G, g = m - tok * a.G;
           u32x2 pk;
           pk[0] = uint32_t(f2bf(O[0] * inv)) | uint32_t(f2bf(O[1] * inv)) << 16;
           pk[1] = uint32_t(f2bf(O[2] * inv)) | uint32_t(f2bf(O[3] * inv)) << 16;
@@ -1266,7 +1267,7 @@ __global__ __launch_bounds__(256) void paged_f32_kernel(PagedKernelArgs a) {
   __shared__ float ms[4][16], ls[4][16];
   const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, grp = lane >> 4;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int item = int(blockIdx.x) / a.pool.Hkv, kvh = int(blockIdx.x) - item * a.pool.Hkv;
+  const int item = int(blockIdx.x) / a.by_Hkv, kvh = int(blockIdx.x) - item * a.pool.Hkv;
   const PagedItem it = paged_item(a, item, lane);
   if (it.b < 0) return;
   const PagedWork w = paged_work(a, it);
@@ -1274,16 +1275,16 @@ __global__ __launch_bounds__(256) void paged_f32_kernel(PagedKernelArgs a) {
   const int m0 = w.tile * 16;
   f32x4 qf[NK];
   {
-    const int mc = min(m0 + r16, w.M - 1), tok = mc / a.G, g = mc - tok * a.G;
+    const int mc = min(m0 + r16, w.M - 1), tok = mc / a.by_G, g = mc - tok * a.G;
     const float* qp = static_cast<const float*>(a.q) + int64_t(w.row0 + tok) * a.q_row + int64_t(kvh * a.G + g) * a.q_head;
 #pragma unroll
     for (int s = 0; s < NK; ++s) qf[s] = *reinterpret_cast<const f32x4*>(qp + 16 * s + 4 * grp);
   }
   int slot_of[4];  // of rows m0 + 4 grp + i
 #pragma unroll
-  for (int i = 0; i < 4; ++i) slot_of[i] = w.p0 + min(m0 + 4 * grp + i, w.M - 1) / a.G;
-  const int see_hi = w.p0 + m0 / a.G + 1;
-  const int see_lo = a.window ? w.p0 + min(m0 + 15, w.M - 1) / a.G - a.window + 1 : 0;
+  for (int i = 0; i < 4; ++i) slot_of[i] = w.p0 + min(m0 + 4 * grp + i, w.M - 1) / a.by_G;
+  const int see_hi = w.p0 + m0 / a.by_G + 1;
+  const int see_lo = a.window ? w.p0 + min(m0 + 15, w.M - 1) / a.by_G - a.window + 1 : 0;
   const float scale = 1.0f / sqrtf(float(HD));
   float m[4], l[4];
   f32x4 o[DPL];  // o[e][i]: row m0 + 4 grp + i, dim DPL r16 + e
@@ -1460,7 +1461,7 @@ __global__ __launch_bounds__(256) void paged_f32_kernel(PagedKernelArgs a) {
       a.part_o[slot * HD + d] = O;
       if (d == 0) a.part_ml[slot] = make_float2(M, L);
     } else {
-      const int tok = mr / a.G, g = mr - tok * a.G;
+      const int tok = mr / a.by_G, g = mr - tok * a.G;
       static_cast<float*>(a.out)[int64_t(w.row0 + tok) * a.o_row + int64_t(kvh * a.G + g) * a.o_head + d] =
           L == 0.f ? 0.f : O / L;
     }
@@ -1544,7 +1545,7 @@ __device__ __forceinline__ void paged_join(const PagedKernelArgs& a, int block, 
   }
   const int parts = (1 << a.bm_shift) / kJoinRows;
   for (int unit = block;; unit += blocks) {
-    int tile = unit / parts / a.pool.Hkv;
+    int tile = unit / parts / a.by_Hkv;
     const int part = unit % parts, kvh = unit / parts - tile * a.pool.Hkv;
     // the sequence that has the tile, and where its items (FLAT: units) begin
     PagedShape w = w0, s = {};
@@ -1596,7 +1597,7 @@ __device__ __forceinline__ void paged_join(const PagedKernelArgs& a, int block, 
     for (int e = tid; e < kJoinRows * (HD / 4); e += 256) {
       const int row = part * kJoinRows + e / (HD / 4), d = e % (HD / 4) * 4, m = (tile << a.bm_shift) + row;
       if (m >= s.M) break;
-      const int tok = m / a.G, g = m - tok * a.G;
+      const int tok = m / a.by_G, g = m - tok * a.G;
       paged_join_row<HD, T>(a, (at0 << a.bm_shift) + row, (at1 << a.bm_shift) + row, step << a.bm_shift, n, d,
                             static_cast<T*>(a.out) + int64_t(s.row0 + tok) * a.o_row + int64_t(kvh * a.G + g) * a.o_head + d);
     }
@@ -1748,6 +1749,8 @@ hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t s) {
     k[i].o_row = a.o_row;
     k[i].o_head = a.o_head;
     k[i].G = a.Hq / a.pool.Hkv;
+    k[i].by_G = divisor(k[i].G);
+    k[i].by_Hkv = divisor(a.pool.Hkv);
     k[i].window = a.window;
     k[i].bm_shift = p[i].bm_shift;
     k[i].m_lo = p[i].m_lo;

@@ -8,6 +8,22 @@
 
 namespace dsf {
 
+// A number known before the launch to divide by, 1 <= n < 2^31. With 2^(l - 1)
+// < n <= 2^l and mul the next whole number over 2^(31 + l) / n, which is below
+// 2^32, m * mul / 2^(31 + l) is over m / n by at most m / 2^(31 + l), for m <
+// 2^31 less than 1 / n: its whole part is m / n's.
+struct Divisor {
+  uint32_t mul;
+  int l;
+};
+inline Divisor divisor(int n) {
+  Divisor d = {0, 0};
+  while ((int64_t(1) << d.l) < n) ++d.l;
+  d.mul = uint32_t((uint64_t(1) << (31 + d.l)) / uint64_t(n) + 1);
+  return d;
+}
+__device__ __forceinline__ int operator/(int m, const Divisor& d) { return int(__umulhi(2u * uint32_t(m), d.mul) >> d.l); }
+
 // Sequence b of the batch: rows [row0, row0 + n) of the step, at slots
 // kv - n .. kv - 1. Whatever the arrays hold, rows stay within the launch's
 // n_rows and slots within the page table.
