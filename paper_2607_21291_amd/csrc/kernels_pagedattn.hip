@@ -173,10 +173,10 @@ __device__ __forceinline__ PagedItem paged_item(const PagedKernelArgs& a, int it
 // share of a tile that began before it at place 2 j, of one that goes on
 // behind it at place 2 j + 1. Short work is not cut up: with tiles for
 // everybody, none longer than kWholeUnits, each workgroup has whole tiles.
-// kWholeUnits: whole, 900 slots of one sequence take 11.1 us, cut up 11.4, and
-// 513 slots 9.2 and 10.5; but 2000 slots of four sequences 18.4 and 10.4.
-// kLeastUnits: 2000 slots of four sequences take 10.5 us; with 2, for more
-// shares to join, 11.3, with 8, for fewer workgroups, 11.9.
+// kWholeUnits: whole, 900 slots of one sequence take 9.7 us, cut up 10.8, and
+// 513 slots 8.3 and 11.0; but 2000 slots 14.4 and 10.5.
+// kLeastUnits: 2000 slots of four sequences take 10.6 us; with 2, for more
+// shares to join, 11.4, with 8, for fewer workgroups, 11.8.
 constexpr int kWholeUnits = 16;  // 1024 slots
 constexpr int kLeastUnits = 4;   // of a share
 struct PagedFlat {
@@ -964,15 +964,20 @@ struct ValueSlots {
   }
 };
 
-// A workgroup of four waves takes its share of the line (paged_flat), one
+// A workgroup of W waves takes its share of the line (paged_flat), one
 // tile of 16 NR rows after the other; of a tile's slots each wave runs through
-// every fourth piece of TK by itself, with a softmax of its own, and the four
-// are joined in wave order. Memory bound (the rows of one token of a few
+// every W-th piece of TK by itself, with a softmax of its own, and they are
+// joined in wave order. Memory bound (the rows of one token of a few
 // heads are far too few for the matrix cores to matter), so what counts is
 // bytes on the way: keys are loaded as the matrix operand they will be,
 // straight into registers, values into registers and on through LDS, which
 // transposes them; the next piece's loads are issued as soon as this one's
-// registers are free, and several workgroups share a CU.
+// registers are free. 16 rows leave registers for two waves to a SIMD: eight
+// waves, one workgroup to a CU, so that short sequences take fewer turns and
+// long ones have half the shares to join (two workgroups of four waves: one
+// token over 513 slots 9.0 us for 8.1, 64 tokens 99.5 for 97.2, 9 long e4m3
+// sequences 55.2 for 53.5; two of eight, in two rounds: 101.6 and 59.2). More
+// rows have four (32 rows by eight waves spill: 112 -> 151 us).
 //
 // S^T = K Q^T with v_mfma_f32_16x16x32_bf16: lane (r16, grp) holds of row r16
 // the scores of slots 16 kb + 4 grp + i, which is the B operand of
@@ -982,18 +987,18 @@ struct ValueSlots {
 // nothing here.
 //
 // 64 tokens over 60 to 8100 slots each (28 heads over 4 of 128, bf16, 516 MB):
-// 100 us, the kernel 95.5, 5.4 TB/s (a large copy: 5.4). 9 tokens over 20000
-// to 33000 slots, e4m3 (235 MB): 55 us, the kernel 49.9, 4.7 TB/s. One token
-// over 513 slots, 14 heads over 2 of 64: 9.1 us, all of it waits. Two pieces
-// on their way instead of one: 105 us in place of 100, for registers.
+// 97 us, 5.3 TB/s with the join (a large copy: 5.4). 9 tokens over 20000 to
+// 33000 slots, e4m3 (235 MB): 53.3 us. One token over 513 slots, 14 heads over
+// 2 of 64: 8.3 us, all of it waits. With four waves, two pieces on their way
+// instead of one: 105 us in place of 100, for registers.
 //
-// LDS: the waves' values, or 16 rows of all four waves (rows HD + 4 floats
+// LDS: the waves' values, or 16 rows of all the waves (rows HD + 4 floats
 // apart, so that they spread over the banks); then maxima and sums.
-template <int HD>
-constexpr int kTokenShare = 4 * 8192 > 4 * 16 * (HD + 4) * 4 ? 4 * 8192 : 4 * 16 * (HD + 4) * 4;
-template <int HD, int NR>
-constexpr int kTokenLds = kTokenShare<HD> + 2 * 4 * 16 * NR * 4;
-template <int HD, bool E8, int NR>
+template <int HD, int W>
+constexpr int kTokenShare = W * (8192 > 16 * (HD + 4) * 4 ? 8192 : 16 * (HD + 4) * 4);
+template <int HD, int NR, int W>
+constexpr int kTokenLds = kTokenShare<HD, W> + 2 * W * 16 * NR * 4;
+template <int HD, bool E8, int NR, int W>
 __device__ __forceinline__ void paged_token(const PagedKernelArgs& a, int block, char* smem) {
   using S = SlotTile<HD>;
   using K = KeySlots<HD, E8>;
@@ -1002,8 +1007,8 @@ __device__ __forceinline__ void paged_token(const PagedKernelArgs& a, int block,
   constexpr int kTile = TK * S::kRowBytes;  // values of a piece
   constexpr int OS = HD + 4;                // floats per row of the join
   static_assert(kTile == 8192, "values of a piece");
-  auto ms = reinterpret_cast<float(*)[BM]>(smem + kTokenShare<HD>);  // [4][BM]
-  auto ls = ms + 4;
+  auto ms = reinterpret_cast<float(*)[BM]>(smem + kTokenShare<HD, W>);  // [W][BM]
+  auto ls = ms + W;
   const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, grp = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wg = block / a.by_Hkv, kvh = block - wg * a.pool.Hkv;
@@ -1058,7 +1063,7 @@ __device__ __forceinline__ void paged_token(const PagedKernelArgs& a, int block,
     }
 
     const int s0 = begin + TK * wave;
-    const int nt = end > s0 ? (end - s0 + 4 * TK - 1) / (4 * TK) : 0;
+    const int nt = end > s0 ? (end - s0 + W * TK - 1) / (W * TK) : 0;
     PagedTable tab;
     tab.load(a, spot.b, begin >> a.pb.page_shift, lane);
     K kx[KB];
@@ -1074,7 +1079,7 @@ __device__ __forceinline__ void paged_token(const PagedKernelArgs& a, int block,
     };
     if (nt > 0) fetch(s0);
     for (int t = 0; t < nt; ++t) {
-      const int kb0 = s0 + 4 * TK * t;
+      const int kb0 = s0 + W * TK * t;
       f32x4 s[NR][KB];
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
@@ -1091,7 +1096,7 @@ __device__ __forceinline__ void paged_token(const PagedKernelArgs& a, int block,
       // the values into LDS (this wave has read the last piece's), and the next piece's loads
 #pragma unroll
       for (int i = 0; i < KB; ++i) vx[i].store(vt + 16 * i * S::kRowBytes, lane);
-      if (t + 1 < nt) fetch(kb0 + 4 * TK);
+      if (t + 1 < nt) fetch(kb0 + W * TK);
       const bool masked = kb0 + TK > min(see_hi, end) || kb0 < see_lo;
       bf16x8 ph[NR][KB / 2], pl[NR][KB / 2];
 #pragma unroll
@@ -1174,7 +1179,7 @@ __device__ __forceinline__ void paged_token(const PagedKernelArgs& a, int block,
       }
     }
 
-    // the four waves' results, in wave order; 16 rows at a time
+    // the waves' results, in wave order; 16 rows at a time
     float* os = reinterpret_cast<float*>(smem);
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
@@ -1187,15 +1192,15 @@ __device__ __forceinline__ void paged_token(const PagedKernelArgs& a, int block,
 #pragma unroll
       for (int db = 0; db < ND; ++db) *reinterpret_cast<f32x4*>(os + (wave * 16 + r16) * OS + 16 * db + 4 * grp) = o[r][db];
       __syncthreads();
-      for (int e = tid; e < 16 * HD / 4; e += 256) {
+      for (int e = tid; e < 16 * HD / 4; e += 64 * W) {
         const int q = e / (HD / 4), d = e % (HD / 4) * 4, m = m0 + 16 * r + q;
         if (m >= w.M) break;
         float M = -INFINITY, L = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) M = fmaxf(M, ms[i][16 * r + q]);
+        for (int i = 0; i < W; ++i) M = fmaxf(M, ms[i][16 * r + q]);
         f32x4 O = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < W; ++i) {
           // a wave whose slots are all hidden (maximum -inf) has zeros (NaN where a score was)
           const float mi = ms[i][16 * r + q], f = mi == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mi - M);
           L += ls[i][16 * r + q] * f;
@@ -1227,10 +1232,10 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedKernelArgs a) 
   __shared__ __attribute__((aligned(16))) char smem[kChunkLds<HD, E8>];
   paged_chunk<HD, E8>(a, blockIdx.x, smem);
 }
-template <int HD, bool E8, int NR>
-__global__ __launch_bounds__(256) void paged_token_kernel(PagedKernelArgs a) {
-  __shared__ __attribute__((aligned(16))) char smem[kTokenLds<HD, NR>];
-  paged_token<HD, E8, NR>(a, blockIdx.x, smem);
+template <int HD, bool E8, int NR, int W>
+__global__ __launch_bounds__(64 * W) void paged_token_kernel(PagedKernelArgs a) {
+  __shared__ __attribute__((aligned(16))) char smem[kTokenLds<HD, NR, W>];
+  paged_token<HD, E8, NR, W>(a, blockIdx.x, smem);
 }
 // Both, for batches that may have either: the chunks' workgroups first (their
 // work is longer), the tokens' beside them. 24 sequences, six of them with
@@ -1240,11 +1245,11 @@ __global__ __launch_bounds__(256) void paged_token_kernel(PagedKernelArgs a) {
 // at 1.5 us, the average is 18) after 5.5 us to the first scores.
 template <int HD, bool E8>
 __global__ __launch_bounds__(256, 2) void paged_mixed_kernel(PagedKernelArgs chunks, PagedKernelArgs tokens) {
-  constexpr int kLds = kChunkLds<HD, E8> > kTokenLds<HD, 1> ? kChunkLds<HD, E8> : kTokenLds<HD, 1>;
+  constexpr int kLds = kChunkLds<HD, E8> > kTokenLds<HD, 1, 4> ? kChunkLds<HD, E8> : kTokenLds<HD, 1, 4>;
   __shared__ __attribute__((aligned(16))) char smem[kLds];
   const int first = chunks.items * chunks.pool.Hkv;
   if (int(blockIdx.x) < first) paged_chunk<HD, E8>(chunks, blockIdx.x, smem);
-  else paged_token<HD, E8, 1>(tokens, int(blockIdx.x) - first, smem);
+  else paged_token<HD, E8, 1, 4>(tokens, int(blockIdx.x) - first, smem);
 }
 
 // -------------------------------------------------------------------- fp32
@@ -1634,8 +1639,7 @@ struct PagedPlan {
 // Rows of a sequence (tokens times heads of a kv head) up to which the token
 // kernel takes it, with weights of 16 bits. A choice for what a decoding step
 // answers, not for time: 16 sequences of 49 rows over 500 to 6000 slots take
-// 42.3 us, as chunks 33.1; 64 of 28 rows 116.5 and 114.8; one of 28 rows 23.6
-// and 23.1.
+// 42.2 us, as chunks 33.1; 64 of 28 rows 112.5 and 114.8.
 constexpr int kTokenRows = 64;
 // Workgroups aimed at with splits, of all kv heads: two to a CU. A chunk of
 // 512 over 8192 slots takes 45.5 us (256: 46.6, 1024: 60.2), the mixed batch
@@ -1652,12 +1656,6 @@ constexpr int kSplitMinBlocks = 4;
 // are split) 35.7; two of 300 over 1000 slots 24.1, with 12 (so that they are
 // not) 29.9. fp32 turns are longer: short chunks 20.9 with 0, 26.6 with 8.
 constexpr int kSplitGain = 8;
-
-// Workgroups of the token kernel that a CU holds, for 16, 32 and 64 rows.
-// One of 16 rows: 9 long e4m3 sequences 75.1 us for 55.6; 3, 2 and 2: 68.8
-// (a second round), 64 bf16 sequences 110.3 for 100, 16 of 49 rows 58.7 for
-// 42.4.
-constexpr int kTokenPerCu[3] = {2, 1, 1};
 
 size_t align256(size_t n) { return (n + 255) & ~size_t(255); }
 
@@ -1691,7 +1689,7 @@ PagedPlan split_plan(const PagedBatch& pb, int G, int Hkv, int bm_shift, int m_l
 
 PagedPlan flat_plan(const PagedBatch& pb, int G, int Hkv, int bm_shift, int m_hi) {
   PagedPlan p = tiles_plan(pb, G, bm_shift, 0, m_hi);
-  p.items = std::max(256 * kTokenPerCu[bm_shift - 4] / Hkv, 1);
+  p.items = std::max(256 / Hkv, 1);  // a workgroup to a CU, one round of equal shares (comment at paged_token)
   const int64_t slots = int64_t(pb.max_pages) << pb.page_shift;
   // (row_start that does not ascend may claim all tiles of every sequence)
   const int64_t most = int64_t(pb.B) * (((m_hi - 1) >> bm_shift) + 1);
@@ -1785,9 +1783,9 @@ hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t s) {
       if (joins[1]) paged_join_kernel<HD, uint16_t, false><<<joins[1], 256, 0, s>>>(k[1]);
     }
     if (p[0].on) {
-      if (p[0].bm_shift == 4) paged_token_kernel<HD, E8, 1><<<grid[0], 256, 0, s>>>(k[0]);
-      else if (p[0].bm_shift == 5) paged_token_kernel<HD, E8, 2><<<grid[0], 256, 0, s>>>(k[0]);
-      else paged_token_kernel<HD, E8, 4><<<grid[0], 256, 0, s>>>(k[0]);
+      if (p[0].bm_shift == 4) paged_token_kernel<HD, E8, 1, 8><<<grid[0], 512, 0, s>>>(k[0]);
+      else if (p[0].bm_shift == 5) paged_token_kernel<HD, E8, 2, 4><<<grid[0], 256, 0, s>>>(k[0]);
+      else paged_token_kernel<HD, E8, 4, 4><<<grid[0], 256, 0, s>>>(k[0]);
       if (joins[0]) paged_join_kernel<HD, uint16_t, true><<<joins[0], 256, 0, s>>>(k[0]);
     }
     return hipGetLastError();
