@@ -585,11 +585,11 @@ size_t dsf_paged_attention_workspace_size(const dsf_paged_cache* cache, const ds
  * above; out does not overlap q or the pool). Scores, maximum, sum and
  * accumulation are fp32. bf16: the probabilities go into the product with v
  * as bf16 (off by 2^-8 at most each; sequences of up to 64 rows times heads
- * per kv head have a second part that brings it to 2^-16). What lies in slots a row does not see
- * has no effect on it, infinite and NaN values included. Work is split over
- * the slots where rows are few, the shares added in a fixed order: equal
- * inputs give equal bits; another batch around a sequence may split it
- * elsewhere and round differently. */
+ * per kv head have a second part that brings it to 2^-16). What lies in slots
+ * a row does not see has no effect on it, infinite and NaN values included.
+ * Work is split over the slots where rows are few, the shares added in a fixed
+ * order: equal inputs give equal bits; another batch around a sequence may
+ * split it elsewhere and round differently. */
 int dsf_paged_attention(const dsf_paged_cache* cache, const dsf_paged_batch* batch, int dtype, int Hq, const void* q,
                         int64_t q_row, int64_t q_head, int window, void* out, int64_t out_row, int64_t out_head,
                         void* workspace, size_t workspace_bytes, hipStream_t stream);

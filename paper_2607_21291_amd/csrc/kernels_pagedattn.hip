@@ -498,7 +498,7 @@ __device__ __forceinline__ float not_finite_sum(float c) {
 //
 // Bound by LDS reads at head dim 128: 32 keys and 32 values of 128 are 16 KB
 // for a wave and half turn, 128 bytes a clock and CU for keys and (transpose
-// loads) half that for values, 3072 of the 3800 clocks that two workgroups
+// loads) half that for values, four fifths of the clocks that two workgroups
 // take for a turn each. Two chunks of some 4000 tokens over 12000 to 20000
 // slots (28 heads over 4, 1.48 TFLOP): 1400 us, 1.06 PFLOP/s (a large library
 // product of the same type: 1.61). Slower there: 64 rows a wave, for half the
