@@ -336,6 +336,11 @@ struct SlotTile {
 
 // N DMA instructions of a wave: lane l of the e-th brings the 16 bytes at
 // offset(e) of `src` to lds + 1024 e + 16 l, zeros for those past `bytes`.
+// A scalar register that a vector instruction (v_readfirstlane, a spill's
+// v_readlane) writes may be an operand of a memory instruction five wait
+// states later, M0 one state after it is written; the compiler does not count
+// for inline assembly, so each of these brings its own six. (M0 is reserved:
+// the compiler keeps nothing in it, and nothing else here uses it.)
 template <int N, typename F>
 __device__ __forceinline__ void lds_dma(const char* src, int bytes, char* lds, F offset) {
   auto uniform = [](uint32_t x) { return uint32_t(__builtin_amdgcn_readfirstlane(int(x))); };
@@ -348,7 +353,7 @@ __device__ __forceinline__ void lds_dma(const char* src, int bytes, char* lds, F
   for (int e = 0; e < N; ++e)
     asm volatile(
         "s_mov_b32 m0, %0\n\t"
-        "s_nop 0\n\t"
+        "s_nop 4\n\t"
         "buffer_load_dwordx4 %1, %2, 0 offen lds"
         :
         : "s"(at + 1024 * e), "v"(offset(e)), "s"(rsrc)
