@@ -513,8 +513,12 @@ int dsf_stack_prefill(const dsf_layer_desc* desc, const dsf_layer_weights* weigh
  * Writing takes the least power of two that brings the row's largest finite
  * magnitude to 448 or less (2^-126 at least; an all-zero row has 2^-126) and
  * rounds to the nearest code, ties to even; infinities become the largest
- * code, NaN stays NaN. Powers of two leave that rounding the only one: codes
- * widen to bf16 and fp32 exactly. */
+ * code, NaN stays NaN. In a row that needs 2^120 the largest code is 240, as
+ * 256 * 2^120 is past the types' numbers, so what was written finite or
+ * infinite is read back finite. Powers of two leave that rounding the only
+ * one: codes widen to fp32 exactly, and to bf16 but for values below 2^-126,
+ * which become the nearest multiple of 2^-133. Bytes are 1 to 247 then; a
+ * cache filled otherwise keeps to them and to those codes. */
 enum { DSF_E4M3 = 2 };
 
 typedef struct dsf_paged_cache {

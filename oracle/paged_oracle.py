@@ -24,11 +24,11 @@ def e4m3_value(code: int) -> float:
 E4M3 = np.array([e4m3_value(c) for c in range(256)])
 
 
-def e4m3_code(x: np.ndarray) -> np.ndarray:
-    """Codes of the nearest e4m3 numbers, ties to the even code; |x| over 448 saturates, NaN is 0x7f."""
+def e4m3_code(x: np.ndarray, limit: float = 448.0) -> np.ndarray:
+    """Codes of the nearest e4m3 numbers, ties to the even code; |x| over `limit` (a code) saturates, NaN is 0x7f."""
     x = np.asarray(x, dtype=np.float64)
     mags = E4M3[:0x7f]  # ascending
-    a = np.minimum(np.abs(x), 448.0)
+    a = np.minimum(np.abs(x), limit)
     hi = np.minimum(np.searchsorted(mags, a), 0x7e)
     lo = np.maximum(hi - 1, 0)
     with np.errstate(invalid="ignore"):
@@ -50,14 +50,14 @@ def row_exponent(row: np.ndarray) -> int:
 
 
 def quantise(rows: np.ndarray):
-    """rows [..., hd] -> (codes, exponent bytes [...])."""
+    """rows [..., hd] -> (codes, exponent bytes [...]); with 2^120 codes up to 240, so that all of them widen to fp32."""
     rows = np.asarray(rows, dtype=np.float64)
     flat = rows.reshape(-1, rows.shape[-1])
     codes = np.empty(flat.shape, dtype=np.uint8)
     exps = np.empty(flat.shape[0], dtype=np.uint8)
     for i, r in enumerate(flat):
         e = row_exponent(r)
-        codes[i] = e4m3_code(r * math.ldexp(1.0, -e))
+        codes[i] = e4m3_code(r * math.ldexp(1.0, -e), 240.0 if e == 120 else 448.0)
         exps[i] = e + 127
     return codes.reshape(rows.shape), exps.reshape(rows.shape[:-1])
 

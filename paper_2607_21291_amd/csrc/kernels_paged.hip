@@ -52,9 +52,9 @@ __device__ __forceinline__ void paged_put(const Raw8<T>& raw, void* pool, uint8_
       top = fmaxf(top, a < INFINITY ? a : 0.f);  // NaN compares false
     }
     const uint32_t e = paged_exponent(lanes_max<HD / 8>(top));
-    const float inv = paged_scale(254 - e);
+    const float inv = paged_scale(254 - e), limit = paged_code_limit(e);
     *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(pool) + slot_row * HD + 8 * part) =
-        u32x2{paged_codes4(x, inv), paged_codes4(x + 4, inv)};
+        u32x2{paged_codes4(x, inv, limit), paged_codes4(x + 4, inv, limit)};
     if (part == 0) exps[slot_row] = uint8_t(e);
   }
 }

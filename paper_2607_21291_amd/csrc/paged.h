@@ -59,28 +59,32 @@ __device__ __forceinline__ uint32_t paged_exponent(float top) {
   const int e = int(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);
   return uint32_t(max(e, 1));
 }
+// The largest code of a row with that byte: 448, and 240 where e is 120, its
+// greatest value: 256 * 2^120, the next code, is past fp32's and bf16's numbers.
+__device__ __forceinline__ float paged_code_limit(uint32_t byte) { return byte >= 247 ? 240.f : 448.f; }
 // Four numbers times inv (2^-e: exact) to four codes, round to nearest even.
 // Infinities become the largest code, NaN the NaN code.
-__device__ __forceinline__ uint32_t paged_codes4(const float* x, float inv) {
+__device__ __forceinline__ uint32_t paged_codes4(const float* x, float inv, float limit) {
   float y[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float t = x[i] * inv;
-    y[i] = t != t ? t : fminf(fmaxf(t, -448.f), 448.f);
+    y[i] = t != t ? t : fminf(fmaxf(t, -limit), limit);
   }
   int r = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
   r = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], r, true);
   return uint32_t(r);
 }
-// Four codes times 2^e as bf16 (exact: four significant bits, and bf16 has
-// fp32's exponents).
+// Four codes times 2^e as bf16: exact (four significant bits, and bf16 has
+// fp32's exponents) down to 2^-126, below it to the nearest multiple of
+// 2^-133.
 __device__ __forceinline__ u32x2 paged_widen4(uint32_t c, float scale) {
   u32x2 r;
   r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, false));
   r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, true));
   return r;
 }
-// and as fp32
+// and as fp32 (exact)
 __device__ __forceinline__ f32x4 paged_widen4_f32(uint32_t c, float scale) {
   const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, scale, false);
   const auto b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, scale, true);

@@ -1,0 +1,57 @@
+"""Paged caches at the edges of their types and of a batch."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2607_21291_amd as P
+from oracle import paged_oracle as G
+
+from gpu_util import announce
+from paged_util import DT, Setup
+
+pytestmark = pytest.mark.gpu
+
+MARK = 9.0
+
+
+def _run(dev, s, hq, window=0, q=None):
+    q = s.rows(hq, seed=11) if q is None else q
+    c, batch = s.device(dev)
+    out = torch.full((s.n_rows, hq, s.hd), MARK, dtype=DT[s.dtype], device=dev)
+    P.paged_attention(c, batch, q.to(dev), out, window=window)
+    torch.cuda.synchronize()
+    return q, out.cpu()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_codes_of_the_largest_numbers_read_back_finite(dev, dtype):
+    """Rows whose largest number lies around 448 2^119 and 248 2^120, up to the type's largest, with and without an
+    infinity: 240 2^120 is the most that comes back, and what attention over such values gives is finite."""
+    top = torch.finfo(DT[dtype]).max
+    edges = [1.5 * 2.0 ** 127, 1.75 * 2.0 ** 127, 1.765625 * 2.0 ** 127, 1.9375 * 2.0 ** 127, 3.38e38, top]
+    rows = [torch.full((64,), float(e), dtype=torch.float64).to(DT[dtype]) for e in edges]
+    for r in list(rows):
+        x = r.clone()
+        x[7], x[8], x[9] = float("inf"), float("-inf"), -1.0
+        rows.append(x)
+    x = torch.stack(rows)[:, None]
+    n = x.shape[0]
+    s = Setup([(n, n)], hkv=1, hd=64, page=16, dtype=dtype, cache="e4m3")
+    announce(f"paged write of the largest numbers {dtype}")
+    c, batch = s.device(dev)
+    P.paged_cache_write(c, batch, x.to(dev), x.to(dev))
+    k, v = (torch.empty_like(x, device=dev) for _ in range(2))
+    P.paged_cache_read(c, batch, k, v)
+    # one slot seen by each row, so that nothing but its value counts
+    out = torch.empty(n, 1, 64, dtype=DT[dtype], device=dev)
+    P.paged_attention(c, batch, torch.zeros_like(out), out, window=1)
+    torch.cuda.synchronize()
+    want = torch.from_numpy(G.widen(*G.quantise(x.double().numpy())))
+    assert want.abs().max() == 240 * 2.0 ** 120
+    for got in (k, v):
+        assert torch.equal(got.cpu().double(), want)
+    finite = torch.isfinite(x)
+    # half a step: 2^-4 relative for normal codes, and the least codes (the -1) lie 2^-9 2^e apart, e at most 120
+    off = (want - x.double()).abs()[finite] - (2.0 ** -4 * x.double().abs()[finite]).clamp_min(2.0 ** 110)
+    assert off.max() <= 0
+    assert torch.equal(out.cpu().double(), want)
