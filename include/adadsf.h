@@ -590,7 +590,10 @@ size_t dsf_paged_attention_workspace_size(const dsf_paged_cache* cache, const ds
  * accumulation are fp32. bf16: the probabilities go into the product with v
  * as bf16 (off by 2^-8 at most each; sequences of up to 64 rows times heads
  * per kv head have a second part that brings it to 2^-16). What lies in slots
- * a row does not see has no effect on it, infinite and NaN values included.
+ * a row does not see has no effect on it, infinite and NaN values included;
+ * an infinite value that it does see makes that dimension infinite (NaN with
+ * one of the other sign, and possibly where its weight is below 2^-126).
+ * Scores of -inf weigh nothing; a row that has no other gives zeros.
  * Work is split over the slots where rows are few, the shares added in a fixed
  * order: equal inputs give equal bits; another batch around a sequence may
  * split it elsewhere and round differently. */

@@ -434,10 +434,11 @@ struct CodeSlots {
 };
 
 // A masked slot weighs nothing, but 0 times an infinite or NaN value is NaN.
-// Where a tile hides slots from some of its rows, such values are therefore
-// taken out of the product (finite_or_zero) and counted in a second one of
-// codes (1: inf, 256: -inf, 65536: NaN, exact sums of at most 64) with ones
-// at the slots that a row sees, and what a row saw is added to its sum.
+// Where a tile hides slots from some of its rows (bf16 tokens: everywhere),
+// such values are therefore taken out of the product (finite_or_zero) and
+// counted in a second one of codes (1: inf, 256: -inf, 65536: NaN, exact sums
+// of at most 64) with ones at the slots that a row sees, and what a row saw is
+// added to its sum.
 //
 // Bits 15 and 31 of the result: whether a half of some word has an exponent
 // field of ones (adding one to that field carries into them then).
@@ -1150,30 +1151,39 @@ __device__ __forceinline__ void paged_token(const PagedKernelArgs& a, int block,
           at[c] = vs + (((2 * db + vch) ^ S::swz(vrow)) << 4) + 32 * ks * S::kRowBytes;
         }
         lds_read_tr4x2<S::kRowBytes>(at, v);
+        auto values = [&v](int c) DSF_INLINE {
+          return __builtin_bit_cast(bf16x8, u32x4{v[2 * c][0], v[2 * c][1], v[2 * c + 1][0], v[2 * c + 1][1]});
+        };
+        // bf16 also where every row sees every slot: infinity times a weight's second part, which is 0 or below, would
+        // make it NaN. Codes are finite or NaN.
+        bool fix = false;
+        if (!E8 || masked) {
+          uint32_t odd = 0;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) odd |= not_finite_bits(values(c));
+          fix = __builtin_amdgcn_ballot_w64(odd != 0) != 0;
+        }
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           const int db = (c0 + c) % ND, ks = (c0 + c) / ND;
-          const u32x4 raw = {v[2 * c][0], v[2 * c][1], v[2 * c + 1][0], v[2 * c + 1][1]};
-          bf16x8 vf = __builtin_bit_cast(bf16x8, raw);
-          if (masked) {
-            if (__builtin_amdgcn_ballot_w64(not_finite_bits(vf) != 0)) {
+          bf16x8 vf = values(c);
+          if (fix) {
 #pragma unroll
-              for (int r = 0; r < NR; ++r) {
-                const int top = min(slot_of[r], end - 1) - kb0 - 4 * grp - 32 * ks;
-                const int lo = a.window ? slot_of[r] - a.window + 1 - kb0 - 4 * grp - 32 * ks : -TK;
-                bf16x8 one;
+            for (int r = 0; r < NR; ++r) {
+              const int top = min(slot_of[r], end - 1) - kb0 - 4 * grp - 32 * ks;
+              const int lo = a.window ? slot_of[r] - a.window + 1 - kb0 - 4 * grp - 32 * ks : -TK;
+              bf16x8 one;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                  const int x = 16 * (j / 4) + j % 4;
-                  one[j] = (__bf16)(x > top || x < lo ? 0.f : 1.f);
-                }
-                const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-                const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(not_finite_codes(vf), one, zero, 0, 0, 0);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[r][db][i] += not_finite_sum(n[i]);
+              for (int j = 0; j < 8; ++j) {
+                const int x = 16 * (j / 4) + j % 4;
+                one[j] = (__bf16)(x > top || x < lo ? 0.f : 1.f);
               }
-              vf = finite_or_zero(vf);
+              const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+              const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(not_finite_codes(vf), one, zero, 0, 0, 0);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[r][db][i] += not_finite_sum(n[i]);
             }
+            vf = finite_or_zero(vf);
           }
 #pragma unroll
           for (int r = 0; r < NR; ++r) {

@@ -7,7 +7,7 @@ import paper_2607_21291_amd as P
 from oracle import paged_oracle as G
 
 from gpu_util import announce
-from paged_util import DT, Setup
+from paged_util import DT, Setup, attention_bound
 
 pytestmark = pytest.mark.gpu
 
@@ -55,3 +55,46 @@ def test_codes_of_the_largest_numbers_read_back_finite(dev, dtype):
     off = (want - x.double()).abs()[finite] - (2.0 ** -4 * x.double().abs()[finite]).clamp_min(2.0 ** 110)
     assert off.max() <= 0
     assert torch.equal(out.cpu().double(), want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [1, 10, 30, 100])  # times two heads: every form of the kernels
+@pytest.mark.parametrize("hd", [32, 64, 128])
+def test_values_that_are_not_finite_reach_every_row_that_sees_them(dev, dtype, rows, hd):
+    """One infinite or NaN value, in slots of whole tiles and of the first and last: that dimension of every row is it
+    (its weight is far from 0), the others are what they were."""
+    kv, at = 700, (0, 130, 400, 700 - rows)
+    for value in (float("inf"), float("-inf"), float("nan")):
+        for i, slot in enumerate(at):
+            s = Setup([(rows, kv), (1, 20)], hkv=1, hd=hd, page=16, dtype=dtype, cache=dtype)
+            announce(f"paged attention {dtype} hd={hd} rows={rows}: {value} in slot {slot}")
+            q = s.rows(2, seed=11)
+            ref, spread = s.attention(q)
+            s.v[s.pages[0, slot // 16], 0, slot % 16, 5 + i] = value
+            got = _run(dev, s, 2, q=q)[1].double().numpy()
+            seen, col = got[:rows, :, 5 + i], 5 + i
+            assert np.all(np.isnan(seen) if np.isnan(value) else seen == value)
+            got[:rows, :, col] = ref[:rows, :, col]
+            assert np.all(np.abs(got - ref) <= attention_bound(s, q, ref, spread, 2 * rows <= 64))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [1, 10, 30, 100])
+def test_scores_of_minus_infinity_weigh_nothing(dev, dtype, rows):
+    """Keys of -inf under queries above 0 in all slots but some: rows attend to those; in all slots: zeros."""
+    for kept in ([3, 350, 699 - rows], []):
+        s = Setup([(rows, 700)], hkv=1, hd=64, page=16, dtype=dtype, cache=dtype)
+        q = s.rows(2, seed=11).abs() + 0.125
+        k = torch.stack([s.k[s.pages[0, j // 16], 0, j % 16] for j in kept]).double() if kept else None
+        v = torch.stack([s.v[s.pages[0, j // 16], 0, j % 16] for j in kept]).double() if kept else None
+        for j in set(range(700)) - set(kept):
+            s.k[s.pages[0, j // 16], 0, j % 16] = float("-inf")
+        announce(f"paged attention {dtype} rows={rows}: scores of -inf but in {kept}")
+        got = _run(dev, s, 2, q=q)[1].double()
+        if not kept:
+            assert (got == 0).all()
+            continue
+        w = torch.softmax(q.double() @ k.t() / 8.0, -1)
+        far = (got - w @ v).abs().numpy()
+        # (the bound's score sum goes by the finite keys)
+        assert np.all(far <= attention_bound(s, q, (w @ v).numpy(), (w @ v.abs()).numpy(), 2 * rows <= 64))
