@@ -40,6 +40,15 @@ struct PagedKernelArgs {
   float2* part_ml; // [item][kv head][BM]: maximum (log2 units), sum
 };
 
+// Rows of a sequence (tokens times heads of a kv head) up to which its weights
+// have 16 bits, whatever else is in the batch and whichever kernel takes it:
+// the token kernel where no sequence may have more by the batch's bounds, else
+// the chunk kernel (but for the sequences of one token). A choice for what a
+// decoding step answers, not for time: 16 sequences of 49 rows over 500 to
+// 6000 slots take 44.1 us, as chunks with 8 bits 33.1; 64 of 28 rows 112.5 and
+// 114.8; those 16 beside a chunk of 512 over 4096 slots 75, with 8 bits 67.
+constexpr int kTokenRows = 64;
+
 // ------------------------------------------------------------ work items
 
 // Sum and inclusive prefix sum of a small number over the wave.
@@ -498,6 +507,15 @@ __device__ __forceinline__ float not_finite_sum(float c) {
 // in use and one on its way. Turns with hidden slots and the last run in a
 // general form of the same.
 //
+// PRECISE, for sequences of up to kTokenRows rows: two waves' rows are all, so
+// a wave takes one half of every tile, with a second bf16 part of the weights
+// in the product (the sum is of the fp32 ones), and at the end the second
+// halves' results go to the first ones' waves. Scores, softmax and product
+// follow each other. (Both halves by one wave: 16 sequences of 49 rows beside
+// a chunk 90 us where weights of 8 bits took 64, with 60 to 120 bytes of
+// spills; this way 75 and 67. A function of its own, so that neither form's
+// registers count for the other.)
+//
 // DMA into LDS is issued in inline assembly: the compiler, which cannot tell
 // the stages apart, would wait for it before every transpose load. e4m3 codes
 // come as they are and are widened on their way to the stage a turn later.
@@ -520,8 +538,9 @@ template <int HD>
 constexpr int kCodeBytes = 16 * HD > 1024 ? 16 * HD : 1024;
 template <int HD, bool E8>
 constexpr int kChunkLds = 4 * 64 * SlotTile<HD>::kRowBytes + (E8 ? 8 * kCodeBytes<HD> : 0);
-template <int HD, bool E8>
-__device__ __forceinline__ void paged_chunk(const PagedKernelArgs& a, int block, char* smem) {
+template <int HD, bool E8, bool PRECISE>
+__device__ __forceinline__ void paged_chunk_tile(const PagedKernelArgs& a, const PagedItem& it, int block, int kvh,
+                                                 char* smem) {
   using S = SlotTile<HD>;
   constexpr int BM = 128, NS = HD / 16, ND = HD / 32;
   constexpr int kTile = 64 * S::kRowBytes;
@@ -529,16 +548,12 @@ __device__ __forceinline__ void paged_chunk(const PagedKernelArgs& a, int block,
   constexpr float kNothing = -3.0e38f;  // the maximum of nothing: finite, so that -inf less it is -inf
   const int tid = threadIdx.x, lane = tid & 63, r32 = lane & 31, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // kv head innermost: consecutive workgroups go to different XCDs, so that
-  // (with 8 heads or a divisor of 8) an XCD's L2 sees the slots of few heads
-  const int item = block / a.by_Hkv, kvh = block - item * a.pool.Hkv;
-  const PagedItem it = paged_item(a, item, lane);
-  if (it.b < 0) return;
+  const int half = wave >> 1;  // PRECISE
   const PagedWork w = paged_work(a, it);
   if (w.splits > 1 && w.begin >= w.end) return;  // a split that none of the tile's rows sees
 
   // this wave's rows: row m of the sequence, its token's slot
-  const int m0 = w.tile * BM + wave * 32, m = m0 + r32, mc = min(m, w.M - 1);
+  const int m0 = w.tile * BM + (PRECISE ? wave & 1 : wave) * 32, m = m0 + r32, mc = min(m, w.M - 1);
   const int tok = mc / a.by_G, g = mc - tok * a.G, my_slot = w.p0 + tok;
   bf16x8 qf[NS];
   {
@@ -682,8 +697,8 @@ __device__ __forceinline__ void paged_chunk(const PagedKernelArgs& a, int block,
     l_run += f.sum;
     m_run = f.m_new;
   };
-  // product of a half of tile t, where some row may not see some slot
-  auto product = [&](int t, int half, const bf16x8 (&p)[2]) DSF_INLINE {
+  // product of a half of tile t, where some row may not see some slot; `low`: the weights' second parts, or none
+  auto product = [&](int t, int half, const bf16x8 (&p)[2], const bf16x8* low) DSF_INLINE {
     const int at = (t & 1) * kTile + 32 * half * S::kRowBytes;
 #pragma unroll
     for (int db = 0; db < ND; ++db) {
@@ -711,7 +726,10 @@ __device__ __forceinline__ void paged_chunk(const PagedKernelArgs& a, int block,
         for (int i = 0; i < 16; ++i) o[db][i] += not_finite_sum(c[i]);
       }
 #pragma unroll
-      for (int st = 0; st < 2; ++st) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[st], p[st], o[db], 0, 0, 0);
+      for (int st = 0; st < 2; ++st) {
+        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[st], p[st], o[db], 0, 0, 0);
+        if (low) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[st], low[st], o[db], 0, 0, 0);
+      }
     }
   };
   auto hide = [&](int t, int half, f32x16& s) DSF_INLINE {
@@ -760,6 +778,26 @@ __device__ __forceinline__ void paged_chunk(const PagedKernelArgs& a, int block,
     asm volatile("" : "+v"(p_now[0]), "+v"(p_now[1]), "+v"(f.sum));
     settle(f);
   };
+  // PRECISE: a half's scores to weights of 16 bits, as two bf16 numbers, and their product with its values
+  auto precise_half = [&](int t, int half, f32x16& s) DSF_INLINE {
+    hide(t, half, s);
+    float mx = s[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+    Soft f;
+    f.m_new = fmaxf(pair32_max(mx) * sc, m_run);
+    f.sum = 0.f;
+    bf16x8 high[2], low[2];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float x = __builtin_amdgcn_exp2f(fmaf(s[i], sc, -f.m_new));
+      f.sum += x;
+      high[i / 8][i % 8] = (__bf16)x;
+      low[i / 8][i % 8] = (__bf16)(x - float((__bf16)x));
+    }
+    settle(f);
+    product(t, half, high, low);
+  };
   auto soft_all = [&](Soft& f, f32x16& s, bf16x8 (&p)[2]) DSF_INLINE {
 #pragma unroll
     for (int step = 0; step < 12; ++step) soft(step, f, s, p);
@@ -787,11 +825,15 @@ __device__ __forceinline__ void paged_chunk(const PagedKernelArgs& a, int block,
       else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kTileDma) : "memory");
     }
     meet();
-    scores(0, 0, s0x);
-    scores(0, 1, s1);
-    hide(0, 0, s0x);
-    soft_all(f, s0x, p0);
-    settle(f);
+    if constexpr (PRECISE) {
+      scores(0, half, s0x);
+    } else {
+      scores(0, 0, s0x);
+      scores(0, 1, s1);
+      hide(0, 0, s0x);
+      soft_all(f, s0x, p0);
+      settle(f);
+    }
     if constexpr (E8) {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       if (nt > 1) widen(1, false);
@@ -817,36 +859,75 @@ __device__ __forceinline__ void paged_chunk(const PagedKernelArgs& a, int block,
     const int t1 = max((see_hi - w.begin) / 64 - 1, t0);
     constexpr int kHalf = 32 * S::kRowBytes;
     int t = 0;
-    while (t < my_nt) {
-      if (t >= t0 && !(t & 1)) {
-        for (; t + 1 < t1; t += 2) {
-          open(t);
-          half_turn(kTile, s0x, s1, p1, 0, p0);
-          half_turn(kTile + kHalf, s1, s0x, p0, kHalf, p1);
-          open(t + 1);
-          half_turn(0, s0x, s1, p1, kTile, p0);
-          half_turn(kHalf, s1, s0x, p0, kTile + kHalf, p1);
+    if constexpr (PRECISE) {
+      // (scores of tile t before its turn, in which its keys' stage is filled again)
+      for (; t < my_nt; ++t) {
+        open(t);
+        precise_half(t, half, s0x);
+        if (t + 1 < my_nt) scores(t + 1, half, s0x);
+      }
+    } else {
+      while (t < my_nt) {
+        if (t >= t0 && !(t & 1)) {
+          for (; t + 1 < t1; t += 2) {
+            open(t);
+            half_turn(kTile, s0x, s1, p1, 0, p0);
+            half_turn(kTile + kHalf, s1, s0x, p0, kHalf, p1);
+            open(t + 1);
+            half_turn(0, s0x, s1, p1, kTile, p0);
+            half_turn(kHalf, s1, s0x, p0, kTile + kHalf, p1);
+          }
+          if (t >= my_nt) break;
         }
-        if (t >= my_nt) break;
+        open(t);
+        const bool more = t + 1 < my_nt;
+        if (more) scores(t + 1, 0, s0x);
+        hide(t, 1, s1);
+        soft_all(f, s1, p1);
+        product(t, 0, p0, nullptr);
+        settle(f);
+        if (more) {
+          scores(t + 1, 1, s1);
+          hide(t + 1, 0, s0x);
+          soft_all(f, s0x, p0);
+        }
+        product(t, 1, p1, nullptr);
+        if (more) settle(f);
+        ++t;
       }
-      open(t);
-      const bool more = t + 1 < my_nt;
-      if (more) scores(t + 1, 0, s0x);
-      hide(t, 1, s1);
-      soft_all(f, s1, p1);
-      product(t, 0, p0);
-      settle(f);
-      if (more) {
-        scores(t + 1, 1, s1);
-        hide(t + 1, 0, s0x);
-        soft_all(f, s0x, p0);
-      }
-      product(t, 1, p1);
-      if (more) settle(f);
-      ++t;
     }
     for (; t < nt; ++t) open(t);  // for the other waves
+    if constexpr (PRECISE) {
+      // the second halves' results to the waves that have the first ones'
+      meet();  // every wave is done with the stages
+      f32x4* os = reinterpret_cast<f32x4*>(smem) + (wave & 1) * 8 * HD + lane;
+      float2* mls = reinterpret_cast<float2*>(smem + 256 * HD) + (wave & 1) * 64 + lane;
+      if (half) {
+#pragma unroll
+        for (int db = 0; db < ND; ++db)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            os[64 * (4 * db + i)] = f32x4{o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]};
+        *mls = make_float2(m_run, l_run);
+      }
+      meet();
+      if (half) return;
+      const float2 ml = *mls;
+      const float top = fmaxf(m_run, ml.x);
+      const float f0 = __builtin_amdgcn_exp2f(m_run - top), f1 = __builtin_amdgcn_exp2f(ml.x - top);
+#pragma unroll
+      for (int db = 0; db < ND; ++db)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f32x4 x = os[64 * (4 * db + i)];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[db][4 * i + j] = o[db][4 * i + j] * f0 + x[j] * f1;
+        }
+      l_run = l_run * f0 + ml.y * f1;
+      m_run = top;
+    }
   }
+  if (PRECISE && half) return;
 
   // lane holds O^T[dim 32 db + 8 (i / 4) + 4 hi + i % 4][row r32]
   const float l = pair32_sum(l_run);
@@ -874,6 +955,17 @@ __device__ __forceinline__ void paged_chunk(const PagedKernelArgs& a, int block,
         *reinterpret_cast<u32x2*>(op + 32 * db + 8 * i + 4 * hi) = pk;
       }
   }
+}
+
+template <int HD, bool E8>
+__device__ __forceinline__ void paged_chunk(const PagedKernelArgs& a, int block, char* smem) {
+  // kv head innermost: consecutive workgroups go to different XCDs, so that
+  // (with 8 heads or a divisor of 8) an XCD's L2 sees the slots of few heads
+  const int item = block / a.by_Hkv, kvh = block - item * a.pool.Hkv;
+  const PagedItem it = paged_item(a, item, threadIdx.x & 63);
+  if (it.b < 0) return;
+  if (it.w.M > kTokenRows) paged_chunk_tile<HD, E8, false>(a, it, block, kvh, smem);
+  else paged_chunk_tile<HD, E8, true>(a, it, block, kvh, smem);
 }
 
 // ------------------------------------------------------------ a few tokens
@@ -1651,11 +1743,6 @@ struct PagedPlan {
   size_t places;   // of shares, per kv head
 };
 
-// Rows of a sequence (tokens times heads of a kv head) up to which the token
-// kernel takes it, with weights of 16 bits. A choice for what a decoding step
-// answers, not for time: 16 sequences of 49 rows over 500 to 6000 slots take
-// 42.2 us, as chunks 33.1; 64 of 28 rows 112.5 and 114.8.
-constexpr int kTokenRows = 64;
 // Workgroups aimed at with splits, of all kv heads: two to a CU. A chunk of
 // 512 over 8192 slots takes 45.5 us (256: 46.6, 1024: 60.2), the mixed batch
 // 57 (59.2, 58.5), a window 55.5 (55.5, 78.5).

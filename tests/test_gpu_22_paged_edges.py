@@ -98,3 +98,47 @@ def test_scores_of_minus_infinity_weigh_nothing(dev, dtype, rows):
         far = (got - w @ v).abs().numpy()
         # (the bound's score sum goes by the finite keys)
         assert np.all(far <= attention_bound(s, q, (w @ v).numpy(), (w @ v.abs()).numpy(), 2 * rows <= 64))
+
+
+def _within_its_rows_bound(s, q, out, window=0):
+    """Every sequence against the bound of its own rows times heads, whatever else is in the batch."""
+    ref, spread = s.attention(q, window)
+    got = out.double().numpy()
+    group = q.shape[1] // s.hkv
+    for b, (n, _) in enumerate(s.seqs):
+        n = min(n, s.max_rows)
+        rows = slice(s.row_start[b], s.row_start[b] + n)
+        bound = attention_bound(s, q, ref[rows], spread[rows], n * group <= 64)
+        far = np.abs(got[rows] - ref[rows]) - bound
+        assert far.max(initial=-1.0) <= 0.0, f"sequence {b}, {n} rows of {group} heads: {far.max():.3e} over the bound"
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("window", [0, 200])
+@pytest.mark.parametrize("hq,hkv,seqs", [
+    (14, 2, [(3, 300), (200, 400), (1, 1500), (9, 90), (10, 200), (2, 2)]),
+    (2, 2, [(40, 300), (64, 700), (65, 1300), (130, 130), (17, 2100), (16, 64)]),
+    (20, 1, [(1, 300), (2, 1400), (3, 500), (100, 200), (4, 70)]),
+    (40, 1, [(1, 300), (2, 200), (50, 90), (1, 2000)]),
+    (70, 1, [(1, 300), (2, 200)]),
+    (100, 100, [(50, 80), (100, 120), (64, 1100), (1, 9)]),
+])
+def test_precision_goes_by_the_sequences_own_rows(dev, cache, window, hq, hkv, seqs):
+    """Up to 64 rows times heads have 16 bits of each weight beside chunks too."""
+    s = Setup(seqs, hkv=hkv, hd=32 if hkv > 2 else 64, page=16, cache=cache, pad=1)
+    announce(f"paged attention {cache} heads {hq}/{hkv} window {window}: precision by rows")
+    q, out = _run(dev, s, hq, window=window)
+    _within_its_rows_bound(s, q, out, window)
+    assert (out[-1] == MARK).all()
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("hq,hkv", [(14, 2), (12, 12), (20, 1)])
+def test_precision_does_not_go_by_the_batchs_bounds(dev, cache, hq, hkv):
+    """A captured step of up to 512 rows that brings one token, or a few: 16 bits as well."""
+    for n in (1, 3):
+        s = Setup([(n, 1600)], hkv=hkv, hd=128, page=64, cache=cache, pad=512 - n, max_rows=512)
+        announce(f"paged attention {cache} heads {hq}/{hkv}: {n} rows of up to 512")
+        q, out = _run(dev, s, hq)
+        _within_its_rows_bound(s, q, out)
+        assert (out[n:] == MARK).all()
