@@ -1789,9 +1789,15 @@ PagedPlan split_plan(const PagedBatch& pb, int G, int Hkv, int bm_shift, int m_l
   return p;
 }
 
-PagedPlan flat_plan(const PagedBatch& pb, int G, int Hkv, int bm_shift, int m_hi) {
+// per_cu: workgroups to a CU, for one round of equal shares: eight waves of 16
+// rows (comment at paged_token), or four of more rows, fill it; beside chunks 16
+// rows have four, two to a CU. One to a CU there: 9 tokens over long e4m3
+// sequences in a batch with room for chunks 83.2 us for 57.5, 64 bf16 tokens
+// 137 for 102; with a chunk of 512 over 4096 slots 129 for 110 and 188 for 164.
+// (32 sequences of 14 rows with a chunk of 256: 25.4 for 26.4.)
+PagedPlan flat_plan(const PagedBatch& pb, int G, int Hkv, int bm_shift, int m_hi, int per_cu) {
   PagedPlan p = tiles_plan(pb, G, bm_shift, 0, m_hi);
-  p.items = std::max(256 / Hkv, 1);  // a workgroup to a CU, one round of equal shares (comment at paged_token)
+  p.items = std::max(256 * per_cu / Hkv, 1);
   const int64_t slots = int64_t(pb.max_pages) << pb.page_shift;
   // (row_start that does not ascend may claim all tiles of every sequence)
   const int64_t most = int64_t(pb.B) * (((m_hi - 1) >> bm_shift) + 1);
@@ -1812,7 +1818,8 @@ void paged_plans(int dtype, int Hq, const PagedPool& pool, const PagedBatch& pb,
   const int64_t most = int64_t(std::min(pb.max_rows, pb.n_rows)) * G;
   // sequences of one token stay with the token kernel beside ones with chunks
   const int few = most <= kTokenRows ? int(most) : std::min((G + 15) / 16 * 16, kTokenRows);
-  if (most <= kTokenRows || pb.B > 1) p[0] = flat_plan(pb, G, pool.Hkv, few <= 16 ? 4 : few <= 32 ? 5 : 6, few);
+  const int shift = few <= 16 ? 4 : few <= 32 ? 5 : 6;
+  if (most <= kTokenRows || pb.B > 1) p[0] = flat_plan(pb, G, pool.Hkv, shift, few, most > kTokenRows && shift == 4 ? 2 : 1);
   if (most > kTokenRows) p[1] = split_plan(pb, G, pool.Hkv, 7, pb.B > 1 ? few : 0, 0x7fffffff, kChunkItems);
 }
 
