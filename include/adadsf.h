@@ -543,7 +543,8 @@ typedef struct dsf_paged_cache {
  * others: n_rows and max_rows are then upper bounds. row_start ascends within
  * [0, n_rows]; values outside, lengths outside [0, max_pages * page_size] and
  * page numbers outside [0, n_pages) are clamped by the kernels (the result is
- * then unspecified). max_pages * page_size is at most 2^24. */
+ * then unspecified). max_pages is at least 1, max_pages * page_size at most
+ * 2^24. */
 typedef struct dsf_paged_batch {
   const int32_t* row_start; /* [B + 1] */
   const int32_t* kv_len;    /* [B] */

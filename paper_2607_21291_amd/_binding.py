@@ -471,10 +471,10 @@ class PagedBatch:
     values may change between calls (also between replays of a captured one)."""
 
     def __init__(self, row_start, kv_len, pages, n_rows: int, max_rows: int):
-        B = kv_len.shape[0]
         if any(t.dtype != torch.int32 for t in (row_start, kv_len, pages)):
             raise ValueError("row_start, kv_len and pages must be int32")
-        if kv_len.dim() != 1 or row_start.shape != (B + 1,) or pages.dim() != 2 or pages.shape[0] != B:
+        B = kv_len.shape[0] if kv_len.dim() == 1 else -1
+        if B < 0 or row_start.shape != (B + 1,) or pages.dim() != 2 or pages.shape[0] != B:
             raise ValueError("row_start [B + 1], kv_len [B], pages [B, max_pages]")
         if not (0 <= n_rows < 2**31 and 0 <= max_rows < 2**31):
             raise ValueError("n_rows and max_rows must be from 0 to 2^31 - 1")

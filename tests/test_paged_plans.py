@@ -1,7 +1,9 @@
-"""How the paged attention's launches are sized, as far as the workspace shows it. Nothing here launches a kernel."""
+"""How the paged attention's launches are sized, as far as the workspace shows it, and batches that are none. Nothing
+here launches a kernel."""
 import ctypes
 
 import pytest
+import torch
 
 import paper_2607_21291_amd as P
 from paper_2607_21291_amd import _binding as B
@@ -23,3 +25,12 @@ def test_tokens_beside_chunks_have_a_whole_chip_too(hq, hkv):
     beside = _need(hq, hkv, 40, 1 << 20, 1 << 15)
     assert alone == 2 * (256 // hkv) * hkv * place
     assert beside == 2 * (512 // hkv) * hkv * place
+
+
+def test_batches_of_other_dimensions_are_refused():
+    i = lambda *a: torch.tensor(a, dtype=torch.int32)
+    table = torch.zeros(1, 3, dtype=torch.int32)
+    for args in ((i(0, 1), torch.tensor(7, dtype=torch.int32), table), (i(0, 1), i(7).view(1, 1), table),
+                 (i(0, 1).view(1, 2), i(7), table), (i(0, 1), i(7), table[0])):
+        with pytest.raises(ValueError, match="row_start"):
+            P.PagedBatch(*args, 1, 1)
