@@ -118,7 +118,10 @@ __device__ __forceinline__ int paged_splits(const PagedShape& w, int per) { retu
 // Where there are fewer tiles than that, so many longer that the items are no
 // more: one round of workgroups, and a few in a second would double the time.
 // No splits where they would shorten the longest tile by a.split_gain or less.
-// w: shapes of the first 64 sequences, in lanes.
+// w: shapes of the first 64 sequences, in lanes. Batches of more are only cut
+// by the share: the two rules after it need the sequences several times over
+// (60 tokens and 4 chunks of 300, 64 sequences: 39.8 us; with one token more
+// 44.6).
 // (Even splits of what a tile sees, not of its sequence: 24 sequences with six
 // chunks 60.2 -> 57.1 us, chunks with a window 56.7 -> 55.5. Splits of one
 // place kept on one XCD, for its L2: 2 to 15 % slower, the XCDs' loads differ.)
@@ -521,19 +524,22 @@ __device__ __forceinline__ float not_finite_sum(float c) {
 // come as they are and are widened on their way to the stage a turn later.
 //
 // Bound by LDS reads at head dim 128: 32 keys and 32 values of 128 are 16 KB
-// for a wave and half turn, 128 bytes a clock and CU for keys and (transpose
-// loads) half that for values, four fifths of the clocks that two workgroups
-// take for a turn each. Two chunks of some 4000 tokens over 12000 to 20000
-// slots (28 heads over 4, 1.48 TFLOP): 1400 us, 1.06 PFLOP/s (a large library
-// product of the same type: 1.61). Slower there: 64 rows a wave, for half the
-// reads, 1595 us (one wave to a SIMD issues a vector instruction every 7
-// clocks); eight waves with 256 rows and four stages 1430; LDS addresses that
-// move with the turn instead of constant ones 1412 against 1377.
-// One chunk of 512 over 8192 slots (12 heads over 2): 45 us, the kernel 37: 5
+// for a wave and half turn. A loop of nothing else reads 124 bytes a clock and
+// CU with the keys' loads and 67 with the values' (transpose loads, in either
+// case from these addresses), so the 6.8e7 loads of the batch below, a third of
+// them keys', take 5.3e8 of the CUs' 6.8e8 clocks; matrix products take 53 % of
+// the SIMDs'. (SQ_LDS_IDX_ACTIVE counts 4 clocks for a load of keys that takes
+// 8, and 2 for one of values.) Two chunks of some 4000 tokens over 12000 to
+// 20000 slots (28 heads over 4, 1.48 TFLOP): 1360 us, 1.09 PFLOP/s (a large
+// library product of the same type: 1.61); 1420 to 1680 on some hosts. Slower,
+// where this took 1405: 64 rows a wave, for half the reads, 1595 us (one wave
+// to a SIMD issues a vector instruction every 7 clocks); eight waves with 256
+// rows and four stages 1430; LDS addresses that move with the turn instead of
+// constant ones 1412 against 1377.
+// One chunk of 512 over 8192 slots (12 heads over 2): 44 us, the kernel 38: 5
 // us to the first scores, 13 turns of 1.8 us, 6 us for 29 MB of shares.
 // LDS: two tiles of keys, two of values; e4m3: each wave's codes of a tile of
-// either. Four stages at head dim 64 gained nothing (mixed batch below: 51 us
-// either way).
+// either. Four stages at head dim 64 gained nothing.
 template <int HD>
 constexpr int kCodeBytes = 16 * HD > 1024 ? 16 * HD : 1024;
 template <int HD, bool E8>
@@ -1085,10 +1091,14 @@ struct ValueSlots {
 // nothing here.
 //
 // 64 tokens over 60 to 8100 slots each (28 heads over 4 of 128, bf16, 516 MB):
-// 97 us, 5.3 TB/s with the join (a large copy: 5.4). 9 tokens over 20000 to
-// 33000 slots, e4m3 (235 MB): 53.3 us. One token over 513 slots, 14 heads over
-// 2 of 64: 8.3 us, all of it waits. With four waves, two pieces on their way
-// instead of one: 105 us in place of 100, for registers.
+// 99 us, 5.2 TB/s with the join (a large copy: 5.4). 9 tokens over 20000 to
+// 33000 slots, e4m3 (235 MB): 53.4 us. One token over 513 slots, 14 heads over
+// 2 of 64: 8.3 us, all of it waits. Every workgroup reads all sequences'
+// lengths, and the line again for each tile it begins, so batches of very many
+// cost more than their bytes: 256 tokens over 60 to 1000 slots (14 heads over 2
+// of 64, 70 MB) 38 us, 1024 (282 MB) 153, 4096 (1.13 GB) 1095. With four
+// waves, two pieces on their way instead of one: 105 us in place of 100, for
+// registers.
 //
 // LDS: the waves' values, or 16 rows of all the waves (rows HD + 4 floats
 // apart, so that they spread over the banks); then maxima and sums.
@@ -1345,11 +1355,13 @@ __global__ __launch_bounds__(64 * W) void paged_token_kernel(PagedKernelArgs a) 
   paged_token<HD, E8, NR, W>(a, blockIdx.x, smem);
 }
 // Both, for batches that may have either: the chunks' workgroups first (their
-// work is longer), the tokens' beside them. 24 sequences, six of them with
-// chunks of 158 to 616 tokens (14 heads over 2 of 64, e4m3): 57.7 us, as two
-// launches 72.2; five chunks with a window 55.5 and 58.6; two long chunks 1380
-// either way. What bounds the first is its longest items (26 turns of 64 slots
-// at 1.5 us, the average is 18) after 5.5 us to the first scores.
+// work is longer), the tokens' where those leave places, which chunks cut for
+// the whole chip do only as they end. 24 sequences, six of them with chunks of
+// 158 to 616 tokens (14 heads over 2 of 64, e4m3): 55.4 us (as two launches
+// 72.2, where one took 57.7); five chunks with a window 55.9 (58.6 and 55.5);
+// two long chunks the same either way. What bounds the first is its longest
+// items (26 turns of 64 slots at 1.5 us, the average is 18) after 5.5 us to the
+// first scores.
 template <int HD, bool E8>
 __global__ __launch_bounds__(256, 2) void paged_mixed_kernel(PagedKernelArgs chunks, PagedKernelArgs tokens) {
   constexpr int kLds = kChunkLds<HD, E8> > kTokenLds<HD, 1, 4> ? kChunkLds<HD, E8> : kTokenLds<HD, 1, 4>;
@@ -1370,7 +1382,10 @@ __global__ __launch_bounds__(256, 2) void paged_mixed_kernel(PagedKernelArgs chu
 // 4 s + grp as they come from memory. Loads of the next piece during this
 // one's product cost more in registers than they hid (21.0 -> 24.1 us): other
 // waves hide them. Two chunks of 77 to 200 tokens over 350 to 1000 slots, 12
-// heads of 64 (0.39 GFLOP): 21 us, the kernel 16.5; at head dim 128 47 us.
+// heads of 64 (0.39 GFLOP): 21.5 us, the kernel 17; at head dim 128 47 us. 900
+// over 3900 slots and 500 over 2000 (12.2 GFLOP): 213 us, 57 TFLOP/s, 229 from
+// e4m3 pages. 16 tokens over 500 to 6000 slots, 12 heads over 2 of 128: 33.1
+// us (91 MB), from e4m3 29.5 (23 MB).
 template <int HD, bool E8>
 __global__ __launch_bounds__(256) void paged_f32_kernel(PagedKernelArgs a) {
   constexpr int NK = HD / 16, DPL = HD / 16, KV = 32;
@@ -1744,8 +1759,8 @@ struct PagedPlan {
 };
 
 // Workgroups aimed at with splits, of all kv heads: two to a CU. A chunk of
-// 512 over 8192 slots takes 45.5 us (256: 46.6, 1024: 60.2), the mixed batch
-// 57 (59.2, 58.5), a window 55.5 (55.5, 78.5).
+// 512 over 8192 slots took 45.5 us (256: 46.6, 1024: 60.2), the mixed batch
+// 57 (59.2, 58.5), a window 55.5 (55.5, 78.5), each in one comparison.
 constexpr int kChunkItems = 512;
 // fp32: three to a CU. Short chunks 20.9 us (512: 22.1, 1536: 20.9), 500 to
 // 900 tokens over 2000 to 4000 slots 314.5 (314.1, 317.4).
@@ -1781,7 +1796,9 @@ PagedPlan split_plan(const PagedBatch& pb, int G, int Hkv, int bm_shift, int m_l
   PagedPlan p = tiles_plan(pb, G, bm_shift, m_lo, m_hi);
   const int64_t blocks = (int64_t(pb.max_pages) << pb.page_shift) / 64;
   // (with two rounds of tiles and more nothing is split: the last round is a small part then, and 4 chunks of 500 to 900
-  // tokens over 3000 to 9000 slots, 1.1 rounds, are split and take 104 us)
+  // tokens over 3000 to 9000 slots, 1.1 rounds, are split and take 104 us. Tiles are counted by n_rows, so a captured
+  // step should not have room for many more rows than it brings: a chunk of 512 over 8192 slots, 44 us, takes 146 in a
+  // batch with room for 11000)
   if (blocks > kSplitMinBlocks && p.tiles <= 4096 && int64_t(p.tiles) * Hkv < 2 * total) p.target = std::max(total / Hkv, 1);
   p.items = p.tiles + p.target;
   p.join = p.target != 0;
