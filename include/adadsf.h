@@ -648,6 +648,108 @@ int dsf_align_stack_forward(const dsf_layer_desc* desc, const dsf_layer_weights*
                             int flags, double* hid_accum, void* workspace, size_t workspace_bytes,
                             hipStream_t stream);
 
+/* ------------------- the ends of a training step: embedding, norm, head */
+
+/* What stands before and behind the stack when a model is trained: tokens to
+ * rows, the norm before the head, and the head's losses, each with its
+ * gradients. dL/dh of a loss goes through dsf_norm_backward into the gradient at
+ * the stack's output, dsf_sparse_block_backward's per layer lead to the gradient
+ * at its input, and dsf_embed_backward ends the step. Weight gradients come in
+ * fp32 or in the weights' type. Launches of these calls have no timing class. */
+
+/* out[i, :] = scale * table[tokens[i], :] for i < n_tokens; zeros for a token
+ * outside [0, n_classes). tokens: device int32; table [n_classes, d], out
+ * [n_tokens, d] in dtype, 16-byte aligned; d a multiple of 8. The product is
+ * rounded once; with scale 1 the rows are copied bit by bit. */
+int dsf_embed_forward(const int32_t* tokens, const void* table, int dtype, int64_t n_tokens, int n_classes, int d,
+                      float scale, void* out, hipStream_t stream);
+
+/* Workspace bytes of dsf_embed_backward (0 on a bad argument). */
+size_t dsf_embed_backward_workspace_size(int64_t n_tokens, int d, int n_classes);
+
+/* The table's gradient: dtable[v, :] = scale * sum over the positions i with
+ * tokens[i] == v of dy[i, :], zeros for tokens that do not occur; with
+ * accumulate != 0 it is added to what dtable holds (rows of tokens that do not
+ * occur are not touched), for a table that is the head's as well. Positions
+ * whose token lies outside [0, n_classes) have no effect, whatever their dy.
+ * dy [n_tokens, d] in dtype; dtable [n_classes, d] of type dtable_type: DSF_F32,
+ * or dtype. Sums are fp32, in an order that tokens fix: equal calls give equal
+ * bits. n_tokens below 2^30. The workspace (256-byte aligned) needs no
+ * initialisation; calls that overlap in time, and graphs whose replays may, need
+ * separate ones. */
+int dsf_embed_backward(const int32_t* tokens, const void* dy, int dtype, int64_t n_tokens, int n_classes, int d,
+                       float scale, int accumulate, void* dtable, int dtable_type, void* workspace,
+                       size_t workspace_bytes, hipStream_t stream);
+
+/* LayerNorm or (rms != 0) RMSNorm of n_rows rows: with m the row's mean (0 with
+ * rms) and r = (mean (x - m)^2 + eps)^(-1/2),
+ *   out = (x - m) r w + b.
+ * x, out [n_rows, d], w, b [d] in dtype, 16-byte aligned; b nullable. out may be
+ * x. d a multiple of 8, at most 16384. Statistics are fp32, the row's mean
+ * subtracted before the squares are taken. */
+int dsf_norm_forward(const void* x, const void* w, const void* b, int dtype, int64_t n_rows, int d, float eps, int rms,
+                     void* out, hipStream_t stream);
+
+/* Workspace bytes of dsf_norm_backward (0 on a bad argument). */
+size_t dsf_norm_backward_workspace_size(int64_t n_rows, int d);
+
+/* The adjoint of dsf_norm_forward. With xh = (x - m) r and g = dy w,
+ *   dx = add + r (g - mean g - xh mean(g xh))   (rms: without mean g),
+ *   dw = sum over rows of dy xh,  db = sum over rows of dy.
+ * dx [n_rows, d] in dtype, nullable; add nullable, in dtype (the gradient that
+ * goes past the norm); dx may be dy or add. dw, db: device float [d], nullable,
+ * overwritten (zeros for n_rows == 0); db null with rms. Statistics are taken
+ * from x again. Sums in an order that n_rows and d fix. The workspace as above. */
+int dsf_norm_backward(const void* x, const void* dy, const void* w, const void* add, int dtype, int64_t n_rows, int d,
+                      float eps, int rms, void* dx, float* dw, float* db, void* workspace, size_t workspace_bytes,
+                      hipStream_t stream);
+
+/* Workspace bytes of the head's losses: top = 0 for dsf_head_cross_entropy, the
+ * entries of a row for dsf_head_distill; gradients != 0 if dh or dw are wanted
+ * (also enough for calls without). It holds 16 bits (fp32: 32) for each logit of
+ * as many rows as fit 2 GiB, and for calls of more rows than that the sum of dw
+ * in fp32; never the logits of a call at once. 0 on a bad argument. */
+size_t dsf_head_workspace_size(int dtype, int64_t n_rows, int d, int n_classes, int top, int gradients);
+
+/* Cross entropy of a linear head. For rows h[i] and logits z_i = h[i] W^T over
+ * n_classes classes,
+ *   loss_i = log sum_c exp(z_ic) - z_i,target(i),
+ *   L = grad_scale * sum_i weight_i loss_i   (mean != 0: over sum_i weight_i),
+ * and, for those of dh, dw that are given, dL/dh and dL/dW. A row whose target
+ * lies outside [0, n_classes), or of weight 0, takes no part: its loss and dh
+ * are 0, and what h holds there has no effect.
+ * h [n_rows, d], w [n_classes, d] in dtype, 16-byte aligned; targets int32
+ * [n_rows]; row_weight float [n_rows], null: ones. row_loss (nullable, float
+ * [n_rows]): loss_i. total (nullable, float [2]): sum_i weight_i loss_i, and
+ * sum_i weight_i (both 0 without rows). dh [n_rows, d] in dtype; dw [n_classes,
+ * d] of type dw_type: DSF_F32, or dtype. All are overwritten. With mean and
+ * weights that sum to 0 the gradients are 0.
+ * bf16: the products' operands are bf16; of the gradient at the logits,
+ * weight (p - q), that is the one rounding (2^-8) but for a relative 2^-11 of p.
+ * Logits, log-sums and accumulation are fp32, total is summed in 64 bits.
+ * d a multiple of 8, at most 16384; n_classes at most 2^21, n_rows at most 2^24.
+ * Equal calls give equal bits. Workspace (256-byte aligned) as above. */
+int dsf_head_cross_entropy(const void* h, const void* w, int dtype, int64_t n_rows, int d, int n_classes,
+                           const int32_t* targets, const float* row_weight, float grad_scale, int mean, float* row_loss,
+                           float* total, void* dh, void* dw, int dw_type, void* workspace, size_t workspace_bytes,
+                           hipStream_t stream);
+
+/* Distillation of a linear head from a teacher's top logits. Row i has top
+ * entries: classes top_classes[i, j] with the teacher's logits top_logits[i, j].
+ * With q_i = softmax over them of top_logits / temperature, and p_i = softmax
+ * over all classes of z_i / temperature,
+ *   loss_i = temperature^2 sum_j q_ij (log q_ij - log p_i,class(j)).
+ * An entry whose class lies outside [0, n_classes), or whose logit is -inf, is
+ * none (lists may be shorter than top); a class that a list names twice counts
+ * with both entries. A row without entries, or of weight 0, takes no part. L,
+ * the outputs and the other arguments are dsf_head_cross_entropy's.
+ * top_classes int32, top_logits float, [n_rows, top], top from 1 to 1024;
+ * temperature positive and finite. */
+int dsf_head_distill(const void* h, const void* w, int dtype, int64_t n_rows, int d, int n_classes,
+                     const int32_t* top_classes, const float* top_logits, int top, float temperature,
+                     const float* row_weight, float grad_scale, int mean, float* row_loss, float* total, void* dh,
+                     void* dw, int dw_type, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
 /* ------------------------------------------------------- kernel timing */
 
 /* Per-kernel timing with HIP events recorded around each launch on the

@@ -13,5 +13,6 @@ from ._binding import (  # noqa: F401
     sparse_block_forward, stack_forward, timing_enable, timing_read, topk_select, version, workspace_size,
     workspace_status, WS_STATUS_SK_TIMEOUT, backward_workspace_size, sparse_block_backward, GRAD_FIELDS,
     LayerGrads, E4M3, PAGE_SIZES, PagedBatch, PagedCache, paged_attention, paged_attention_workspace_size,
-    paged_cache_read, paged_cache_write,
+    paged_cache_read, paged_cache_write, embed_backward, embed_backward_workspace_size, embed_forward,
+    head_cross_entropy, head_distill, head_workspace_size, norm_backward, norm_backward_workspace_size, norm_forward,
 )

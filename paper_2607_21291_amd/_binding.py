@@ -41,6 +41,9 @@ EXPORTS = [
     "dsf_workspace_status", "dsf_decode_static_scratch_bytes", "dsf_decode_step_static",
     "dsf_backward_workspace_size", "dsf_sparse_block_backward",
     "dsf_paged_cache_write", "dsf_paged_cache_read", "dsf_paged_attention_workspace_size", "dsf_paged_attention",
+    "dsf_embed_forward", "dsf_embed_backward_workspace_size", "dsf_embed_backward", "dsf_norm_forward",
+    "dsf_norm_backward_workspace_size", "dsf_norm_backward", "dsf_head_workspace_size", "dsf_head_cross_entropy",
+    "dsf_head_distill",
 ]
 WS_STATUS_SK_TIMEOUT = 1
 
@@ -137,6 +140,16 @@ def lib() -> ctypes.CDLL:
         "dsf_paged_cache_read": ([vp, vp, i32, vp, i64, i64, vp, i64, i64, vp], i32),
         "dsf_paged_attention_workspace_size": ([vp, vp, i32, i32], sz),
         "dsf_paged_attention": ([vp, vp, i32, i32, vp, i64, i64, i32, vp, i64, i64, vp, sz, vp], i32),
+        "dsf_embed_forward": ([vp, vp, i32, i64, i32, i32, f32, vp, vp], i32),
+        "dsf_embed_backward_workspace_size": ([i64, i32, i32], sz),
+        "dsf_embed_backward": ([vp, vp, i32, i64, i32, i32, f32, i32, vp, i32, vp, sz, vp], i32),
+        "dsf_norm_forward": ([vp, vp, vp, i32, i64, i32, f32, i32, vp, vp], i32),
+        "dsf_norm_backward_workspace_size": ([i64, i32], sz),
+        "dsf_norm_backward": ([vp, vp, vp, vp, i32, i64, i32, f32, i32, vp, vp, vp, vp, sz, vp], i32),
+        "dsf_head_workspace_size": ([i32, i64, i32, i32, i32, i32], sz),
+        "dsf_head_cross_entropy": ([vp, vp, i32, i64, i32, i32, vp, vp, f32, i32, vp, vp, vp, vp, i32, vp, sz, vp], i32),
+        "dsf_head_distill": ([vp, vp, i32, i64, i32, i32, vp, vp, i32, f32, vp, f32, i32, vp, vp, vp, vp, i32, vp, sz, vp],
+                             i32),
     }
     for name, (args, res) in sig.items():
         fn = getattr(L, name)
@@ -568,6 +581,158 @@ def paged_attention(cache: PagedCache, batch: PagedBatch, q, out, window: int = 
         raise ValueError("the workspace must be contiguous")
     _paged_call("dsf_paged_attention", cache, batch, stream, dtype, heads, *qp, window, *op, workspace.data_ptr(),
                 workspace.nbytes)
+
+
+# ------------------------------------- the ends of a training step: embedding, norm, head
+
+def _dense(name: str, t, shape, dtypes, like):
+    """Pointer of a contiguous tensor of that shape, of one of the dtypes, on `like`'s device (None: null)."""
+    if t is None:
+        return None
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name}: {' or '.join(str(d) for d in dtypes)} expected, got {t.dtype}")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name}: shape {list(shape)} expected, got {list(t.shape)}")
+    if t.get_device() != like.get_device():
+        raise ValueError(f"{name} lies on {t.device}, not on {like.device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _scratch(workspace, need: int, like, stream):
+    """Pointer, bytes and the tensor of a call's workspace: the caller's, or a new one."""
+    if workspace is None:
+        # on the stream that uses it, so that its memory is not handed on before that
+        with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=like.device)
+    elif workspace.get_device() != like.get_device():
+        raise ValueError(f"workspace lies on {workspace.device}, not on {like.device}")
+    elif not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous")
+    return workspace.data_ptr(), workspace.nbytes, workspace
+
+
+def _call_on(name: str, like, stream, *args):
+    """The C entry point `name` with the tensors' device current, on the given stream or that device's current one."""
+    index = like.get_device()
+    if index < 0:
+        raise ValueError(f"the tensors lie on {like.device}, not on a GPU")
+    if stream is not None and stream.device.index != index:
+        raise ValueError(f"the stream belongs to {stream.device}, the tensors to {like.device}")
+    fn = getattr(_lib or lib(), name)
+    if index == torch.cuda.current_device():
+        rc = fn(*args, _stream(stream))
+    else:
+        with torch.cuda.device(index):
+            rc = fn(*args, _stream(stream))
+    if rc:
+        _check(name, rc)
+
+
+_I32, _F32 = (torch.int32,), (torch.float32,)
+
+
+def embed_forward(tokens, table, out, scale: float = 1.0, stream=None):
+    """out [..., d] = scale * table [n_classes, d] at tokens int32 [...]; zeros for tokens outside the table."""
+    dtype = _dtype_code(table)
+    if table.dim() != 2:
+        raise ValueError("table: [n_classes, d]")
+    V, d = table.shape
+    n = tokens.numel()
+    _call_on("dsf_embed_forward", table, stream, _dense("tokens", tokens, tuple(tokens.shape), _I32, table),
+             _dense("table", table, (V, d), (table.dtype,), table), dtype, n, V, d, float(scale),
+             _dense("out", out, (*tokens.shape, d), (table.dtype,), table))
+
+
+def embed_backward_workspace_size(n_tokens: int, d: int, n_classes: int) -> int:
+    return lib().dsf_embed_backward_workspace_size(n_tokens, d, n_classes)
+
+
+def embed_backward(tokens, dy, dtable, scale: float = 1.0, accumulate: bool = False, workspace=None, stream=None):
+    """dtable [n_classes, d] (float32, or dy's dtype) = or += scale * the sums of dy [..., d] by token."""
+    dtype = _dtype_code(dy)
+    if dtable.dim() != 2:
+        raise ValueError("dtable: [n_classes, d]")
+    V, d = dtable.shape
+    n = tokens.numel()
+    tp = _dense("tokens", tokens, tuple(tokens.shape), _I32, dy)
+    yp = _dense("dy", dy, (*tokens.shape, d), (dy.dtype,), dy)
+    gp = _dense("dtable", dtable, (V, d), (torch.float32, dy.dtype), dy)
+    wp, wb, keep = _scratch(workspace, embed_backward_workspace_size(n, d, V) if workspace is None else 0, dy, stream)
+    _call_on("dsf_embed_backward", dy, stream, tp, yp, dtype, n, V, d, float(scale), int(accumulate), gp,
+             _dtype_code(dtable), wp, wb)
+
+
+def norm_forward(x, w, out, b=None, eps: float = 1e-5, rms: bool = False, stream=None):
+    """out = LayerNorm (rms: RMSNorm) of x [..., d] with gain w [d] and bias b [d] or None. out may be x."""
+    dtype = _dtype_code(x)
+    d = x.shape[-1] if x.dim() else 0
+    n = x.numel() // d if d else 0
+    t = (x.dtype,)
+    _call_on("dsf_norm_forward", x, stream, _dense("x", x, tuple(x.shape), t, x), _dense("w", w, (d,), t, x),
+             _dense("b", b, (d,), t, x), dtype, n, d, float(eps), int(rms), _dense("out", out, tuple(x.shape), t, x))
+
+
+def norm_backward_workspace_size(n_rows: int, d: int) -> int:
+    return lib().dsf_norm_backward_workspace_size(n_rows, d)
+
+
+def norm_backward(x, dy, w, dx, dw=None, db=None, add=None, eps: float = 1e-5, rms: bool = False, workspace=None,
+                  stream=None):
+    """dx [..., d] (or None) = add + the adjoint of norm_forward at dy; dw, db float32 [d] or None."""
+    dtype = _dtype_code(x)
+    d = x.shape[-1] if x.dim() else 0
+    n = x.numel() // d if d else 0
+    t, shape = (x.dtype,), tuple(x.shape)
+    ptrs = [_dense("x", x, shape, t, x), _dense("dy", dy, shape, t, x), _dense("w", w, (d,), t, x),
+            _dense("add", add, shape, t, x)]
+    outs = [_dense("dx", dx, shape, t, x), _dense("dw", dw, (d,), _F32, x), _dense("db", db, (d,), _F32, x)]
+    wp, wb, keep = None, 0, None
+    if workspace is not None or dw is not None or db is not None:
+        wp, wb, keep = _scratch(workspace, norm_backward_workspace_size(n, d) if workspace is None else 0, x, stream)
+    _call_on("dsf_norm_backward", x, stream, *ptrs, dtype, n, d, float(eps), int(rms), *outs, wp, wb)
+
+
+def head_workspace_size(dtype: int, n_rows: int, d: int, n_classes: int, top: int = 0, gradients: bool = True) -> int:
+    return lib().dsf_head_workspace_size(dtype, n_rows, d, n_classes, top, int(gradients))
+
+
+def _head(name: str, h, w, lists, middle, top, row_weight, row_loss, total, dh, dw, grad_scale, mean, workspace, stream):
+    dtype = _dtype_code(h)
+    if h.dim() < 1 or w.dim() != 2:
+        raise ValueError("h: [..., d], w: [n_classes, d]")
+    V, d = w.shape
+    rows = tuple(h.shape[:-1])
+    n = h.numel() // d if d else 0
+    t = (h.dtype,)
+    hp, wp = _dense("h", h, (*rows, d), t, h), _dense("w", w, (V, d), t, h)
+    lp = [_dense(what, x, (*rows, *more), kind, h) for what, x, more, kind in lists]
+    rw, rl = _dense("row_weight", row_weight, rows, _F32, h), _dense("row_loss", row_loss, rows, _F32, h)
+    tp, dhp = _dense("total", total, (2,), _F32, h), _dense("dh", dh, (*rows, d), t, h)
+    dwp = _dense("dw", dw, (V, d), (torch.float32, h.dtype), h)
+    need = head_workspace_size(dtype, n, d, V, top, dh is not None or dw is not None) if workspace is None else 0
+    sp, sb, keep = _scratch(workspace, need, h, stream)
+    _call_on(name, h, stream, hp, wp, dtype, n, d, V, *lp, *middle, rw, float(grad_scale), int(mean), rl, tp, dhp, dwp,
+             _dtype_code(dw) if dw is not None else dtype, sp, sb)
+
+
+def head_cross_entropy(h, w, targets, row_loss=None, total=None, dh=None, dw=None, row_weight=None,
+                       grad_scale: float = 1.0, mean: bool = False, workspace=None, stream=None):
+    """Cross entropy of the head w [n_classes, d] on rows h [..., d] with targets int32 [...] (others than classes: the
+    row takes no part), and its gradients: row_loss, row_weight float32 [...], total float32 [2] (sum of weighted
+    losses, sum of weights), dh as h, dw [n_classes, d] float32 or as w; None: not wanted (row_weight: ones)."""
+    _head("dsf_head_cross_entropy", h, w, [("targets", targets, (), _I32)], (), 0, row_weight, row_loss, total, dh, dw,
+          grad_scale, mean, workspace, stream)
+
+
+def head_distill(h, w, top_classes, top_logits, temperature: float = 1.0, row_loss=None, total=None, dh=None, dw=None,
+                 row_weight=None, grad_scale: float = 1.0, mean: bool = False, workspace=None, stream=None):
+    """The head's loss against a teacher's top logits: top_classes int32, top_logits float32 [..., top]; entries of
+    other numbers than classes are none. The rest as head_cross_entropy."""
+    top = top_classes.shape[-1] if top_classes.dim() else 0
+    _head("dsf_head_distill", h, w, [("top_classes", top_classes, (top,), _I32), ("top_logits", top_logits, (top,), _F32)],
+          (top, float(temperature)), top, row_weight, row_loss, total, dh, dw, grad_scale, mean, workspace, stream)
 
 
 def timing_enable(max_records: int, kinds: Optional[Sequence[str]] = None):

@@ -19,7 +19,8 @@ LIB = os.path.join(PKG, "libadadsf.so")
 
 SOURCES = ["api.hip", "kernels_misc.hip", "kernels_router.hip", "kernels_align.hip", "kernels_gemm.hip",
            "kernels_rowgemm.hip", "kernels_attn.hip", "kernels_decode.hip", "kernels_wgrad.hip", "kernels_bwd.hip",
-           "kernels_paged.hip", "kernels_pagedattn.hip"]
+           "kernels_paged.hip", "kernels_pagedattn.hip", "kernels_embed.hip", "kernels_norm.hip", "kernels_head.hip",
+           "kernels_headgemm.hip", "kernels_headf32.hip"]
 # per-source extra flags: attention keeps its MFMA accumulators in ordinary
 # VGPRs, so the softmax reads scores and rescales outputs without AGPR moves
 EXTRA = {"kernels_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],

@@ -16,6 +16,7 @@
 
 #include "adadsf.h"
 #include "dsf_internal.h"
+#include "head.h"
 
 using namespace dsf;
 
@@ -1785,4 +1786,199 @@ extern "C" int dsf_sparse_block_backward(const dsf_layer_desc* desc, const dsf_l
   // kept rows: dx = dy + the block's gradient (the residual path carries dy)
   DSF_HIP(launch_scatter_grad(dy, F(p.acc), B, T, d, idx, k, dx, s));
   return DSF_OK;
+}
+
+// ---------------- the ends of a training step: embedding, norm, head
+
+// The type of a weight gradient: fp32, or the call's.
+static int check_grad_type(const char* name, int type, int dtype) {
+  DSF_CHECK(type == DSF_F32 || type == dtype, DSF_EUNSUPPORTED, "%s %d is neither DSF_F32 nor the call's dtype", name, type);
+  return DSF_OK;
+}
+
+static int check_width(int d) {
+  DSF_CHECK(d > 0 && d % 8 == 0 && d <= norm_rows_max_d(), DSF_EUNSUPPORTED, "d must be a multiple of 8, from 8 to %d",
+            norm_rows_max_d());
+  return DSF_OK;
+}
+
+static int check_workspace(const void* workspace, size_t have, size_t need) {
+  DSF_CHECK((reinterpret_cast<uintptr_t>(workspace) & 255u) == 0, DSF_EINVAL, "the workspace must be 256-byte aligned");
+  DSF_CHECK(need == 0 || (workspace && have >= need), DSF_EWORKSPACE, "workspace needs %zu bytes", need);
+  return DSF_OK;
+}
+
+static int check_embed(int64_t n_tokens, int n_classes, int d) {
+  DSF_CHECK(n_tokens >= 0 && n_tokens < (int64_t(1) << 30), DSF_EINVAL, "n_tokens must be from 0 to 2^30 - 1");
+  DSF_CHECK(n_classes > 0 && n_classes < (1 << 30), DSF_EINVAL, "n_classes must be from 1 to 2^30 - 1");
+  return check_width(d);
+}
+
+extern "C" int dsf_embed_forward(const int32_t* tokens, const void* table, int dtype, int64_t n_tokens, int n_classes,
+                                 int d, float scale, void* out, hipStream_t stream) {
+  int rc = check_dtype(dtype);
+  if (rc) return rc;
+  rc = check_embed(n_tokens, n_classes, d);
+  if (rc) return rc;
+  if (n_tokens == 0) return DSF_OK;
+  DSF_CHECK(tokens && table && out, DSF_EINVAL, "null pointer");
+  DSF_CHECK(aligned16(table) && aligned16(out) && (uintptr_t(tokens) & 3u) == 0, DSF_EINVAL,
+            "table and out must be 16-byte aligned, tokens 4-byte aligned");
+  rc = check_device();
+  if (rc) return rc;
+  DSF_HIP(launch_embed(dtype, tokens, table, int(n_tokens), n_classes, d, scale, out, stream));
+  return DSF_OK;
+}
+
+extern "C" size_t dsf_embed_backward_workspace_size(int64_t n_tokens, int d, int n_classes) {
+  if (check_embed(n_tokens, n_classes, d)) return 0;
+  return embed_backward_workspace_bytes(int(n_tokens), d, n_classes);
+}
+
+extern "C" int dsf_embed_backward(const int32_t* tokens, const void* dy, int dtype, int64_t n_tokens, int n_classes,
+                                  int d, float scale, int accumulate, void* dtable, int dtable_type, void* workspace,
+                                  size_t workspace_bytes, hipStream_t stream) {
+  int rc = check_dtype(dtype);
+  if (rc) return rc;
+  rc = check_embed(n_tokens, n_classes, d);
+  if (rc) return rc;
+  rc = check_grad_type("dtable_type", dtable_type, dtype);
+  if (rc) return rc;
+  DSF_CHECK(dtable && (n_tokens == 0 || (tokens && dy)), DSF_EINVAL, "null pointer");
+  DSF_CHECK(aligned16(dtable) && aligned16(dy) && (uintptr_t(tokens) & 3u) == 0, DSF_EINVAL,
+            "dy and dtable must be 16-byte aligned, tokens 4-byte aligned");
+  rc = check_workspace(workspace, workspace_bytes, embed_backward_workspace_bytes(int(n_tokens), d, n_classes));
+  if (rc) return rc;
+  if (n_tokens == 0 && accumulate) return DSF_OK;
+  rc = check_device();
+  if (rc) return rc;
+  const EmbedBackwardArgs a{dtype, dtable_type, tokens, dy, int(n_tokens), n_classes, d, scale, accumulate != 0, dtable,
+                            workspace};
+  DSF_HIP(launch_embed_backward(a, stream));
+  return DSF_OK;
+}
+
+static int check_norm(int64_t n_rows, int d, float eps) {
+  DSF_CHECK(n_rows >= 0 && n_rows < (int64_t(1) << 31), DSF_EINVAL, "n_rows must be from 0 to 2^31 - 1");
+  DSF_CHECK(eps >= 0.f && std::isfinite(eps), DSF_EINVAL, "eps must be finite and not negative");
+  return check_width(d);
+}
+
+extern "C" int dsf_norm_forward(const void* x, const void* w, const void* b, int dtype, int64_t n_rows, int d, float eps,
+                                int rms, void* out, hipStream_t stream) {
+  int rc = check_dtype(dtype);
+  if (rc) return rc;
+  rc = check_norm(n_rows, d, eps);
+  if (rc) return rc;
+  if (n_rows == 0) return DSF_OK;
+  DSF_CHECK(x && w && out, DSF_EINVAL, "null pointer");
+  DSF_CHECK(aligned16(x) && aligned16(w) && aligned16(b) && aligned16(out), DSF_EINVAL, "pointers must be 16-byte aligned");
+  rc = check_device();
+  if (rc) return rc;
+  DSF_HIP(launch_norm_rows(dtype, rms != 0, x, w, b, n_rows, d, eps, out, stream));
+  return DSF_OK;
+}
+
+extern "C" size_t dsf_norm_backward_workspace_size(int64_t n_rows, int d) {
+  if (check_norm(n_rows, d, 0.f)) return 0;
+  return up256(norm_backward_workspace_bytes(n_rows, d));
+}
+
+extern "C" int dsf_norm_backward(const void* x, const void* dy, const void* w, const void* add, int dtype,
+                                 int64_t n_rows, int d, float eps, int rms, void* dx, float* dw, float* db,
+                                 void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  int rc = check_dtype(dtype);
+  if (rc) return rc;
+  rc = check_norm(n_rows, d, eps);
+  if (rc) return rc;
+  DSF_CHECK(dx || dw || db, DSF_EINVAL, "no output");
+  DSF_CHECK(!(rms && db), DSF_EINVAL, "an RMSNorm has no bias: db must be null");
+  DSF_CHECK(n_rows == 0 || (x && dy && w), DSF_EINVAL, "null pointer");
+  DSF_CHECK(aligned16(x) && aligned16(dy) && aligned16(w) && aligned16(add) && aligned16(dx) && aligned16(dw) &&
+                aligned16(db),
+            DSF_EINVAL, "pointers must be 16-byte aligned");
+  if (dw || db) {
+    rc = check_workspace(workspace, workspace_bytes, norm_backward_workspace_bytes(n_rows, d));
+    if (rc) return rc;
+  }
+  if (n_rows == 0 && !dw && !db) return DSF_OK;
+  rc = check_device();
+  if (rc) return rc;
+  if (n_rows == 0) {
+    if (dw) DSF_HIP(launch_zero_u32((uint32_t*)dw, d, stream));
+    if (db) DSF_HIP(launch_zero_u32((uint32_t*)db, d, stream));
+    return DSF_OK;
+  }
+  const NormBackwardArgs a{dtype, rms != 0, x, dy, w, add, n_rows, d, eps, dx, dw, db, workspace};
+  DSF_HIP(launch_norm_backward(a, stream));
+  return DSF_OK;
+}
+
+static int check_head(int dtype, int64_t n_rows, int d, int n_classes, int top) {
+  int rc = check_dtype(dtype);
+  if (rc) return rc;
+  DSF_CHECK(n_rows >= 0 && n_rows <= (int64_t(1) << 24), DSF_EINVAL, "n_rows must be from 0 to 2^24");
+  DSF_CHECK(n_classes > 0 && n_classes <= (1 << 21), DSF_EUNSUPPORTED, "n_classes must be from 1 to 2^21");
+  DSF_CHECK(top >= 0 && top <= kHeadMaxTop, DSF_EUNSUPPORTED, "top must be at most %d", kHeadMaxTop);
+  return check_width(d);
+}
+
+extern "C" size_t dsf_head_workspace_size(int dtype, int64_t n_rows, int d, int n_classes, int top, int gradients) {
+  if (check_head(dtype, n_rows, d, n_classes, top)) return 0;
+  if (n_rows == 0) return 256;
+  return head_workspace_bytes(dtype, int(n_rows), d, n_classes, top, gradients != 0);
+}
+
+static int head_loss(const HeadLossArgs& a, int64_t n_rows, int dw_type, size_t workspace_bytes, hipStream_t stream) {
+  int rc = check_grad_type("dw_type", dw_type, a.dtype);
+  if (rc) return rc;
+  DSF_CHECK(std::isfinite(a.grad_scale), DSF_EINVAL, "grad_scale must be finite");
+  DSF_CHECK(n_rows == 0 || (a.h && a.w && a.classes), DSF_EINVAL, "null pointer");
+  DSF_CHECK(aligned16(a.h) && aligned16(a.w) && aligned16(a.dh) && aligned16(a.dw), DSF_EINVAL,
+            "h, w, dh and dw must be 16-byte aligned");
+  DSF_CHECK(((uintptr_t(a.classes) | uintptr_t(a.value) | uintptr_t(a.weight) | uintptr_t(a.row_loss) |
+              uintptr_t(a.total)) & 3u) == 0,
+            DSF_EINVAL, "targets, weights and losses must be 4-byte aligned");
+  DSF_CHECK(a.row_loss || a.total || a.dh || a.dw, DSF_EINVAL, "no output");
+  const size_t need = n_rows == 0 ? 0 : head_workspace_bytes(a.dtype, a.n, a.d, a.V, a.value ? a.k : 0, a.dh || a.dw);
+  rc = check_workspace(a.workspace, workspace_bytes, need);
+  if (rc) return rc;
+  if (n_rows == 0 && !a.total && !a.dw) return DSF_OK;
+  rc = check_device();
+  if (rc) return rc;
+  if (n_rows == 0) {
+    if (a.total) DSF_HIP(launch_zero_u32((uint32_t*)a.total, 2, stream));
+    if (a.dw)
+      DSF_HIP(launch_zero_u32((uint32_t*)a.dw, int64_t(a.V) * a.d * int64_t(elem_bytes(dw_type)) / 4, stream));
+    return DSF_OK;
+  }
+  DSF_HIP(launch_head_loss(a, stream));
+  return DSF_OK;
+}
+
+extern "C" int dsf_head_cross_entropy(const void* h, const void* w, int dtype, int64_t n_rows, int d, int n_classes,
+                                      const int32_t* targets, const float* row_weight, float grad_scale, int mean,
+                                      float* row_loss, float* total, void* dh, void* dw, int dw_type, void* workspace,
+                                      size_t workspace_bytes, hipStream_t stream) {
+  int rc = check_head(dtype, n_rows, d, n_classes, 0);
+  if (rc) return rc;
+  const HeadLossArgs a{dtype, h, w, int(n_rows), d, n_classes, targets, nullptr, 1, 1.f, row_weight, grad_scale,
+                       mean != 0, row_loss, total, dh, dw, dw_type == DSF_F32, workspace};
+  return head_loss(a, n_rows, dw_type, workspace_bytes, stream);
+}
+
+extern "C" int dsf_head_distill(const void* h, const void* w, int dtype, int64_t n_rows, int d, int n_classes,
+                                const int32_t* top_classes, const float* top_logits, int top, float temperature,
+                                const float* row_weight, float grad_scale, int mean, float* row_loss, float* total,
+                                void* dh, void* dw, int dw_type, void* workspace, size_t workspace_bytes,
+                                hipStream_t stream) {
+  int rc = check_head(dtype, n_rows, d, n_classes, top);
+  if (rc) return rc;
+  DSF_CHECK(top >= 1, DSF_EINVAL, "top must be at least 1");
+  DSF_CHECK(temperature > 0.f && std::isfinite(temperature), DSF_EINVAL, "temperature must be positive and finite");
+  DSF_CHECK(n_rows == 0 || top_logits, DSF_EINVAL, "null pointer");
+  static const float none = 0.f;
+  const HeadLossArgs a{dtype, h, w, int(n_rows), d, n_classes, top_classes, n_rows ? top_logits : &none, top, temperature,
+                       row_weight, grad_scale, mean != 0, row_loss, total, dh, dw, dw_type == DSF_F32, workspace};
+  return head_loss(a, n_rows, dw_type, workspace_bytes, stream);
 }

@@ -356,4 +356,58 @@ struct PagedAttnArgs {
 size_t paged_attention_workspace_bytes(int dtype, int Hq, const PagedPool& pool, const PagedBatch& pb);
 hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t s);
 
+// ---- embedding (kernels_embed.hip) ----
+hipError_t launch_embed(int dtype, const int32_t* tokens, const void* table, int n, int V, int d, float scale, void* out,
+                        hipStream_t s);
+struct EmbedBackwardArgs {
+  int dtype, dtable_type;  // of dy and of dtable
+  const int32_t* tokens;
+  const void* dy;
+  int n, V, d;
+  float scale;
+  int accumulate;
+  void* dtable;
+  void* workspace;  // embed_backward_workspace_bytes(n, d, V)
+};
+size_t embed_backward_workspace_bytes(int n, int d, int V);
+hipError_t launch_embed_backward(const EmbedBackwardArgs& a, hipStream_t s);
+
+// ---- norms outside the layers (kernels_norm.hip) ----
+int norm_rows_max_d();
+hipError_t launch_norm_rows(int dtype, bool rms, const void* x, const void* w, const void* b, int64_t n, int d, float eps,
+                            void* out, hipStream_t s);
+struct NormBackwardArgs {
+  int dtype;
+  bool rms;
+  const void* x; const void* dy; const void* w;
+  const void* add;  // nullable: dx = add + the adjoint
+  int64_t n;
+  int d;
+  float eps;
+  void* dx; float* dw; float* db;  // nullable each
+  void* workspace;                 // norm_backward_workspace_bytes(n, d)
+};
+size_t norm_backward_workspace_bytes(int64_t n, int d);
+hipError_t launch_norm_backward(const NormBackwardArgs& a, hipStream_t s);
+
+// ---- the head's losses (kernels_head.hip) ----
+struct HeadLossArgs {
+  int dtype;
+  const void* h; const void* w;
+  int n, d, V;
+  const int32_t* classes;  // targets [n], or the teacher's [n, k]
+  const float* value;      // the teacher's logits [n, k]; null: cross entropy
+  int k;
+  float temperature;
+  const float* weight;     // [n], nullable
+  float grad_scale;
+  int mean;
+  float* row_loss; float* total;  // nullable
+  void* dh; void* dw;             // nullable
+  int dw_f32;
+  void* workspace;  // head_workspace_bytes
+};
+size_t head_workspace_bytes(int dtype, int n, int d, int V, int k, bool grads);
+hipError_t launch_head_loss(const HeadLossArgs& a, hipStream_t s);
+
 }  // namespace dsf

@@ -1,0 +1,42 @@
+// Shared by the head's losses: the plan of a call, and the arguments of its
+// products and of the kernels between them.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace dsf {
+
+// A logit is held as (its tile's row maximum - z) in steps of 2^(-1/1024):
+// 16 bits reach 2^-64 of the maximum (what lies below counts as 0), and half a
+// step changes a probability by 3.4e-4 relative, a tenth of the rounding to
+// bf16 that the product with it needs anyway.
+constexpr float kHeadSteps = 1024.f;
+constexpr int kHeadTile = 256;  // classes of a tile of the logits
+constexpr int kHeadMaxTop = 1024;
+
+enum HeadMode { kHeadLogits = 0, kHeadDh = 1, kHeadDw = 2 };
+
+// One of a call's three products, over a piece of its active rows (bf16; fp32
+// the same with float operands).
+struct HeadGemmArgs {
+  const void* h;        // active rows of this piece [rows, d]
+  const void* w;        // [V, d]
+  const void* z;        // dz [rows, ldz]
+  void* zout;           // codes (fp32: logits in units of log 2) [rows, ldz]; null: statistics alone
+  float2* stats;        // bf16: [classes / 256][rows_ld] (maximum, sum)
+  float* part;          // dh partial sums [splits][rows_ld][d]
+  const float* prev;    // dW so far, fp32 (nullable)
+  float* out32;         // dW in fp32 (nullable)
+  uint16_t* out16;      // dW in bf16 (nullable)
+  const float* scale;   // factor of dW (device)
+  const int32_t* n_active;  // active rows of the call (device)
+  float z_scale;        // log2(e) / temperature
+  int row0, rows, rows_ld;  // the piece: its first active row, its rows at most, leading dimension of the above
+  int V, d, ldz;
+  int splits;           // of the reduction over classes (dh)
+};
+hipError_t launch_head_gemm(int mode, const HeadGemmArgs& g, hipStream_t s);      // kernels_headgemm.hip
+hipError_t launch_head_gemm_f32(int mode, const HeadGemmArgs& g, hipStream_t s);  // kernels_headf32.hip
+
+}  // namespace dsf

@@ -1,0 +1,598 @@
+// The head's losses (cross entropy, distillation from a teacher's top logits)
+// around their three products (kernels_headgemm.hip, kernels_headf32.hip).
+//
+// A row's target is a list of k classes with probabilities q (cross entropy:
+// one class, q = 1). With z = h W^T / T, in units of log 2, lse = log2 sum 2^z:
+//   loss = T^2 sum_j q_j (log q_j - ln 2 (z_j - lse)),  dz = T (p - q).
+// Steps: the teacher's q; the rows that take part (a target, a weight), counted
+// and listed in order; their h, gathered; z at the targets by dot products in
+// fp32; then for pieces of those rows the logits' tiles, lse and losses, dz in
+// place of the logits' codes, dh and dW. Only the listed rows cost products,
+// and what lies in the others (NaN too) has no effect.
+//
+// 16 bits per logit of a piece are all that is kept: with them the backward
+// needs no second product for the logits (three products, not four; 25 % of the
+// large call), at 6 bytes moved per logit, which cost a tenth of that product.
+#include <algorithm>
+
+#include "dsf_device.h"
+#include "dsf_internal.h"
+#include "head.h"
+
+namespace dsf {
+
+namespace {
+constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
+constexpr int kLseRows = 64;  // rows of a workgroup of the lse kernel
+
+__device__ __forceinline__ double block_sum(double v, double* lds, int tid, int nt) {
+  v = wave_sum(v);
+  if ((tid & 63) == 0) lds[tid >> 6] = v;
+  __syncthreads();
+  double t = 0.0;
+  for (int i = 0; i < nt / 64; ++i) t += lds[i];
+  __syncthreads();
+  return t;
+}
+}  // namespace
+
+// q[r][j], and plogp[r] = sum_j q_j log q_j; a row without an entry: live[r] = 0.
+// An entry counts if its class is in [0, V) and its logit is over -inf.
+__global__ __launch_bounds__(256) void head_teacher_kernel(const int32_t* __restrict__ top, const float* __restrict__ value,
+                                                           int n, int k, int V, float c, float* __restrict__ q,
+                                                           float* __restrict__ plogp, int32_t* __restrict__ live) {
+  const int lane = threadIdx.x & 63, r = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (r >= n) return;
+  const int64_t at = int64_t(r) * k;
+  auto logit = [&](int j) {
+    const float v = value[at + j];
+    return uint32_t(top[at + j]) < uint32_t(V) ? v * c : -INFINITY;
+  };
+  float m = -INFINITY;
+  int any = 0;
+  for (int j = lane; j < k; j += 64) {
+    const float v = logit(j);
+    any |= !(v == -INFINITY);
+    m = fmaxf(m, v);
+  }
+  any = __any(any);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  float sum = 0.f;
+  for (int j = lane; j < k; j += 64) {
+    const float v = logit(j);
+    sum += v == -INFINITY ? 0.f : exp2f(v - m);
+  }
+  sum = wave_sum(sum);
+  float h = 0.f;
+  for (int j = lane; j < k; j += 64) {
+    const float v = logit(j);
+    const float p = v == -INFINITY ? 0.f : exp2f(v - m) / sum;
+    q[at + j] = p;
+    if (!(p == 0.f)) h += p * ((v - m) - log2f(sum));
+  }
+  h = wave_sum(h);
+  if (lane == 0) {
+    plogp[r] = h * kLn2;
+    live[r] = any;
+  }
+}
+
+// The rows that take part, in order: act[slot] = row, slot[row] = slot or -1;
+// n_active; wsum = sum of their weights; scale = factor / wsum (mean; 0 for a
+// sum of 0) or factor. Rows that do not take part get a loss of 0. One workgroup.
+__global__ __launch_bounds__(1024) void head_rows_kernel(const int32_t* __restrict__ targets,
+                                                         const int32_t* __restrict__ live,
+                                                         const float* __restrict__ weight, int n, int V, float factor,
+                                                         int mean, int32_t* __restrict__ act, int32_t* __restrict__ slot,
+                                                         int32_t* __restrict__ n_active, double* __restrict__ wsum,
+                                                         float* __restrict__ scale, uint32_t* __restrict__ count,
+                                                         float* __restrict__ row_loss) {
+  __shared__ int part[16];
+  __shared__ double red[16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int per = (n + 1023) / 1024, r0 = std::min(n, tid * per), r1 = std::min(n, r0 + per);
+  auto takes_part = [&](int r) {
+    if (!(targets ? uint32_t(targets[r]) < uint32_t(V) : live[r] != 0)) return false;
+    return !weight || !(weight[r] == 0.f);
+  };
+  int c = 0;
+  double w = 0.0;
+  for (int r = r0; r < r1; ++r)
+    if (takes_part(r)) {
+      ++c;
+      w += weight ? double(weight[r]) : 1.0;
+    }
+  int incl = c;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int v = __shfl_up(incl, o, 64);
+    if (lane >= o) incl += v;
+  }
+  if (lane == 63) part[wave] = incl;
+  __syncthreads();
+  int at = incl - c, all = 0;
+  for (int i = 0; i < 16; ++i) {
+    if (i < wave) at += part[i];
+    all += part[i];
+  }
+  for (int r = r0; r < r1; ++r) {
+    const bool in = takes_part(r);
+    slot[r] = in ? at : -1;
+    if (in) act[at++] = r;
+    else if (row_loss) row_loss[r] = 0.f;
+  }
+  w = block_sum(w, red, tid, 1024);
+  if (tid == 0) {
+    *n_active = all;
+    *wsum = w;
+    *scale = mean ? (w == 0.0 ? 0.f : float(double(factor) / w)) : factor;
+    *count = 0u;
+  }
+}
+
+// hc[slot] = h[act[slot]], and z2[slot][j] = <h, W[class j]> z_scale for the row's
+// classes (0 for those outside [0, V)). A wave takes a row and kDots classes.
+constexpr int kDots = 4;
+template <typename T>
+__global__ __launch_bounds__(256) void head_gather_kernel(const T* __restrict__ h, const T* __restrict__ w,
+                                                          const int32_t* __restrict__ classes, int k, int V, int d,
+                                                          const int32_t* __restrict__ act,
+                                                          const int32_t* __restrict__ n_active, float z_scale,
+                                                          T* __restrict__ hc, float* __restrict__ z2) {
+  constexpr int VEC = Elem<T>::kVec;
+  const int lane = threadIdx.x & 63;
+  const int groups = (k + kDots - 1) / kDots;
+  const int64_t task = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  const int s = int(task / groups), g = int(task - int64_t(s) * groups);
+  if (s >= *n_active) return;
+  const int row = act[s];
+  const T* src = h + int64_t(row) * d;
+  const T* wr[kDots];
+  bool in[kDots];
+#pragma unroll
+  for (int u = 0; u < kDots; ++u) {
+    const int j = g * kDots + u;
+    const int c = j < k ? classes[int64_t(row) * k + j] : -1;
+    in[u] = uint32_t(c) < uint32_t(V);
+    wr[u] = w + int64_t(in[u] ? c : 0) * d;
+  }
+  float acc[kDots] = {0.f, 0.f, 0.f, 0.f};
+  for (int c = lane * VEC; c < d; c += 64 * VEC) {
+    const u32x4 raw = *reinterpret_cast<const u32x4*>(src + c);
+    if (hc && g == 0) *reinterpret_cast<u32x4*>(hc + int64_t(s) * d + c) = raw;
+    float x[VEC];
+    load_vec(src + c, x);
+#pragma unroll
+    for (int u = 0; u < kDots; ++u) {
+      float y[VEC];
+      if (in[u]) {
+        load_vec(wr[u] + c, y);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) acc[u] = fmaf(x[i], y[i], acc[u]);
+      }
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kDots; ++u) {
+    const float v = wave_sum(acc[u]);
+    if (lane == 0 && g * kDots + u < k) z2[int64_t(s) * k + g * kDots + u] = v * z_scale;
+  }
+}
+
+// fp32: (maximum, sum of 2^(z - maximum)) of a row of logits, stats[row].
+__global__ __launch_bounds__(256) void head_stats_f32_kernel(const float* __restrict__ z, int ldz, int row0, int rows_max,
+                                                             const int32_t* __restrict__ n_active,
+                                                             float2* __restrict__ stats) {
+  __shared__ float red[8];
+  const int rows = std::min(*n_active - row0, rows_max), s = blockIdx.x;
+  if (s >= rows) return;
+  const float* p = z + int64_t(s) * ldz;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  float m = -INFINITY;
+  for (int c = threadIdx.x * 4; c < ldz; c += 1024) {
+    float v[4];
+    load_vec(p + c, v);
+    m = fmaxf(fmaxf(fmaxf(m, v[0]), fmaxf(v[1], v[2])), v[3]);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  if (lane == 0) red[wave] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  const float ref = m == -INFINITY ? 0.f : m;
+  float sum = 0.f;
+  for (int c = threadIdx.x * 4; c < ldz; c += 1024) {
+    float v[4];
+    load_vec(p + c, v);
+    sum += (exp2f(v[0] - ref) + exp2f(v[1] - ref)) + (exp2f(v[2] - ref) + exp2f(v[3] - ref));
+  }
+  sum = wave_sum(sum);
+  if (lane == 0) red[4 + wave] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) stats[s] = float2{m, (red[4] + red[5]) + (red[6] + red[7])};
+}
+
+// lse[s] from the tiles' statistics, the row's loss, and the sum of weight x
+// loss: a partial sum of each workgroup, added in order by the last of the
+// call's to finish. 64 rows by 16 groups of tiles (and of target classes).
+struct HeadLseArgs {
+  const float2* stats; int tiles, rows_ld;
+  const float* z2; const float* q; const float* plogp;  // q null: one class, q = 1
+  const float* weight;
+  const int32_t* act; const int32_t* n_active;
+  const double* wsum;
+  float* lse; float* row_loss; float* total; double* partial; uint32_t* count;
+  int row0, rows, k, first, workgroups;  // first: index of this launch's first partial sum; workgroups of the call
+  float T;
+};
+__global__ __launch_bounds__(1024) void head_lse_kernel(HeadLseArgs a) {
+  __shared__ float2 st[16][kLseRows];
+  __shared__ float ls[16][kLseRows];
+  __shared__ double red[16];
+  __shared__ int last;
+  const int tid = threadIdx.x, rl = tid & 63, grp = tid >> 6;
+  const int rows = std::min(*a.n_active - a.row0, a.rows), s = blockIdx.x * kLseRows + rl;
+  const bool in = s < rows;
+  const int g = a.row0 + s;  // slot in the call
+  float M = -INFINITY, S = 0.f;
+  if (in)
+    for (int t = grp; t < a.tiles; t += 16) {
+      const float2 v = a.stats[int64_t(t) * a.rows_ld + s];
+      const float m = fmaxf(M, v.x), ref = m == -INFINITY ? 0.f : m;
+      S = S * exp2f(M - ref) + v.y * exp2f(v.x - ref);
+      M = m;
+    }
+  st[grp][rl] = float2{M, S};
+  __syncthreads();
+  M = st[0][rl].x;
+  for (int i = 1; i < 16; ++i) M = fmaxf(M, st[i][rl].x);
+  const float ref = M == -INFINITY ? 0.f : M;
+  S = 0.f;
+  for (int i = 0; i < 16; ++i) S += st[i][rl].y * exp2f(st[i][rl].x - ref);
+  const float lse = ref + log2f(S);
+  if (in && grp == 0) a.lse[s] = lse;
+  // sum_j q_j (lse - z_j)
+  const int row = in ? a.act[g] : 0;
+  float part = 0.f;
+  if (in)
+    for (int j = grp; j < a.k; j += 16) {
+      const float q = a.q ? a.q[int64_t(row) * a.k + j] : 1.f;
+      if (!(q == 0.f)) part += q * (lse - a.z2[int64_t(g) * a.k + j]);
+    }
+  ls[grp][rl] = part;
+  __syncthreads();
+  double wl = 0.0;
+  if (grp == 0 && in) {
+    float x = 0.f;
+    for (int i = 0; i < 16; ++i) x += ls[i][rl];
+    const float loss = a.T * a.T * ((a.q ? a.plogp[row] : 0.f) + kLn2 * x);
+    if (a.row_loss) a.row_loss[row] = loss;
+    wl = (a.weight ? double(a.weight[row]) : 1.0) * double(loss);
+  }
+  if (!a.total) return;
+  wl = block_sum(wl, red, tid, 1024);
+  if (tid == 0) {
+    __hip_atomic_store(a.partial + a.first + blockIdx.x, wl, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    last = __hip_atomic_fetch_add(a.count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == uint32_t(a.workgroups - 1);
+  }
+  __syncthreads();
+  if (!last) return;
+  double t = 0.0;
+  for (int i = tid; i < a.workgroups; i += 1024)
+    t += __hip_atomic_load(a.partial + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  t = block_sum(t, red, tid, 1024);
+  if (tid == 0) {
+    a.total[0] = float(t);
+    a.total[1] = float(*a.wsum);
+  }
+}
+
+// dz / T in place of the logits: weight (p - q). A workgroup takes a row and a
+// range of its classes: p from all codes, then the target classes' entries
+// from their fp32 logits (p - sum of the q of a class, also where a list names
+// it twice).
+struct HeadProbsArgs {
+  void* z; int ldz;
+  const float2* stats; int rows_ld;  // bf16: the tiles' maxima
+  const float* lse; const float* z2; const float* q;
+  const float* weight; const int32_t* classes;
+  const int32_t* act; const int32_t* n_active;
+  int row0, rows, k, V, cuts, cols;  // cols: classes of a range, a multiple of 2048
+};
+template <typename T>
+__global__ __launch_bounds__(256) void head_probs_kernel(HeadProbsArgs a) {
+  constexpr int VEC = Elem<T>::kVec;
+  const int s = int(blockIdx.x) / a.cuts, c0 = (int(blockIdx.x) - s * a.cuts) * a.cols;
+  if (s >= std::min(*a.n_active - a.row0, a.rows)) return;
+  const int c1 = std::min(a.ldz, c0 + a.cols), g = a.row0 + s;
+  const float lse = a.lse[s];
+  const int row = a.act[g];
+  const float wt = a.weight ? a.weight[row] : 1.f;
+  T* z = (T*)a.z + int64_t(s) * a.ldz;
+  for (int c = c0 + int(threadIdx.x) * VEC; c < c1; c += 256 * VEC) {
+    float p[VEC];
+    if constexpr (sizeof(T) == 2) {
+      const float top = a.stats[int64_t(c / kHeadTile) * a.rows_ld + s].x - lse;
+      const u32x4 raw = *reinterpret_cast<const u32x4*>(z + c);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t code = e ? raw[i] >> 16 : raw[i] & 0xffffu;
+          const float x = __builtin_amdgcn_exp2f(fmaf(float(code), -1.f / kHeadSteps, top));
+          p[2 * i + e] = code == 0xffffu ? 0.f : wt * x;
+        }
+    } else {
+      load_vec(z + c, p);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) p[i] = p[i] == -INFINITY ? 0.f : wt * exp2f(p[i] - lse);
+    }
+    store_vec(z + c, p);
+  }
+  __syncthreads();  // (with it the stores above have completed)
+  const int32_t* cls = a.classes + int64_t(row) * a.k;
+  const float* q = a.q ? a.q + int64_t(row) * a.k : nullptr;
+  const int hi = std::min(c1, a.V);
+  for (int j = threadIdx.x; j < a.k; j += 256) {
+    const int c = cls[j];
+    if (c < c0 || c >= hi) continue;
+    float sum = q ? q[j] : 1.f;
+    bool first = true;
+    for (int i = 0; i < a.k; ++i)
+      if (i != j && cls[i] == c) {
+        first = first && i > j;
+        sum += q ? q[i] : 1.f;
+      }
+    if (first) z[c] = Elem<T>::from_f(wt * (exp2f(a.z2[int64_t(g) * a.k + j] - lse) - sum));
+  }
+}
+
+// dh of every row: scale times the sum of its partial sums, zeros for rows that
+// do not take part (written with the first piece).
+template <typename T>
+__global__ __launch_bounds__(256) void head_dh_kernel(const float* __restrict__ part, int splits, int rows_ld, int d,
+                                                      const int32_t* __restrict__ slot, int n, int row0, int rows,
+                                                      const float* __restrict__ scale, T* __restrict__ dh) {
+  constexpr int VEC = Elem<T>::kVec;
+  const int nv = d / VEC;
+  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < int64_t(n) * nv; i += int64_t(gridDim.x) * 256) {
+    const int r = int(i / nv), c = int(i - int64_t(r) * nv) * VEC;
+    const int s = slot[r] - row0;
+    float v[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) v[e] = 0.f;
+    if (slot[r] < 0) {
+      if (row0 != 0) continue;
+    } else {
+      if (s < 0 || s >= rows) continue;
+      for (int sp = 0; sp < splits; ++sp) {
+        const float* p = part + (int64_t(sp) * rows_ld + s) * d + c;
+#pragma unroll
+        for (int e = 0; e < VEC; e += 4) {
+          float x[4];
+          load_vec(p + e, x);
+#pragma unroll
+          for (int b = 0; b < 4; ++b) v[e + b] += x[b];
+        }
+      }
+      const float f = *scale;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) v[e] *= f;
+    }
+    store_vec(dh + int64_t(r) * d + c, v);
+  }
+}
+
+// ------------------------------------------------------------------- host
+
+namespace {
+struct HeadPlan {
+  int ldz, rows, pieces, tiles, splits, cuts, cols;
+  size_t act, slot, live, scalars, q, plogp, z2, hc, lse, stats, partial, z, part, acc, total;
+};
+
+size_t up(size_t v) { return (v + 255) & ~size_t(255); }
+
+// Bytes of a piece's logits (codes), at most: rows for which a tile of products
+// still costs far more than a tile's pass over dW, which a further piece repeats.
+constexpr size_t kPieceBytes = size_t(2) << 30;
+constexpr size_t kDhPartBytes = size_t(1) << 29;
+
+HeadPlan head_plan(int dtype, int n, int d, int V, int k, bool grads) {
+  HeadPlan p{};
+  const bool f32 = dtype == DSF_F32;
+  const size_t eb = f32 ? 4 : 2;
+  p.ldz = (V + kHeadTile - 1) / kHeadTile * kHeadTile;
+  p.tiles = f32 ? 1 : p.ldz / kHeadTile;
+  const int64_t n256 = (int64_t(n) + 255) / 256 * 256;
+  // statistics alone (bf16): no logits are kept, a piece is bounded by its statistics
+  const size_t per_row = (grads || f32) ? size_t(p.ldz) * eb : size_t(p.tiles) * sizeof(float2);
+  const int64_t most = std::max<int64_t>(256, int64_t(kPieceBytes / per_row) / 256 * 256);
+  p.pieces = int((n256 + most - 1) / most);
+  p.rows = int(((n256 + p.pieces - 1) / p.pieces + 255) / 256 * 256);
+  // dh: cut the classes so that the workgroups fill their last round: a round
+  // costs nk / s k-tiles and about eight more; s partial sums are written and read
+  const int t = f32 ? 128 : 256, slots = f32 ? 512 : 256;
+  const double tiles = double((p.rows + t - 1) / t) * ((d + t - 1) / t);
+  const double nk = p.ldz / 64.0, join = double(p.rows) * d * 8 / (f32 ? 4e6 : 3e6);  // in k-tiles (0.6 us)
+  double best = 0;
+  for (int s = 1; s <= 128; ++s) {
+    if (s > 1 && (size_t(s) * p.rows * d * 4 > kDhPartBytes || nk / s < 4)) break;
+    const double cost = double(int64_t((tiles * s + slots - 1) / slots)) * (nk / s + 8) + s * join;
+    if (s == 1 || cost < best) best = cost, p.splits = s;
+  }
+  // ranges of a row for dz: about four workgroups per CU
+  p.cuts = std::max(1, std::min(p.ldz / 2048, (1024 + p.rows - 1) / p.rows));
+  p.cols = ((p.ldz + p.cuts - 1) / p.cuts + 2047) / 2048 * 2048;
+  p.cuts = (p.ldz + p.cols - 1) / p.cols;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += up(bytes);
+    return here;
+  };
+  p.scalars = take(256);
+  p.act = take(size_t(n) * 4);
+  p.slot = take(size_t(n) * 4);
+  p.live = take(size_t(n) * 4);
+  p.plogp = take(size_t(n) * 4);
+  p.q = take(size_t(n) * k * 4);
+  p.z2 = take(size_t(n) * std::max(k, 1) * 4);
+  p.lse = take(size_t(p.rows) * 4);
+  p.partial = take(size_t(p.pieces) * ((p.rows + kLseRows - 1) / kLseRows) * 8);
+  p.stats = take(size_t(p.tiles) * p.rows * sizeof(float2));
+  p.hc = take(size_t(n) * d * eb);
+  if (grads || f32) p.z = take(size_t(p.rows) * p.ldz * eb);
+  if (grads) {
+    p.part = take(size_t(p.splits) * p.rows * d * 4);
+    if (!f32 && p.pieces > 1) p.acc = take(size_t(V) * d * 4);
+  }
+  p.total = at;
+  return p;
+}
+}  // namespace
+
+size_t head_workspace_bytes(int dtype, int n, int d, int V, int k, bool grads) {
+  return head_plan(dtype, n, d, V, k, grads).total;
+}
+
+hipError_t launch_head_loss(const HeadLossArgs& a, hipStream_t s) {
+  const bool grads = a.dh || a.dw, f32 = a.dtype == DSF_F32, distill = a.value != nullptr;
+  const int k = distill ? a.k : 1;
+  const HeadPlan p = head_plan(a.dtype, a.n, a.d, a.V, distill ? a.k : 0, grads);
+  char* ws = (char*)a.workspace;
+  int32_t* n_active = (int32_t*)(ws + p.scalars);
+  float* scale = (float*)(ws + p.scalars + 8);
+  uint32_t* count = (uint32_t*)(ws + p.scalars + 16);
+  double* wsum = (double*)(ws + p.scalars + 24);
+  int32_t* act = (int32_t*)(ws + p.act);
+  int32_t* slot = (int32_t*)(ws + p.slot);
+  float* q = distill ? (float*)(ws + p.q) : nullptr;
+  float* z2 = (float*)(ws + p.z2);
+  float* lse = (float*)(ws + p.lse);
+  float2* stats = (float2*)(ws + p.stats);
+  const float z_scale = kLog2e / a.temperature;
+  hipError_t e;
+#define DSF_TRY(x) do { if ((e = (x)) != hipSuccess) return e; } while (0)
+  if (distill) {
+    head_teacher_kernel<<<(a.n + 3) / 4, 256, 0, s>>>(a.classes, a.value, a.n, k, a.V, z_scale, q, (float*)(ws + p.plogp),
+                                                      (int32_t*)(ws + p.live));
+    DSF_TRY(hipGetLastError());
+  }
+  head_rows_kernel<<<1, 1024, 0, s>>>(distill ? nullptr : a.classes, (const int32_t*)(ws + p.live), a.weight, a.n, a.V,
+                                      a.grad_scale * a.temperature, a.mean, act, slot, n_active, wsum, scale, count,
+                                      a.row_loss);
+  DSF_TRY(hipGetLastError());
+  const int64_t tasks = int64_t(a.n) * ((k + kDots - 1) / kDots);
+  const dim3 gg(uint32_t((tasks + 3) / 4));
+  if (f32)
+    head_gather_kernel<float><<<gg, 256, 0, s>>>((const float*)a.h, (const float*)a.w, a.classes, k, a.V, a.d, act,
+                                                 n_active, z_scale, (float*)(ws + p.hc), z2);
+  else
+    head_gather_kernel<uint16_t><<<gg, 256, 0, s>>>((const uint16_t*)a.h, (const uint16_t*)a.w, a.classes, k, a.V, a.d,
+                                                    act, n_active, z_scale, (uint16_t*)(ws + p.hc), z2);
+  DSF_TRY(hipGetLastError());
+  const int lse_wgs = (p.rows + kLseRows - 1) / kLseRows;
+  for (int i = 0; i < p.pieces; ++i) {
+    HeadGemmArgs g{};
+    g.row0 = i * p.rows;
+    g.rows = std::min(p.rows, a.n - g.row0);
+    if (g.rows <= 0) break;  // (the last piece may be rounded away)
+    g.rows_ld = p.rows;
+    g.h = ws + p.hc + size_t(g.row0) * a.d * (f32 ? 4 : 2);
+    g.w = a.w;
+    g.V = a.V;
+    g.d = a.d;
+    g.ldz = p.ldz;
+    g.z = ws + p.z;
+    g.zout = grads || f32 ? ws + p.z : nullptr;
+    g.stats = stats;
+    g.part = (float*)(ws + p.part);
+    g.scale = scale;
+    g.n_active = n_active;
+    g.z_scale = z_scale;
+    g.splits = 1;
+    auto product = [&](int mode) { return f32 ? launch_head_gemm_f32(mode, g, s) : launch_head_gemm(mode, g, s); };
+    DSF_TRY(product(kHeadLogits));
+    if (f32) {
+      head_stats_f32_kernel<<<g.rows, 256, 0, s>>>((const float*)g.z, p.ldz, g.row0, g.rows, n_active, stats);
+      DSF_TRY(hipGetLastError());
+    }
+    HeadLseArgs l{};
+    l.stats = stats;
+    l.tiles = p.tiles;
+    l.rows_ld = p.rows;
+    l.z2 = z2;
+    l.q = q;
+    l.plogp = (const float*)(ws + p.plogp);
+    l.weight = a.weight;
+    l.act = act;
+    l.n_active = n_active;
+    l.wsum = wsum;
+    l.lse = lse;
+    l.row_loss = a.row_loss;
+    l.total = a.total;
+    l.partial = (double*)(ws + p.partial);
+    l.count = count;
+    l.row0 = g.row0;
+    l.rows = g.rows;
+    l.k = k;
+    l.first = i * lse_wgs;
+    l.workgroups = 0;
+    for (int b = 0; b < p.pieces; ++b)
+      l.workgroups += (std::max(0, std::min(p.rows, a.n - b * p.rows)) + kLseRows - 1) / kLseRows;
+    l.T = a.temperature;
+    head_lse_kernel<<<(g.rows + kLseRows - 1) / kLseRows, 1024, 0, s>>>(l);
+    DSF_TRY(hipGetLastError());
+    if (!grads) continue;
+    HeadProbsArgs b{};
+    b.z = ws + p.z;
+    b.ldz = p.ldz;
+    b.stats = stats;
+    b.rows_ld = p.rows;
+    b.lse = lse;
+    b.z2 = z2;
+    b.q = q;
+    b.weight = a.weight;
+    b.classes = a.classes;
+    b.act = act;
+    b.n_active = n_active;
+    b.row0 = g.row0;
+    b.rows = g.rows;
+    b.k = k;
+    b.V = a.V;
+    b.cuts = p.cuts;
+    b.cols = p.cols;
+    if (f32) head_probs_kernel<float><<<g.rows * p.cuts, 256, 0, s>>>(b);
+    else head_probs_kernel<uint16_t><<<g.rows * p.cuts, 256, 0, s>>>(b);
+    DSF_TRY(hipGetLastError());
+    if (a.dh) {
+      g.splits = p.splits;
+      DSF_TRY(product(kHeadDh));
+      g.splits = 1;
+      const int64_t nv = int64_t(a.n) * a.d / (f32 ? 4 : 8);
+      const dim3 grid(uint32_t(std::min<int64_t>((nv + 255) / 256, 8192)));
+      if (f32)
+        head_dh_kernel<float><<<grid, 256, 0, s>>>(g.part, p.splits, p.rows, a.d, slot, a.n, g.row0, g.rows, scale,
+                                                   (float*)a.dh);
+      else
+        head_dh_kernel<uint16_t><<<grid, 256, 0, s>>>(g.part, p.splits, p.rows, a.d, slot, a.n, g.row0, g.rows, scale,
+                                                      (uint16_t*)a.dh);
+      DSF_TRY(hipGetLastError());
+    }
+    if (a.dw) {
+      const bool last = i + 1 == p.pieces || (i + 1) * p.rows >= a.n;
+      float* sum = a.dw_f32 ? (float*)a.dw : (float*)(ws + p.acc);
+      g.prev = i > 0 ? sum : nullptr;
+      g.out32 = a.dw_f32 || !last ? sum : nullptr;
+      g.out16 = !a.dw_f32 && last ? (uint16_t*)a.dw : nullptr;
+      DSF_TRY(product(kHeadDw));
+    }
+  }
+#undef DSF_TRY
+  return hipSuccess;
+}
+
+}  // namespace dsf

@@ -1,0 +1,296 @@
+// LayerNorm / RMSNorm of dense rows and the adjoint with the gradients of gain
+// and bias, for the norms outside the layers (the final one before the head).
+// With xh = (x - m) r, r = (mean (x - m)^2 + eps)^-1/2 (RMSNorm: m = 0):
+//   y = xh w + b;  g = dy w,  dx = r (g - mean g - xh mean(g xh)) (+ add)
+//   (RMSNorm: without mean g),  dw = sum dy xh,  db = sum dy.
+// Rows stay in registers between their one read and their write; one wave or
+// one workgroup to a row. The adjoint's workgroups walk the rows with the
+// gradients of gain and bias in registers; their partial sums are added in a
+// second launch, in an order that the number of rows fixes.
+#include <algorithm>
+#include <type_traits>
+
+#include "dsf_device.h"
+#include "dsf_internal.h"
+
+namespace dsf {
+
+namespace {
+constexpr int kBwdWgs = 1024;
+
+// Sum over the WAVES waves of a row; red: WAVES values of LDS that no other
+// sum in flight uses.
+template <int WAVES>
+__device__ __forceinline__ float row_sum(float v, float* red) {
+  v = wave_sum_fast(v);
+  if constexpr (WAVES > 1) {
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = red[0];
+#pragma unroll
+    for (int i = 1; i < WAVES; ++i) v += red[i];
+  }
+  return v;
+}
+}  // namespace
+
+// C vectors of 16 bytes a lane. WAVES 1: four rows a workgroup; 4: one.
+template <typename T, int C, int WAVES, bool RMS>
+__global__ __launch_bounds__(256) void norm_rows_kernel(const T* __restrict__ x, const T* __restrict__ w,
+                                                        const T* __restrict__ b, int64_t n, int d, float eps,
+                                                        T* __restrict__ out) {
+  constexpr int V = Elem<T>::kVec, L = 64 * WAVES;
+  __shared__ float red[2][4];
+  const int l = WAVES == 1 ? int(threadIdx.x & 63) : int(threadIdx.x);
+  const int64_t r = WAVES == 1 ? int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6) : int64_t(blockIdx.x);
+  if (r >= n) return;
+  float v[C][V];
+  float s = 0.f;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int at = (l + L * c) * V;
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[c][i] = 0.f;
+    if (at < d) load_vec(x + r * d + at, v[c]);
+  }
+  float m = 0.f;
+  if constexpr (!RMS) {
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int i = 0; i < V; ++i) s += v[c][i];
+    m = row_sum<WAVES>(s, red[0]) / float(d);
+  }
+  float q = 0.f;
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+    if ((l + L * c) * V < d)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        v[c][i] -= m;
+        q += v[c][i] * v[c][i];
+      }
+  const float rstd = 1.0f / sqrtf(row_sum<WAVES>(q, red[1]) / float(d) + eps);
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int at = (l + L * c) * V;
+    if (at >= d) continue;
+    float wv[V], bv[V];
+    load_vec(w + at, wv);
+#pragma unroll
+    for (int i = 0; i < V; ++i) bv[i] = 0.f;
+    if (b) load_vec(b + at, bv);
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[c][i] = v[c][i] * rstd * wv[i] + bv[i];
+    store_vec(out + r * d + at, v[c]);
+  }
+}
+
+// SUMS: also partial[workgroup][0] = sum dy xh, [1] = sum dy over its rows.
+template <typename T, int C, int WAVES, bool RMS, bool SUMS>
+__global__ __launch_bounds__(256) void norm_grad_kernel(const T* __restrict__ x, const T* __restrict__ dy,
+                                                        const T* __restrict__ w, const T* __restrict__ add, int64_t n,
+                                                        int d, float eps, T* __restrict__ dx,
+                                                        float* __restrict__ partial) {
+  constexpr int V = Elem<T>::kVec, L = 64 * WAVES, RPW = 4 / WAVES;  // rows of a workgroup at a time
+  __shared__ float red[2][4][4];
+  const int l = WAVES == 1 ? int(threadIdx.x & 63) : int(threadIdx.x);
+  float dw[SUMS ? C : 1][V], db[SUMS && !RMS ? C : 1][V];
+#pragma unroll
+  for (int c = 0; c < (SUMS ? C : 1); ++c)
+#pragma unroll
+    for (int i = 0; i < V; ++i) dw[c][i] = 0.f;
+#pragma unroll
+  for (int c = 0; c < (SUMS && !RMS ? C : 1); ++c)
+#pragma unroll
+    for (int i = 0; i < V; ++i) db[c][i] = 0.f;
+  const float rd = 1.0f / float(d);
+  int turn = 0;
+  for (int64_t r = int64_t(blockIdx.x) * RPW + (WAVES == 1 ? threadIdx.x >> 6 : 0); r < n;
+       r += int64_t(gridDim.x) * RPW, turn ^= 1) {
+    float xv[C][V], gv[C][V];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int at = (l + L * c) * V;
+#pragma unroll
+      for (int i = 0; i < V; ++i) xv[c][i] = gv[c][i] = 0.f;
+      if (at < d) {
+        load_vec(x + r * d + at, xv[c]);
+        load_vec(dy + r * d + at, gv[c]);
+      }
+    }
+    float m = 0.f;
+    if constexpr (!RMS) {
+      float s = 0.f;
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < V; ++i) s += xv[c][i];
+      m = row_sum<WAVES>(s, red[turn][0]) * rd;
+    }
+    float q = 0.f, sg = 0.f, sgx = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int at = (l + L * c) * V;
+      if (at >= d) continue;
+      float wv[V];
+      load_vec(w + at, wv);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        xv[c][i] -= m;
+        q += xv[c][i] * xv[c][i];
+        const float g = gv[c][i] * wv[i];
+        sg += g;
+        sgx += g * xv[c][i];
+      }
+    }
+    // three sums, one barrier
+    q = wave_sum_fast(q);
+    sgx = wave_sum_fast(sgx);
+    if constexpr (!RMS) sg = wave_sum_fast(sg);
+    if constexpr (WAVES > 1) {
+      const int wv = threadIdx.x >> 6;
+      if ((threadIdx.x & 63) == 0) {
+        red[turn][1][wv] = q;
+        red[turn][2][wv] = sgx;
+        red[turn][3][wv] = sg;
+      }
+      __syncthreads();
+      q = red[turn][1][0];
+      sgx = red[turn][2][0];
+      sg = red[turn][3][0];
+#pragma unroll
+      for (int i = 1; i < WAVES; ++i) {
+        q += red[turn][1][i];
+        sgx += red[turn][2][i];
+        sg += red[turn][3][i];
+      }
+    }
+    const float rstd = 1.0f / sqrtf(q * rd + eps);
+    const float mgx = sgx * rd * rstd * rstd, mg = RMS ? 0.f : sg * rd;  // mean(g xh) r, mean g
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int at = (l + L * c) * V;
+      if (at >= d) continue;
+      float wv[V], o[V];
+      load_vec(w + at, wv);
+#pragma unroll
+      for (int i = 0; i < V; ++i) o[i] = 0.f;
+      if (add) load_vec(add + r * d + at, o);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        o[i] += rstd * (gv[c][i] * wv[i] - mg - xv[c][i] * mgx);
+        if constexpr (SUMS) {
+          dw[c][i] += gv[c][i] * (xv[c][i] * rstd);
+          if constexpr (!RMS) db[c][i] += gv[c][i];
+        }
+      }
+      if (dx) store_vec(dx + r * d + at, o);
+    }
+  }
+  if constexpr (SUMS) {
+    // WAVES 1: the workgroup's four waves hold rows of their own, each a partial sum
+    const int64_t slot = WAVES == 1 ? int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6) : int64_t(blockIdx.x);
+    float* p = partial + slot * (RMS ? 1 : 2) * d;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int at = (l + L * c) * V;
+      if (at >= d) continue;
+#pragma unroll
+      for (int i = 0; i < V; i += 4) {
+        store_vec(p + at + i, &dw[c][i]);
+        if constexpr (!RMS) store_vec(p + d + at + i, &db[c][i]);
+      }
+    }
+  }
+}
+
+// dw[c] (and db[c]) = sum over the partial sums: 16 columns of a workgroup, 16
+// threads to a column's partial sums.
+__global__ __launch_bounds__(1024) void norm_grad_sums_kernel(const float* __restrict__ partial, int slots, int d, int two,
+                                                              float* __restrict__ dw, float* __restrict__ db) {
+  __shared__ float red[16][64];
+  const int col = threadIdx.x & 63, grp = threadIdx.x >> 6;
+  const int c = blockIdx.x * 64 + col, width = d << two;
+  float v = 0.f;
+  if (c < width)
+    for (int i = grp; i < slots; i += 16) v += partial[int64_t(i) * width + c];
+  red[grp][col] = v;
+  __syncthreads();
+  if (grp != 0 || c >= width) return;
+  v = 0.f;
+  for (int i = 0; i < 16; ++i) v += red[i][col];
+  float* out = c < d ? dw : db;
+  if (out) out[c < d ? c : c - d] = v;
+}
+
+namespace {
+// (vectors a lane, waves a row) by the row's 16-byte vectors
+template <typename F>
+bool norm_shape(int nv, bool many, F f) {
+  auto go = [&](auto Cc, auto Wc) { f(Cc, Wc); return true; };
+#define DSF_SHAPE(c, w) go(std::integral_constant<int, c>(), std::integral_constant<int, w>())
+  if (many && nv <= 64) return DSF_SHAPE(1, 1);
+  if (many && nv <= 128) return DSF_SHAPE(2, 1);
+  if (nv <= 256) return DSF_SHAPE(1, 4);
+  if (nv <= 512) return DSF_SHAPE(2, 4);
+  if (nv <= 1024) return DSF_SHAPE(4, 4);
+  if (nv <= 2048) return DSF_SHAPE(8, 4);
+  if (nv <= 4096) return DSF_SHAPE(16, 4);
+#undef DSF_SHAPE
+  return false;
+}
+}  // namespace
+
+int norm_rows_max_d() { return 16384; }
+
+hipError_t launch_norm_rows(int dtype, bool rms, const void* x, const void* w, const void* b, int64_t n, int d, float eps,
+                            void* out, hipStream_t s) {
+  auto run = [&](auto Tz) {
+    using T = decltype(Tz);
+    norm_shape(d / Elem<T>::kVec, n >= 1024, [&](auto Cc, auto Wc) {
+      constexpr int C = decltype(Cc)::value, W = decltype(Wc)::value;
+      const dim3 grid(uint32_t(W == 1 ? (n + 3) / 4 : n));
+      if (rms) norm_rows_kernel<T, C, W, true><<<grid, 256, 0, s>>>((const T*)x, (const T*)w, (const T*)b, n, d, eps, (T*)out);
+      else norm_rows_kernel<T, C, W, false><<<grid, 256, 0, s>>>((const T*)x, (const T*)w, (const T*)b, n, d, eps, (T*)out);
+    });
+  };
+  if (dtype == DSF_F32) run(float());
+  else run(uint16_t());
+  return hipGetLastError();
+}
+
+// partial sums: up to four a workgroup
+size_t norm_backward_workspace_bytes(int64_t n, int d) {
+  return size_t(std::min<int64_t>((n + 3) / 4, kBwdWgs)) * 4 * 2 * d * sizeof(float);
+}
+
+hipError_t launch_norm_backward(const NormBackwardArgs& a, hipStream_t s) {
+  auto run = [&](auto Tz) {
+    using T = decltype(Tz);
+    norm_shape(a.d / Elem<T>::kVec, a.n >= 1024, [&](auto Cc, auto Wc) {
+      constexpr int C = decltype(Cc)::value, W = decltype(Wc)::value;
+      const int wgs = int(std::min<int64_t>(W == 1 ? (a.n + 3) / 4 : a.n, kBwdWgs));
+      const bool sums = a.dw || a.db;
+      auto go = [&](auto R, auto S) {
+        norm_grad_kernel<T, C, W, decltype(R)::value, decltype(S)::value><<<wgs, 256, 0, s>>>(
+            (const T*)a.x, (const T*)a.dy, (const T*)a.w, (const T*)a.add, a.n, a.d, a.eps, (T*)a.dx, (float*)a.workspace);
+      };
+      using Y = std::true_type;
+      using N = std::false_type;
+      if (a.rms && sums) go(Y(), Y());
+      else if (a.rms) go(Y(), N());
+      else if (sums) go(N(), Y());
+      else go(N(), N());
+      if (!sums) return;
+      const int slots = W == 1 ? wgs * 4 : wgs, width = a.d * (a.rms ? 1 : 2);
+      norm_grad_sums_kernel<<<(width + 63) / 64, 1024, 0, s>>>((const float*)a.workspace, slots, a.d, a.rms ? 0 : 1, a.dw,
+                                                              a.db);
+    });
+  };
+  if (a.dtype == DSF_F32) run(float());
+  else run(uint16_t());
+  return hipGetLastError();
+}
+
+}  // namespace dsf
