@@ -707,7 +707,7 @@ int dsf_norm_backward(const void* x, const void* dy, const void* w, const void* 
 /* Workspace bytes of the head's losses: top = 0 for dsf_head_cross_entropy, the
  * entries of a row for dsf_head_distill; gradients != 0 if dh or dw are wanted
  * (also enough for calls without). It holds 16 bits (fp32: 32) for each logit of
- * as many rows as fit 2 GiB, and for calls of more rows than that the sum of dw
+ * as many rows as fit 4 GiB, and for calls of more rows than that the sum of dw
  * in fp32; never the logits of a call at once. 0 on a bad argument. */
 size_t dsf_head_workspace_size(int dtype, int64_t n_rows, int d, int n_classes, int top, int gradients);
 

@@ -7,11 +7,12 @@
 
 namespace dsf {
 
-// A logit is held as (its tile's row maximum - z) in steps of 2^(-1/1024):
-// 16 bits reach 2^-64 of the maximum (what lies below counts as 0), and half a
-// step changes a probability by 3.4e-4 relative, a tenth of the rounding to
-// bf16 that the product with it needs anyway.
-constexpr float kHeadSteps = 1024.f;
+// A logit is held as its distance below its tile's row maximum, in 65535 steps of
+// kHeadReach factors of two (1024 steps to a factor; what lies lower counts as 0).
+// Half a step changes a probability by 3.4e-4 relative, a tenth of the rounding
+// to bf16 that the product with it needs anyway.
+constexpr float kHeadReach = 64.f;
+constexpr int kHeadGrid = 256;  // workgroups of a product: one per CU
 constexpr int kHeadTile = 256;  // classes of a tile of the logits
 constexpr int kHeadMaxTop = 1024;
 
@@ -25,7 +26,7 @@ struct HeadGemmArgs {
   const void* z;        // dz [rows, ldz]
   void* zout;           // codes (fp32: logits in units of log 2) [rows, ldz]; null: statistics alone
   float2* stats;        // bf16: [classes / 256][rows_ld] (maximum, sum)
-  float* part;          // dh partial sums [splits][rows_ld][d]
+  float* part;          // partial sums: of dh [splits][rows_ld][d], of dW's last round [kHeadGrid][256][256]
   const float* prev;    // dW so far, fp32 (nullable)
   float* out32;         // dW in fp32 (nullable)
   uint16_t* out16;      // dW in bf16 (nullable)
@@ -34,7 +35,8 @@ struct HeadGemmArgs {
   float z_scale;        // log2(e) / temperature
   int row0, rows, rows_ld;  // the piece: its first active row, its rows at most, leading dimension of the above
   int V, d, ldz;
-  int splits;           // of the reduction over classes (dh)
+  const int32_t* splits;  // dh: shares of the classes (device), at most `most`
+  int most;
 };
 hipError_t launch_head_gemm(int mode, const HeadGemmArgs& g, hipStream_t s);      // kernels_headgemm.hip
 hipError_t launch_head_gemm_f32(int mode, const HeadGemmArgs& g, hipStream_t s);  // kernels_headf32.hip

@@ -23,7 +23,7 @@ namespace dsf {
 
 namespace {
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
-constexpr int kLseRows = 64;  // rows of a workgroup of the lse kernel
+constexpr int kLseRows = 16;  // rows of a workgroup of the lse kernel
 
 __device__ __forceinline__ double block_sum(double v, double* lds, int tid, int nt) {
   v = wave_sum(v);
@@ -78,56 +78,102 @@ __global__ __launch_bounds__(256) void head_teacher_kernel(const int32_t* __rest
   }
 }
 
+// Shares of the classes for dh: each round of the grid costs its k-tiles and about
+// eight more, each share a partial sum written and read again (at some 3 MB a k-tile).
+__device__ __forceinline__ int head_dh_splits(int rows, int d, int ldz, bool f32, int most) {
+  const int t = f32 ? 128 : 256, slots = f32 ? 512 : kHeadGrid;
+  const int tiles = ((rows + t - 1) / t) * ((d + t - 1) / t);
+  const float nk = float(ldz) / 64.f, join = float(rows) * float(d) * 8.f / (f32 ? 4e6f : 3e6f);
+  int got = 1;
+  float best = 0.f;
+  for (int s = 1; s <= most; ++s) {
+    const float cost = float((tiles * s + slots - 1) / slots) * (nk / float(s) + 8.f) + float(s) * join;
+    if (s == 1 || cost < best) {
+      best = cost;
+      got = s;
+    }
+  }
+  return got;
+}
+
+struct HeadRowsArgs {
+  const int32_t* targets; const int32_t* live; const float* weight;
+  int n, V;
+  float factor;
+  int mean;
+  int32_t* act; int32_t* slot; int32_t* n_active;
+  double* wsum; float* scale; uint32_t* count;
+  float* row_loss;
+  int32_t* splits;  // of each piece (null: not wanted)
+  int pieces, rows, d, ldz, most, f32;
+};
 // The rows that take part, in order: act[slot] = row, slot[row] = slot or -1;
 // n_active; wsum = sum of their weights; scale = factor / wsum (mean; 0 for a
-// sum of 0) or factor. Rows that do not take part get a loss of 0. One workgroup.
-__global__ __launch_bounds__(1024) void head_rows_kernel(const int32_t* __restrict__ targets,
-                                                         const int32_t* __restrict__ live,
-                                                         const float* __restrict__ weight, int n, int V, float factor,
-                                                         int mean, int32_t* __restrict__ act, int32_t* __restrict__ slot,
-                                                         int32_t* __restrict__ n_active, double* __restrict__ wsum,
-                                                         float* __restrict__ scale, uint32_t* __restrict__ count,
-                                                         float* __restrict__ row_loss) {
+// sum of 0) or factor. Rows that do not take part get a loss of 0. One
+// workgroup: each wave counts its stretch of the rows, then places it.
+__global__ __launch_bounds__(1024) void head_rows_kernel(HeadRowsArgs a) {
   __shared__ int part[16];
   __shared__ double red[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int per = (n + 1023) / 1024, r0 = std::min(n, tid * per), r1 = std::min(n, r0 + per);
-  auto takes_part = [&](int r) {
-    if (!(targets ? uint32_t(targets[r]) < uint32_t(V) : live[r] != 0)) return false;
-    return !weight || !(weight[r] == 0.f);
+  const int seg = ((a.n + 15) / 16 + 63) / 64 * 64;
+  const int b = std::min(int64_t(a.n), int64_t(wave) * seg), e = std::min(int64_t(a.n), int64_t(b) + seg);
+  constexpr int U = 8;
+  // rows i .. i + 64 U: whether the lane's take part, and their weights
+  auto look = [&](int i, bool (&in)[U], float (&w)[U]) {
+    int t[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = i + 64 * u + lane;
+      t[u] = r < e ? (a.targets ? a.targets[r] : a.live[r]) : -1;
+      w[u] = a.weight && r < e ? a.weight[r] : 1.f;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      in[u] = (a.targets ? uint32_t(t[u]) < uint32_t(a.V) : t[u] > 0) && !(w[u] == 0.f);
   };
   int c = 0;
-  double w = 0.0;
-  for (int r = r0; r < r1; ++r)
-    if (takes_part(r)) {
-      ++c;
-      w += weight ? double(weight[r]) : 1.0;
-    }
-  int incl = c;
+  double sum = 0.0;
+  for (int i = b; i < e; i += 64 * U) {
+    bool in[U];
+    float w[U];
+    look(i, in, w);
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int v = __shfl_up(incl, o, 64);
-    if (lane >= o) incl += v;
+    for (int u = 0; u < U; ++u) {
+      c += __popcll(__ballot(in[u]));
+      sum += in[u] ? double(w[u]) : 0.0;
+    }
   }
-  if (lane == 63) part[wave] = incl;
-  __syncthreads();
-  int at = incl - c, all = 0;
+  if (lane == 0) part[wave] = c;
+  sum = block_sum(sum, red, tid, 1024);  // (its barriers publish part, too)
+  int at = 0, all = 0;
   for (int i = 0; i < 16; ++i) {
     if (i < wave) at += part[i];
     all += part[i];
   }
-  for (int r = r0; r < r1; ++r) {
-    const bool in = takes_part(r);
-    slot[r] = in ? at : -1;
-    if (in) act[at++] = r;
-    else if (row_loss) row_loss[r] = 0.f;
+  for (int i = b; i < e; i += 64 * U) {
+    bool in[U];
+    float w[U];
+    look(i, in, w);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = i + 64 * u + lane;
+      const uint64_t m = __ballot(in[u]);
+      const int here = at + __popcll(m & ((uint64_t(1) << lane) - 1));
+      at += __popcll(m);
+      if (r >= e) continue;
+      a.slot[r] = in[u] ? here : -1;
+      if (in[u]) a.act[here] = r;
+      else if (a.row_loss) a.row_loss[r] = 0.f;
+    }
   }
-  w = block_sum(w, red, tid, 1024);
+  if (a.splits)
+    for (int p = tid; p < a.pieces; p += 1024)
+      a.splits[p] = head_dh_splits(std::max(0, std::min(all - p * a.rows, a.rows)), a.d, a.ldz, a.f32 != 0, a.most);
   if (tid == 0) {
-    *n_active = all;
-    *wsum = w;
-    *scale = mean ? (w == 0.0 ? 0.f : float(double(factor) / w)) : factor;
-    *count = 0u;
+    *a.n_active = all;
+    *a.wsum = sum;
+    *a.scale = a.mean ? (sum == 0.0 ? 0.f : float(double(a.factor) / sum)) : a.factor;
+    *a.count = 0u;
   }
 }
 
@@ -215,7 +261,7 @@ __global__ __launch_bounds__(256) void head_stats_f32_kernel(const float* __rest
 
 // lse[s] from the tiles' statistics, the row's loss, and the sum of weight x
 // loss: a partial sum of each workgroup, added in order by the last of the
-// call's to finish. 64 rows by 16 groups of tiles (and of target classes).
+// call's to finish. 16 rows by 64 groups of tiles; then a wave to a row's list.
 struct HeadLseArgs {
   const float2* stats; int tiles, rows_ld;
   const float* z2; const float* q; const float* plogp;  // q null: one class, q = 1
@@ -227,53 +273,63 @@ struct HeadLseArgs {
   float T;
 };
 __global__ __launch_bounds__(1024) void head_lse_kernel(HeadLseArgs a) {
-  __shared__ float2 st[16][kLseRows];
-  __shared__ float ls[16][kLseRows];
+  __shared__ float2 st[64][kLseRows];
   __shared__ double red[16];
   __shared__ int last;
-  const int tid = threadIdx.x, rl = tid & 63, grp = tid >> 6;
-  const int rows = std::min(*a.n_active - a.row0, a.rows), s = blockIdx.x * kLseRows + rl;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int rows = std::min(*a.n_active - a.row0, a.rows), s0 = blockIdx.x * kLseRows;
+  {
+    const int rl = tid & 15, grp = tid >> 4, s = s0 + rl;
+    float M = -INFINITY, S = 0.f;
+    if (s < rows)
+      for (int t = grp; t < a.tiles; t += 4 * 64) {
+        float2 v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          v[u] = t + 64 * u < a.tiles ? a.stats[int64_t(t + 64 * u) * a.rows_ld + s] : float2{-INFINITY, 0.f};
+        const float m = fmaxf(fmaxf(fmaxf(M, v[0].x), fmaxf(v[1].x, v[2].x)), v[3].x), ref = m == -INFINITY ? 0.f : m;
+        S *= exp2f(M - ref);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) S += v[u].y * exp2f(v[u].x - ref);
+        M = m;
+      }
+    st[grp][rl] = float2{M, S};
+  }
+  __syncthreads();
+  // wave w: row w of the workgroup
+  const int s = s0 + wave, g = a.row0 + s;  // slot in the piece, in the call
   const bool in = s < rows;
-  const int g = a.row0 + s;  // slot in the call
-  float M = -INFINITY, S = 0.f;
-  if (in)
-    for (int t = grp; t < a.tiles; t += 16) {
-      const float2 v = a.stats[int64_t(t) * a.rows_ld + s];
-      const float m = fmaxf(M, v.x), ref = m == -INFINITY ? 0.f : m;
-      S = S * exp2f(M - ref) + v.y * exp2f(v.x - ref);
-      M = m;
-    }
-  st[grp][rl] = float2{M, S};
-  __syncthreads();
-  M = st[0][rl].x;
-  for (int i = 1; i < 16; ++i) M = fmaxf(M, st[i][rl].x);
+  const float2 mine = st[lane][wave];
+  float M = mine.x;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
   const float ref = M == -INFINITY ? 0.f : M;
-  S = 0.f;
-  for (int i = 0; i < 16; ++i) S += st[i][rl].y * exp2f(st[i][rl].x - ref);
-  const float lse = ref + log2f(S);
-  if (in && grp == 0) a.lse[s] = lse;
-  // sum_j q_j (lse - z_j)
+  const float lse = ref + log2f(wave_sum(mine.y * exp2f(mine.x - ref)));
   const int row = in ? a.act[g] : 0;
-  float part = 0.f;
+  // sum_j q_j (lse - z_j)
+  float x = 0.f;
   if (in)
-    for (int j = grp; j < a.k; j += 16) {
+    for (int j = lane; j < a.k; j += 64) {
       const float q = a.q ? a.q[int64_t(row) * a.k + j] : 1.f;
-      if (!(q == 0.f)) part += q * (lse - a.z2[int64_t(g) * a.k + j]);
+      if (!(q == 0.f)) x += q * (lse - a.z2[int64_t(g) * a.k + j]);
     }
-  ls[grp][rl] = part;
-  __syncthreads();
-  double wl = 0.0;
-  if (grp == 0 && in) {
-    float x = 0.f;
-    for (int i = 0; i < 16; ++i) x += ls[i][rl];
-    const float loss = a.T * a.T * ((a.q ? a.plogp[row] : 0.f) + kLn2 * x);
-    if (a.row_loss) a.row_loss[row] = loss;
-    wl = (a.weight ? double(a.weight[row]) : 1.0) * double(loss);
+  x = wave_sum(x);
+  if (lane == 0) {
+    double wl = 0.0;
+    if (in) {
+      a.lse[s] = lse;
+      const float loss = a.T * a.T * ((a.q ? a.plogp[row] : 0.f) + kLn2 * x);
+      if (a.row_loss) a.row_loss[row] = loss;
+      wl = (a.weight ? double(a.weight[row]) : 1.0) * double(loss);
+    }
+    red[wave] = wl;
   }
   if (!a.total) return;
-  wl = block_sum(wl, red, tid, 1024);
+  __syncthreads();
   if (tid == 0) {
-    __hip_atomic_store(a.partial + a.first + blockIdx.x, wl, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    double t = 0.0;
+    for (int i = 0; i < 16; ++i) t += red[i];
+    __hip_atomic_store(a.partial + a.first + blockIdx.x, t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     last = __hip_atomic_fetch_add(a.count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == uint32_t(a.workgroups - 1);
   }
@@ -321,7 +377,7 @@ __global__ __launch_bounds__(256) void head_probs_kernel(HeadProbsArgs a) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const uint32_t code = e ? raw[i] >> 16 : raw[i] & 0xffffu;
-          const float x = __builtin_amdgcn_exp2f(fmaf(float(code), -1.f / kHeadSteps, top));
+          const float x = __builtin_amdgcn_exp2f(fmaf(float(code), -kHeadReach / 65535.f, top));
           p[2 * i + e] = code == 0xffffu ? 0.f : wt * x;
         }
     } else {
@@ -352,11 +408,11 @@ __global__ __launch_bounds__(256) void head_probs_kernel(HeadProbsArgs a) {
 // dh of every row: scale times the sum of its partial sums, zeros for rows that
 // do not take part (written with the first piece).
 template <typename T>
-__global__ __launch_bounds__(256) void head_dh_kernel(const float* __restrict__ part, int splits, int rows_ld, int d,
+__global__ __launch_bounds__(256) void head_dh_kernel(const float* __restrict__ part, const int32_t* __restrict__ n_splits, int rows_ld, int d,
                                                       const int32_t* __restrict__ slot, int n, int row0, int rows,
                                                       const float* __restrict__ scale, T* __restrict__ dh) {
   constexpr int VEC = Elem<T>::kVec;
-  const int nv = d / VEC;
+  const int nv = d / VEC, splits = *n_splits;
   for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < int64_t(n) * nv; i += int64_t(gridDim.x) * 256) {
     const int r = int(i / nv), c = int(i - int64_t(r) * nv) * VEC;
     const int s = slot[r] - row0;
@@ -389,15 +445,15 @@ __global__ __launch_bounds__(256) void head_dh_kernel(const float* __restrict__ 
 
 namespace {
 struct HeadPlan {
-  int ldz, rows, pieces, tiles, splits, cuts, cols;
-  size_t act, slot, live, scalars, q, plogp, z2, hc, lse, stats, partial, z, part, acc, total;
+  int ldz, rows, pieces, tiles, most, cuts, cols;
+  size_t splits, act, slot, live, scalars, q, plogp, z2, hc, lse, stats, partial, z, part, acc, total;
 };
 
 size_t up(size_t v) { return (v + 255) & ~size_t(255); }
 
 // Bytes of a piece's logits (codes), at most: rows for which a tile of products
 // still costs far more than a tile's pass over dW, which a further piece repeats.
-constexpr size_t kPieceBytes = size_t(2) << 30;
+constexpr size_t kPieceBytes = size_t(4) << 30;
 constexpr size_t kDhPartBytes = size_t(1) << 29;
 
 HeadPlan head_plan(int dtype, int n, int d, int V, int k, bool grads) {
@@ -412,17 +468,9 @@ HeadPlan head_plan(int dtype, int n, int d, int V, int k, bool grads) {
   const int64_t most = std::max<int64_t>(256, int64_t(kPieceBytes / per_row) / 256 * 256);
   p.pieces = int((n256 + most - 1) / most);
   p.rows = int(((n256 + p.pieces - 1) / p.pieces + 255) / 256 * 256);
-  // dh: cut the classes so that the workgroups fill their last round: a round
-  // costs nk / s k-tiles and about eight more; s partial sums are written and read
-  const int t = f32 ? 128 : 256, slots = f32 ? 512 : 256;
-  const double tiles = double((p.rows + t - 1) / t) * ((d + t - 1) / t);
-  const double nk = p.ldz / 64.0, join = double(p.rows) * d * 8 / (f32 ? 4e6 : 3e6);  // in k-tiles (0.6 us)
-  double best = 0;
-  for (int s = 1; s <= 128; ++s) {
-    if (s > 1 && (size_t(s) * p.rows * d * 4 > kDhPartBytes || nk / s < 4)) break;
-    const double cost = double(int64_t((tiles * s + slots - 1) / slots)) * (nk / s + 8) + s * join;
-    if (s == 1 || cost < best) best = cost, p.splits = s;
-  }
+  // shares of the classes for dh, at most
+  const int64_t fit = int64_t(kDhPartBytes / (size_t(p.rows) * d * 4));
+  p.most = int(std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(128, p.ldz / 256), fit)));
   // ranges of a row for dz: about four workgroups per CU
   p.cuts = std::max(1, std::min(p.ldz / 2048, (1024 + p.rows - 1) / p.rows));
   p.cols = ((p.ldz + p.cuts - 1) / p.cuts + 2047) / 2048 * 2048;
@@ -434,6 +482,7 @@ HeadPlan head_plan(int dtype, int n, int d, int V, int k, bool grads) {
     return here;
   };
   p.scalars = take(256);
+  p.splits = take(size_t(p.pieces) * 4);
   p.act = take(size_t(n) * 4);
   p.slot = take(size_t(n) * 4);
   p.live = take(size_t(n) * 4);
@@ -446,7 +495,7 @@ HeadPlan head_plan(int dtype, int n, int d, int V, int k, bool grads) {
   p.hc = take(size_t(n) * d * eb);
   if (grads || f32) p.z = take(size_t(p.rows) * p.ldz * eb);
   if (grads) {
-    p.part = take(size_t(p.splits) * p.rows * d * 4);
+    p.part = take(std::max(size_t(p.most) * p.rows * d * 4, size_t(kHeadGrid) * kHeadTile * kHeadTile * 4));
     if (!f32 && p.pieces > 1) p.acc = take(size_t(V) * d * 4);
   }
   p.total = at;
@@ -481,9 +530,11 @@ hipError_t launch_head_loss(const HeadLossArgs& a, hipStream_t s) {
                                                       (int32_t*)(ws + p.live));
     DSF_TRY(hipGetLastError());
   }
-  head_rows_kernel<<<1, 1024, 0, s>>>(distill ? nullptr : a.classes, (const int32_t*)(ws + p.live), a.weight, a.n, a.V,
-                                      a.grad_scale * a.temperature, a.mean, act, slot, n_active, wsum, scale, count,
-                                      a.row_loss);
+  int32_t* splits = (int32_t*)(ws + p.splits);
+  const HeadRowsArgs r{distill ? nullptr : a.classes, (const int32_t*)(ws + p.live), a.weight, a.n, a.V,
+                       a.grad_scale * a.temperature, a.mean, act, slot, n_active, wsum, scale, count, a.row_loss,
+                       a.dh ? splits : nullptr, p.pieces, p.rows, a.d, p.ldz, p.most, f32};
+  head_rows_kernel<<<1, 1024, 0, s>>>(r);
   DSF_TRY(hipGetLastError());
   const int64_t tasks = int64_t(a.n) * ((k + kDots - 1) / kDots);
   const dim3 gg(uint32_t((tasks + 3) / 4));
@@ -513,7 +564,8 @@ hipError_t launch_head_loss(const HeadLossArgs& a, hipStream_t s) {
     g.scale = scale;
     g.n_active = n_active;
     g.z_scale = z_scale;
-    g.splits = 1;
+    g.splits = splits + i;
+    g.most = p.most;
     auto product = [&](int mode) { return f32 ? launch_head_gemm_f32(mode, g, s) : launch_head_gemm(mode, g, s); };
     DSF_TRY(product(kHeadLogits));
     if (f32) {
@@ -569,16 +621,14 @@ hipError_t launch_head_loss(const HeadLossArgs& a, hipStream_t s) {
     else head_probs_kernel<uint16_t><<<g.rows * p.cuts, 256, 0, s>>>(b);
     DSF_TRY(hipGetLastError());
     if (a.dh) {
-      g.splits = p.splits;
       DSF_TRY(product(kHeadDh));
-      g.splits = 1;
       const int64_t nv = int64_t(a.n) * a.d / (f32 ? 4 : 8);
       const dim3 grid(uint32_t(std::min<int64_t>((nv + 255) / 256, 8192)));
       if (f32)
-        head_dh_kernel<float><<<grid, 256, 0, s>>>(g.part, p.splits, p.rows, a.d, slot, a.n, g.row0, g.rows, scale,
+        head_dh_kernel<float><<<grid, 256, 0, s>>>(g.part, g.splits, p.rows, a.d, slot, a.n, g.row0, g.rows, scale,
                                                    (float*)a.dh);
       else
-        head_dh_kernel<uint16_t><<<grid, 256, 0, s>>>(g.part, p.splits, p.rows, a.d, slot, a.n, g.row0, g.rows, scale,
+        head_dh_kernel<uint16_t><<<grid, 256, 0, s>>>(g.part, g.splits, p.rows, a.d, slot, a.n, g.row0, g.rows, scale,
                                                       (uint16_t*)a.dh);
       DSF_TRY(hipGetLastError());
     }

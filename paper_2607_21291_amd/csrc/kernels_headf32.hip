@@ -56,8 +56,9 @@ __global__ __launch_bounds__(256, 2) void head_f32_kernel(HeadGemmArgs g) {
   const int tr = (rows + kT - 1) / kT, tv = (MODE == kHeadLogits ? g.ldz : g.V + kT - 1) / kT, td = (g.d + kT - 1) / kT;
   const int outer = MODE == kHeadDw ? tv : tr, inner = MODE == kHeadLogits ? tv : td;
   const int nt = outer * inner;
-  if (int(blockIdx.x) >= nt * g.splits) return;
-  const int w = xcd_remap(int(blockIdx.x), nt * g.splits);
+  const int splits = MODE == kHeadDh ? *g.splits : 1;
+  if (int(blockIdx.x) >= nt * splits) return;  // (the grid is for all rows and the most shares)
+  const int w = xcd_remap(int(blockIdx.x), nt * splits);
   const int sp = w / nt, tn = (w - sp * nt) / inner, tm = (w - sp * nt) - tn * inner;
 
   const int K = MODE == kHeadLogits ? g.d : MODE == kHeadDh ? g.ldz : rows;
@@ -66,7 +67,7 @@ __global__ __launch_bounds__(256, 2) void head_f32_kernel(HeadGemmArgs g) {
   F32Op<BCOL> B{(const float*)(MODE == kHeadLogits ? g.h : g.z), MODE == kHeadLogits ? g.d : g.ldz,
                 MODE == kHeadDw ? g.ldz : rows, K};
   const int nk = (K + kBK - 1) / kBK;
-  const int kb = int(int64_t(nk) * sp / g.splits), ke = int(int64_t(nk) * (sp + 1) / g.splits);
+  const int kb = int(int64_t(nk) * sp / splits), ke = int(int64_t(nk) * (sp + 1) / splits);
   const int64_t xm = int64_t(tm) * kT, xn = int64_t(tn) * kT;
 
   f32x16 acc[2][2];
@@ -140,7 +141,7 @@ __global__ __launch_bounds__(256, 2) void head_f32_kernel(HeadGemmArgs g) {
 hipError_t launch_head_gemm_f32(int mode, const HeadGemmArgs& g, hipStream_t s) {
   const int tr = (g.rows + kT - 1) / kT, tv = (g.V + kT - 1) / kT, td = (g.d + kT - 1) / kT;
   if (mode == kHeadLogits) head_f32_kernel<kHeadLogits><<<tr * (g.ldz / kT), 256, 0, s>>>(g);
-  else if (mode == kHeadDh) head_f32_kernel<kHeadDh><<<tr * td * g.splits, 256, 0, s>>>(g);
+  else if (mode == kHeadDh) head_f32_kernel<kHeadDh><<<tr * td * g.most, 256, 0, s>>>(g);
   else head_f32_kernel<kHeadDw><<<tv * td, 256, 0, s>>>(g);
   return hipGetLastError();
 }

@@ -13,6 +13,11 @@
 // LDS transpose load), so nothing is transposed in memory. A's index m is the
 // one that is contiguous in the output: an MFMA leaves four consecutive m in a
 // lane, eight after a swap between 16-lane rows.
+//
+// A workgroup per CU walks its tiles with one stream of k-tiles: the loads run
+// two k-tiles ahead, into the next tile while this one ends, so that only its
+// epilogue is between two tiles' products.
+#include <algorithm>
 #include <type_traits>
 
 #include "dsf_device.h"
@@ -28,6 +33,7 @@ constexpr int kStage = 2 * kOpBytes;     // the other stage's addresses differ i
 constexpr int kSubBytes = kBK * 128 * 2; // 128 columns of an operand stored by rows of k
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+#define DSF_INLINE __attribute__((always_inline))  // for lambdas over register arrays
 #define DSF_LDS __attribute__((address_space(3)))
 typedef DSF_LDS char LdsChar;
 
@@ -37,62 +43,62 @@ typedef DSF_LDS char LdsChar;
 // them; the callers wait and meet at a barrier. The assembly brings the wait
 // states that a scalar operand just written by a vector instruction needs. (M0
 // is reserved: the compiler keeps nothing in it.)
-__device__ __forceinline__ void head_dma2(__amdgpu_buffer_rsrc_t ra, uint32_t va, uint32_t at0,
-                                          __amdgpu_buffer_rsrc_t rb, uint32_t vb, uint32_t at1) {
+__device__ __forceinline__ void head_dma2(u32x4 ra, uint32_t va, uint32_t at0, u32x4 rb, uint32_t vb, uint32_t at1) {
   asm volatile(
       "s_mov_b32 m0, %0\n\t"
       "s_nop 4\n\t"
       "buffer_load_dwordx4 %1, %2, 0 offen lds\n\t"
       "s_mov_b32 m0, %3\n\t"
-      "s_nop 4\n\t"
+      "s_nop 0\n\t"
       "buffer_load_dwordx4 %4, %5, 0 offen lds" ::"s"(at0),
       "v"(va), "s"(ra), "s"(at1), "v"(vb), "s"(rb)
       : "memory");
 }
 
-// An operand in global memory and its share of a stage. The lane's part of an
-// offset is the same for every load; load u of a wave is load l = 8 u + wave of
-// the operand's 32 (1 KiB each).
+// An operand in global memory and its share of a stage: 32 loads of 1 KiB, load
+// l = 8 u + wave the wave's u-th. The lane's part of an offset is the same for
+// every load.
 // COL false: element (x, k) at p[x ld + k]; load l fills tile rows 8 l .. + 7, 128 bytes
 //   each, 16-byte chunk c of row r at c ^ (r & 7).
 // COL true: element (x, k) at p[k ld + x]; subtile l / 16 (128 columns) rows 4 (l % 16) .. + 3
 //   of k, 256 bytes each, chunk c of row r at c ^ key(r), key(r) = 2 ((r & 3) + 4 (r >> 3 & 1)): the
 //   sixteen rows of a transpose load, 32 bytes each, then cover the 64 banks twice, the minimum.
+// What lies past the operand's last row reads as zeros (the resource ends there).
 template <bool COL>
 struct HeadOp {
-  const uint16_t* base;  // at the tile's first x
-  int64_t bytes;         // from there to the end of the operand
-  int ld, kmax;
-  uint32_t voff;
-  int chunk_k;           // COL false: first k of the lane's chunk within a tile
-  __device__ __forceinline__ HeadOp(const uint16_t* p, int ld_, int64_t nx, int64_t nk, int64_t x0, int wave, int lane)
-      : ld(ld_), kmax(int(nk)) {
+  const char* base = nullptr;  // of the next k-tile to load
+  uint32_t ld2 = 0;            // bytes of a row
+  int rows = 0;                // COL: rows of k left; else rows of the tile
+  uint32_t voff = 0;
+  __device__ __forceinline__ void set(const void* p, int ld, int64_t nx, int64_t nk, int64_t x0, int kt, int wave,
+                                      int lane) {
+    ld2 = uint32_t(ld) * 2u;
     if constexpr (COL) {
-      base = p + x0;
-      bytes = (nk * ld - x0) * 2;
+      base = (const char*)p + int64_t(kt) * kBK * ld2;
+      rows = int(nk - int64_t(kt) * kBK);
       const int key = ((lane >> 4) + 4 * ((wave >> 1) & 1)) << 1;
-      voff = uint32_t(lane >> 4) * uint32_t(ld) * 2u + uint32_t(((lane & 15) ^ key) * 16);
-      chunk_k = 0;
+      voff = uint32_t(4 * wave + (lane >> 4)) * ld2 + uint32_t(x0) * 2u + uint32_t(((lane & 15) ^ key) * 16);
     } else {
-      base = p + x0 * ld;
-      bytes = (nx - x0) * ld * 2;
-      const int c = (lane & 7) ^ (lane >> 3);
-      voff = uint32_t(lane >> 3) * uint32_t(ld) * 2u + uint32_t(c * 16);
-      chunk_k = 8 * c;
+      base = (const char*)p + x0 * ld2 + int64_t(kt) * (kBK * 2);
+      rows = int(nx - x0 < kT ? nx - x0 : kT);
+      voff = uint32_t(8 * wave + (lane >> 3)) * ld2 + uint32_t(((lane & 7) ^ (lane >> 3)) * 16);
     }
   }
-  // resource and offset of load l of k-tile kt. The resource ends with the
-  // operand: what lies past it reads as zeros.
-  __device__ __forceinline__ __amdgpu_buffer_rsrc_t source(int kt, int l, uint32_t& v) const {
-    const int64_t at = COL ? int64_t(kt) * kBK * ld : int64_t(kt) * kBK, left = bytes - at * 2;
-    if constexpr (COL) {
-      v = voff + uint32_t(4 * (l & 15)) * uint32_t(ld) * 2u + uint32_t(l >> 4) * 256u;
-    } else {
-      // chunks past the end of a row (a reduction that is no multiple of 64), too
-      v = kt * kBK + chunk_k < kmax ? voff + uint32_t(8 * l) * uint32_t(ld) * 2u : 0x80000000u;
-    }
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(base + at), (short)0,
-                                             int(left < 0 ? 0 : left > 0x7fffffff ? 0x7fffffff : left), 0x00020000);
+  // resource of the next k-tile (none: zeros), which is then the one after. Rows
+  // are counted from the k-tile's first byte: an offset past them is one past the
+  // operand (COL false: or in its last row, past the k-tiles of this call).
+  __device__ __forceinline__ u32x4 next(bool any) {
+    const uint64_t b = reinterpret_cast<uint64_t>(base);
+    const int n = COL && rows > kBK ? kBK : rows;
+    auto uniform = [](uint32_t x) { return uint32_t(__builtin_amdgcn_readfirstlane(int(x))); };
+    const u32x4 r = {uniform(uint32_t(b)), uniform(uint32_t(b >> 32) & 0xffffu),
+                     uniform(any && n > 0 ? uint32_t(n) * ld2 : 0u), 0x00020000u};
+    base += COL ? int64_t(kBK) * ld2 : kBK * 2;
+    if (COL) rows -= kBK;
+    return r;
+  }
+  __device__ __forceinline__ uint32_t offset(int u) const {
+    return voff + (COL ? uint32_t(32 * (u & 1)) * ld2 + uint32_t(u >> 1) * 256u : uint32_t(64 * u) * ld2);
   }
 };
 
@@ -128,6 +134,28 @@ struct HeadFrag {
   }
 };
 
+// A barrier that leaves loads into LDS and stores in flight.
+__device__ __forceinline__ void ring_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Two values of [0, 1] as 16-bit fractions of 65535, clamped.
+__device__ __forceinline__ uint32_t pack_unit(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pknorm_u16(a, b));
+}
+
+// Rows of a piece that take part.
+__device__ __forceinline__ int head_piece_rows(const HeadGemmArgs& g) {
+  const int rows = *g.n_active - g.row0;
+  return rows < 0 ? 0 : rows > g.rows ? g.rows : rows;
+}
+
+// Shares of a tile of dW in the last round, of `left` tiles: as many as fill the grid, each at least
+// eight k-tiles long.
+__device__ __forceinline__ int head_dw_cut(int left, int nk, int grid) {
+  if (left == 0) return 1;
+  const int most = nk / 8, fit = grid / left;
+  return most < 1 ? 1 : most < fit ? most : fit;
+}
+
 __device__ __forceinline__ u32x4 swap_rows8(uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1) {
   // a: four 16-bit values of block i, b: of block i + 1. After the swap of odd with even
   // 16-lane rows a lane holds eight consecutive values: columns 16 (i + (grp & 1)) + 8 (grp >> 1).
@@ -144,49 +172,97 @@ __global__ __launch_bounds__(kThreads) void head_gemm_kernel(HeadGemmArgs g) {
   constexpr bool ACOL = MODE != kHeadLogits, BCOL = MODE == kHeadDw;
   constexpr int MI = 4, NI = 8;
   __shared__ __attribute__((aligned(65536))) char smem[2 * kStage];
+  __shared__ float red[MODE == kHeadLogits ? 8 * kT : 1];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 1, wn = wave & 1, r16 = lane & 15, grp = lane >> 4;
-  // rows of this piece that take part
-  int rows = *g.n_active - g.row0;
-  rows = rows < 0 ? 0 : rows > g.rows ? g.rows : rows;
+  const int rows = head_piece_rows(g);
+  const int K = MODE == kHeadLogits ? g.d : MODE == kHeadDh ? g.ldz : rows;
+  const int nk = (K + kBK - 1) / kBK;
 
-  // the tiles of the rows that take part; a grid for more has workgroups that end here
+  // This workgroup's items (a tile, or a share of a tile's k-tiles): as many whole rounds
+  // of the grid as there are, each XCD a contiguous range of the tile order in which its
+  // workgroups take one item after another; then one of what is left, if it gets one.
   const int tr = (rows + kT - 1) / kT, tv = (g.V + kT - 1) / kT, td = (g.d + kT - 1) / kT;
   const int outer = MODE == kHeadDw ? tv : tr, inner = MODE == kHeadLogits ? tv : td;
-  const int nt = outer * inner;
-  if (int(blockIdx.x) >= nt * g.splits) return;
-  const int w = xcd_remap(int(blockIdx.x), nt * g.splits);
-  const int sp = w / nt;
-  const GemmTile t = gemm_tile(w - sp * nt, outer, inner, MODE == kHeadLogits ? 4 : 0);
-  const int tm = t.tn, tn = t.tm;  // out[n][m]: rows of tiles are n
+  const int nt = outer * inner, per = int(gridDim.x) / kXcds;
+  const int splits = MODE == kHeadDh ? *g.splits : 1;
+  const int xcd = int(blockIdx.x) % kXcds, place = int(blockIdx.x) / kXcds;
+  const int rounds = nt * splits / int(gridDim.x), full = rounds * int(gridDim.x);
+  const int cut = MODE == kHeadDw ? head_dw_cut(nt - full, nk, int(gridDim.x)) : 1;
+  const int left = (nt * splits - full) * cut, lq = left / kXcds, lr = left % kXcds;
+  const int items = rounds + (place < lq + (xcd < lr) ? 1 : 0);
+  if (items == 0) return;
+  struct Item {
+    int tm, tn, kb, ke, split;  // split < 0: a whole tile; else its partial sum's slot
+  };
+  auto item_of = [&](int i) {
+    Item it;
+    int tile, share, shares;
+    if (i < rounds) {
+      const int w = xcd * (full / kXcds) + i * per + place;
+      share = w / nt;
+      tile = w - share * nt;
+      shares = splits;
+      it.split = MODE == kHeadDh ? share : -1;
+    } else {
+      const int w = xcd * lq + (xcd < lr ? xcd : lr) + place;
+      if (MODE == kHeadDw) {
+        tile = full + w / cut;
+        share = w % cut;
+        shares = cut;
+        it.split = cut > 1 ? w : -1;
+      } else {
+        share = (full + w) / nt;
+        tile = full + w - share * nt;
+        shares = splits;
+        it.split = MODE == kHeadDh ? share : -1;
+      }
+    }
+    const GemmTile t = gemm_tile(tile, outer, inner, 4);
+    it.tm = t.tn;
+    it.tn = t.tm;  // out[n][m]: rows of the tile order are n
+    it.kb = int(int64_t(nk) * share / shares);
+    it.ke = int(int64_t(nk) * (share + 1) / shares);
+    return it;
+  };
 
-  const int64_t nm = MODE == kHeadLogits ? g.V : g.d;
-  const int64_t nn = MODE == kHeadDw ? g.ldz : rows;
-  const int K = MODE == kHeadLogits ? g.d : MODE == kHeadDh ? g.ldz : rows;
-  const HeadOp<ACOL> A((const uint16_t*)(MODE == kHeadDw ? g.h : g.w), g.d, nm, MODE == kHeadDh ? g.V : K, int64_t(tm) * kT, wave, lane);
-  const HeadOp<BCOL> B((const uint16_t*)(MODE == kHeadLogits ? g.h : g.z), MODE == kHeadLogits ? g.d : g.ldz, nn, K, int64_t(tn) * kT, wave,
-                       lane);
   const uint32_t lds = uint32_t(__builtin_amdgcn_readfirstlane(int(uint32_t(uintptr_t((DSF_LDS char*)smem)))));
   HeadFrag<ACOL> fa(lds, lane, wm * 64);
   HeadFrag<BCOL> fb(lds + kOpBytes, lane, wn * 128);
-  const int nk = (K + kBK - 1) / kBK;
-  const int kb = int(int64_t(nk) * sp / g.splits), ke = int(int64_t(nk) * (sp + 1) / g.splits);
-
   f32x4 acc[MI][NI];
-#pragma unroll
-  for (int i = 0; i < MI; ++i)
-#pragma unroll
-    for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-#define DSF_INLINE __attribute__((always_inline))
-  // the wave's loads u of A and B of k-tile kt, into the stage at st
-  auto issue = [&](int kt, uint32_t st, int u) DSF_INLINE {
-    const int l = 8 * u + wave;
-    uint32_t va, vb;
-    const auto ra = A.source(kt, l, va);
-    const auto rb = B.source(kt, l, vb);
-    head_dma2(ra, va, st + 1024 * l, rb, vb, st + kOpBytes + 1024 * l);
+  // The stream of loads: k-tile lk of item li, two k-tiles ahead of the products.
+  HeadOp<ACOL> A;
+  HeadOp<BCOL> B;
+  int li = -1, lk = 0, lke = 0;
+  u32x4 ra, rb;
+  const int chunk_k = 8 * ((lane & 7) ^ (lane >> 3));
+  // Sets the next k-tile's resources; returns what moves the chunks past the end of
+  // a row (logits of a width that is no multiple of 64) out of range.
+  auto start = [&]() DSF_INLINE {
+    if (lk == lke && li < items) {
+      if (++li < items) {
+        const Item it = item_of(li);
+        lk = it.kb;
+        lke = it.ke;
+        A.set(MODE == kHeadDw ? g.h : g.w, g.d, MODE == kHeadLogits ? g.V : g.d, MODE == kHeadDh ? g.V : K,
+              int64_t(it.tm) * kT, lk, wave, lane);
+        B.set(MODE == kHeadLogits ? g.h : g.z, MODE == kHeadLogits ? g.d : g.ldz, MODE == kHeadDw ? g.ldz : rows, K,
+              int64_t(it.tn) * kT, lk, wave, lane);
+      }
+    }
+    const bool any = li < items;
+    ra = A.next(any);
+    rb = B.next(any);
+    const uint32_t past = MODE == kHeadLogits && lk * kBK + chunk_k >= K ? 0x80000000u : 0u;
+    lk += any;
+    return past;
+  };
+  // The wave's loads u of A and B, into the stage at st.
+  auto issue = [&](uint32_t st, int u, uint32_t past) DSF_INLINE {
+    head_dma2(ra, A.offset(u) + past, st + 1024u * uint32_t(8 * u + wave), rb, B.offset(u) + past,
+              st + kOpBytes + 1024u * uint32_t(8 * u + wave));
   };
   bf16x8 af[2][MI], bq[2][NI];
   // read n of a fragment set, in the order of their use: A 0, B 0 .. NI - 1, A 1 .. MI - 1
@@ -197,177 +273,228 @@ __global__ __launch_bounds__(kThreads) void head_gemm_kernel(HeadGemmArgs g) {
   };
   constexpr int R = MI + NI;
   // One substep: the products of fragment set S, and between them the reads of
-  // the other set (substep ks) and the loads of tile kn into the stage at dma.
-  auto substep = [&](auto Sc, int ks, bool do_issue, int kn, uint32_t dma) DSF_INLINE {
+  // the other set (substep ks) and (S = 1) a tile's loads into the stage at dma.
+  // (dW, whose reads are all transpose loads, two to a fragment: one fragment at a
+  // time, 8192 x 151936 x 3584: +3 %; the others lose as much by it.)
+  auto substep = [&](auto Sc, int ks, uint32_t dma, uint32_t past) DSF_INLINE {
     constexpr int S = decltype(Sc)::value;
 #pragma unroll
-    for (int i = 0; i < MI; ++i) {
-      acc[i][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(af[S][i], bq[S][0], acc[i][0], 0, 0, 0);
-      __builtin_amdgcn_sched_barrier(0);
-      if (i < MI - 1) {
+    for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int n = i * R / (MI - 1); n < (i + 1) * R / (MI - 1); ++n) read_n(1 - S, ks, n);
-      }
-      if (S == 1 && do_issue) issue(kn, dma, i);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int j = 1; j < NI; ++j)
+      for (int j = 0; j < NI; ++j) {
         acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(af[S][i], bq[S][j], acc[i][j], 0, 0, 0);
-      __builtin_amdgcn_sched_barrier(0);
-    }
+        if constexpr (MODE == kHeadDw) {
+          const int x = i * NI + j;
+          __builtin_amdgcn_sched_barrier(0);
+          if (x % 2 == 1 && x / 2 < R) read_n(1 - S, ks, x / 2);
+          if (S == 1 && j == 5) issue(dma, i, past);
+          __builtin_amdgcn_sched_barrier(0);
+        } else if (j == 0) {
+          __builtin_amdgcn_sched_barrier(0);
+          if (i < MI - 1) {
+#pragma unroll
+            for (int n = i * R / (MI - 1); n < (i + 1) * R / (MI - 1); ++n) read_n(1 - S, ks, n);
+          }
+          if (S == 1) issue(dma, i, past);
+          __builtin_amdgcn_sched_barrier(0);
+        } else if (j == NI - 1) {
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
   };
-  if (kb < ke) {
+  if (nk > 0) {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) issue(kb, lds, u);
-    if (kb + 1 < ke) {
+    for (int t = 0; t < 2; ++t) {
+      const uint32_t past = start();
 #pragma unroll
-      for (int u = 0; u < 4; ++u) issue(kb + 1, lds ^ kStage, u);
-      asm volatile("s_waitcnt vmcnt(8)\n\ts_barrier" ::: "memory");
-    } else {
-      asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+      for (int u = 0; u < 4; ++u) issue(lds ^ (t * kStage), u, past);
     }
+    asm volatile("s_waitcnt vmcnt(8)\n\ts_barrier" ::: "memory");
 #pragma unroll
     for (int n = 0; n < R; ++n) read_n(0, 0, n);
-    uint32_t cur = lds;
+  }
+  uint32_t cur = lds;
+  for (int item = 0; item < items; ++item) {
+    const Item it = item_of(item);
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     // One k-tile. All its fragments are in registers by the middle, where the
-    // barrier publishes the next tile and frees this one's stage. (The last
-    // tile reads stale LDS there; nothing uses it.)
-    for (int kt = kb; kt < ke; ++kt) {
-      substep(std::integral_constant<int, 0>(), 1, false, 0, 0);
+    // barrier publishes the next k-tile and frees this one's stage. (Past the
+    // stream's end zeros are loaded and read; nothing uses them.)
+    for (int kt = it.kb; kt < it.ke; ++kt) {
+      substep(std::integral_constant<int, 0>(), 1, 0, 0);
+      const uint32_t past = start();
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
       fa.at ^= kStage;
       fb.at ^= kStage;
-      substep(std::integral_constant<int, 1>(), 0, kt + 2 < ke, kt + 2, cur);
+      substep(std::integral_constant<int, 1>(), 0, cur, past);
       cur ^= kStage;
     }
-  }
-
-  // lane holds out[n = 16 j + r16][m = 16 i + 4 grp + e] of its wave's part
-  const int m0 = tm * kT + wm * 64, n0 = tn * kT + wn * 128 + r16;
-  if constexpr (MODE == kHeadLogits) {
-    // per row: the maximum over the tile's classes (in units of log 2, at the
-    // temperature), the sum of 2^(z - max), codes (max - z) * kHeadSteps
-    float* red = reinterpret_cast<float*>(smem);  // [2][4][256]
-    const float c = g.z_scale;
-    const bool ragged = (tm + 1) * kT > g.V;
-    float mx[NI];
+    // lane holds out[n = 16 j + r16][m = 16 i + 4 grp + e] of its wave's part
+    const int m0 = it.tm * kT + wm * 64, n0 = it.tn * kT + wn * 128 + r16;
+    if constexpr (MODE == kHeadLogits) {
+      // per row: the maximum over the tile's classes (in units of log 2, at the
+      // temperature), the sum of 2^(z - max), and codes of max - z
+      const float c = g.z_scale;
+      if ((it.tm + 1) * kT > g.V) {
 #pragma unroll
-    for (int j = 0; j < NI; ++j) {
-      mx[j] = -INFINITY;
+        for (int i = 0; i < MI; ++i)
 #pragma unroll
-      for (int i = 0; i < MI; ++i)
+          for (int e = 0; e < 4; ++e)
+            if (m0 + 16 * i + 4 * grp + e >= g.V)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float z = acc[i][j][e] * c;
-          if (ragged && m0 + 16 * i + 4 * grp + e >= g.V) z = -INFINITY;
-          acc[i][j][e] = z;
-          mx[j] = fmaxf(mx[j], z);
+              for (int j = 0; j < NI; ++j) acc[i][j][e] = -INFINITY;
+      }
+      float mx[NI];
+#pragma unroll
+      for (int j = 0; j < NI; ++j) {
+        mx[j] = acc[0][j][0];
+#pragma unroll
+        for (int x = 1; x < 16; ++x) mx[j] = fmaxf(mx[j], acc[x >> 2][j][x & 3]);
+        mx[j] = rows4_max(mx[j]);
+      }
+      if (grp == 0)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) red[wm * kT + wn * 128 + 16 * j + r16] = mx[j];
+      ring_barrier();
+      float* const red2 = red + 4 * kT;
+      float top[NI];
+#pragma unroll
+      for (int j = 0; j < NI; ++j) {
+        const float* r = red + wn * 128 + 16 * j + r16;
+        top[j] = c * fmaxf(fmaxf(r[0], r[kT]), fmaxf(r[2 * kT], r[3 * kT]));
+        const float ref = top[j] == -INFINITY ? 0.f : top[j];
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float below = fmaf(-c, acc[i][j][e], ref);
+            sum += __builtin_amdgcn_exp2f(-below);
+            acc[i][j][e] = below * (1.f / kHeadReach);
+          }
+        sum = rows4_sum(sum);
+        if (grp == 0) red2[wm * kT + wn * 128 + 16 * j + r16] = sum;
+      }
+      ring_barrier();
+      if (wm == 0 && grp == 0)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+          const int n = n0 + 16 * j;
+          const float* r = red2 + wn * 128 + 16 * j + r16;
+          if (n < rows)
+            g.stats[int64_t(it.tm) * g.rows_ld + n] = float2{top[j], (r[0] + r[kT]) + (r[2 * kT] + r[3 * kT])};
         }
-      mx[j] = rows4_max(mx[j]);
-    }
-    __syncthreads();  // every wave has read the last tile
-    if (grp == 0)
+      if (g.zout) {
 #pragma unroll
-      for (int j = 0; j < NI; ++j) red[wm * kT + wn * 128 + 16 * j + r16] = mx[j];
-    __syncthreads();
-    float sum[NI];
+        for (int j = 0; j < NI; ++j) {
+          const int n = n0 + 16 * j;
+          uint16_t* row = (uint16_t*)g.zout + int64_t(n) * g.ldz + m0 + 16 * (grp & 1) + 8 * (grp >> 1);
 #pragma unroll
-    for (int j = 0; j < NI; ++j) {
-      const float* r = red + wn * 128 + 16 * j + r16;
-      const float m = fmaxf(fmaxf(r[0], r[kT]), fmaxf(r[2 * kT], r[3 * kT]));
-      const float ref = m == -INFINITY ? 0.f : m;
-      mx[j] = m;
-      sum[j] = 0.f;
-#pragma unroll
-      for (int i = 0; i < MI; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float below = ref - acc[i][j][e];
-          sum[j] += __builtin_amdgcn_exp2f(-below);
-          acc[i][j][e] = below;
+          for (int i = 0; i < MI; i += 2) {
+            const f32x4 x = acc[i][j], y = acc[i + 1][j];
+            const u32x4 v = swap_rows8(pack_unit(x[0], x[1]), pack_unit(x[2], x[3]), pack_unit(y[0], y[1]),
+                                       pack_unit(y[2], y[3]));
+            if (n < rows) *reinterpret_cast<u32x4*>(row + 16 * i) = v;
+          }
         }
-      sum[j] = rows4_sum(sum[j]);
-    }
-    float* red2 = red + 4 * kT;
-    if (grp == 0)
+      }
+    } else if (MODE == kHeadDh || it.split >= 0) {
+      // a partial sum: dh [split][n][m]; dW [slot][256][256]
+      float* out = MODE == kHeadDh ? g.part + int64_t(it.split) * g.rows_ld * g.d + int64_t(n0) * g.d + m0
+                                   : g.part + (int64_t(it.split) * kT + wn * 128 + r16) * kT + wm * 64;
+      const int ld = MODE == kHeadDh ? g.d : kT;
 #pragma unroll
-      for (int j = 0; j < NI; ++j) red2[wm * kT + wn * 128 + 16 * j + r16] = sum[j];
-    __syncthreads();
-    if (wm == 0 && grp == 0)
+      for (int j = 0; j < NI; ++j)
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+          if (MODE == kHeadDw || (n0 + 16 * j < rows && m0 + 16 * i + 4 * grp < g.d))
+            *reinterpret_cast<f32x4*>(out + int64_t(16 * j) * ld + 16 * i + 4 * grp) = acc[i][j];
+    } else {
+      const float scale = *g.scale;
 #pragma unroll
       for (int j = 0; j < NI; ++j) {
         const int n = n0 + 16 * j;
-        const float* r = red2 + wn * 128 + 16 * j + r16;
-        if (n < rows) g.stats[int64_t(tm) * g.rows_ld + n] = float2{mx[j], (r[0] + r[kT]) + (r[2 * kT] + r[3 * kT])};
-      }
-    if (!g.zout) return;
+        const bool in = n < g.V;
+        const int64_t row = int64_t(n) * g.d;
 #pragma unroll
-    for (int j = 0; j < NI; ++j) {
-      const int n = n0 + 16 * j;
+        for (int i = 0; i < MI; i += 2) {
+          f32x4 v[2];
 #pragma unroll
-      for (int i = 0; i < MI; i += 2) {
-        uint32_t pk[2][2];
-#pragma unroll
-        for (int ii = 0; ii < 2; ++ii)
-#pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            const uint32_t lo = uint32_t(fminf(fmaf(acc[i + ii][j][2 * q], kHeadSteps, 0.5f), 65535.f));
-            const uint32_t hi = uint32_t(fminf(fmaf(acc[i + ii][j][2 * q + 1], kHeadSteps, 0.5f), 65535.f));
-            pk[ii][q] = lo | hi << 16;
+          for (int ii = 0; ii < 2; ++ii) {
+            const int m = m0 + 16 * (i + ii) + 4 * grp;
+            v[ii] = acc[i + ii][j] * scale;
+            if (g.prev && in && m < g.d) v[ii] += *reinterpret_cast<const f32x4*>(g.prev + row + m);
+            if (g.out32 && in && m < g.d) *reinterpret_cast<f32x4*>(g.out32 + row + m) = v[ii];
           }
-        const u32x4 v = swap_rows8(pk[0][0], pk[0][1], pk[1][0], pk[1][1]);
-        if (n < rows)
-          *reinterpret_cast<u32x4*>((uint16_t*)g.zout + int64_t(n) * g.ldz + m0 + 16 * (i + (grp & 1)) + 8 * (grp >> 1)) = v;
-      }
-    }
-  } else if constexpr (MODE == kHeadDh) {
-    float* out = g.part + int64_t(sp) * g.rows_ld * g.d;
+          if (!g.out16) continue;
+          uint32_t pk[2][2];
 #pragma unroll
-    for (int j = 0; j < NI; ++j) {
-      const int n = n0 + 16 * j;
+          for (int ii = 0; ii < 2; ++ii)
 #pragma unroll
-      for (int i = 0; i < MI; ++i) {
-        const int m = m0 + 16 * i + 4 * grp;
-        if (n < rows && m < g.d) *reinterpret_cast<f32x4*>(out + int64_t(n) * g.d + m) = acc[i][j];
-      }
-    }
-  } else {
-    const float scale = *g.scale;
-#pragma unroll
-    for (int j = 0; j < NI; ++j) {
-      const int n = n0 + 16 * j;
-      const bool in = n < g.V;
-      const int64_t row = int64_t(n) * g.d;
-#pragma unroll
-      for (int i = 0; i < MI; i += 2) {
-        f32x4 v[2];
-#pragma unroll
-        for (int ii = 0; ii < 2; ++ii) {
-          const int m = m0 + 16 * (i + ii) + 4 * grp;
-          v[ii] = acc[i + ii][j] * scale;
-          if (g.prev && in && m < g.d) v[ii] += *reinterpret_cast<const f32x4*>(g.prev + row + m);
-          if (g.out32 && in && m < g.d) *reinterpret_cast<f32x4*>(g.out32 + row + m) = v[ii];
+            for (int q = 0; q < 2; ++q)
+              pk[ii][q] = uint32_t(f2bf(v[ii][2 * q])) | uint32_t(f2bf(v[ii][2 * q + 1])) << 16;
+          const u32x4 u = swap_rows8(pk[0][0], pk[0][1], pk[1][0], pk[1][1]);
+          const int m = m0 + 16 * (i + (grp & 1)) + 8 * (grp >> 1);
+          if (in && m < g.d) *reinterpret_cast<u32x4*>(g.out16 + row + m) = u;
         }
-        if (!g.out16) continue;
-        uint32_t pk[2][2];
-#pragma unroll
-        for (int ii = 0; ii < 2; ++ii)
-#pragma unroll
-          for (int q = 0; q < 2; ++q)
-            pk[ii][q] = uint32_t(f2bf(v[ii][2 * q])) | uint32_t(f2bf(v[ii][2 * q + 1])) << 16;
-        const u32x4 u = swap_rows8(pk[0][0], pk[0][1], pk[1][0], pk[1][1]);
-        const int m = m0 + 16 * (i + (grp & 1)) + 8 * (grp >> 1);
-        if (in && m < g.d) *reinterpret_cast<u32x4*>(g.out16 + row + m) = u;
       }
     }
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // loads past the stream's end write LDS
+}
+
+// dW of the tiles that the last, incomplete round cut along the rows: their partial sums
+// added in order, then as in the kernel above. A workgroup takes 32 rows of a tile.
+__global__ __launch_bounds__(256) void head_dw_join_kernel(HeadGemmArgs g, int grid) {
+  const int rows = head_piece_rows(g), nk = (rows + kBK - 1) / kBK;
+  const int tv = (g.V + kT - 1) / kT, td = (g.d + kT - 1) / kT, nt = tv * td, full = nt / grid * grid;
+  const int cut = head_dw_cut(nt - full, nk, grid);
+  if (cut <= 1) return;
+  const int t = int(blockIdx.x) >> 3;
+  const GemmTile gt = gemm_tile(full + t, tv, td, 4);
+  const int n = gt.tm * kT + (int(blockIdx.x) & 7) * 32 + int(threadIdx.x >> 3);
+  const float scale = *g.scale;
+  if (n >= g.V) return;
+  const float* src = g.part + (int64_t(t) * cut * kT + (n & (kT - 1))) * kT;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int mc = 8 * (int(threadIdx.x & 7) + 8 * u), m = gt.tn * kT + mc;
+    if (m >= g.d) continue;
+    float v[8], x[8];
+    load8(src + mc, v);
+    for (int s = 1; s < cut; ++s) {
+      load8(src + int64_t(s) * kT * kT + mc, x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += x[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= scale;
+    const int64_t at = int64_t(n) * g.d + m;
+    if (g.prev) {
+      load8(g.prev + at, x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += x[e];
+    }
+    if (g.out32) store8(g.out32 + at, v);
+    if (g.out16) store8(g.out16 + at, v);
   }
 }
 
 hipError_t launch_head_gemm(int mode, const HeadGemmArgs& g, hipStream_t s) {
-  const int tr = (g.rows + kT - 1) / kT, tv = (g.V + kT - 1) / kT, td = (g.d + kT - 1) / kT;
-  if (mode == kHeadLogits) head_gemm_kernel<kHeadLogits><<<tr * tv, kThreads, 0, s>>>(g);
-  else if (mode == kHeadDh) head_gemm_kernel<kHeadDh><<<tr * td * g.splits, kThreads, 0, s>>>(g);
-  else head_gemm_kernel<kHeadDw><<<tv * td, kThreads, 0, s>>>(g);
+  const int64_t tr = (g.rows + kT - 1) / kT, tv = (g.V + kT - 1) / kT, td = (g.d + kT - 1) / kT;
+  auto grid = [](int64_t items) { return dim3(uint32_t(std::min<int64_t>(kHeadGrid, (items + kXcds - 1) / kXcds * kXcds))); };
+  if (mode == kHeadLogits) {
+    head_gemm_kernel<kHeadLogits><<<grid(tr * tv), kThreads, 0, s>>>(g);
+  } else if (mode == kHeadDh) {
+    head_gemm_kernel<kHeadDh><<<kHeadGrid, kThreads, 0, s>>>(g);
+  } else {
+    const int nt = int(tv * td), left = nt % kHeadGrid;
+    head_gemm_kernel<kHeadDw><<<kHeadGrid, kThreads, 0, s>>>(g);
+    if (left && 2 * left <= kHeadGrid) head_dw_join_kernel<<<left * 8, 256, 0, s>>>(g, kHeadGrid);
+  }
   return hipGetLastError();
 }
 

@@ -8,7 +8,7 @@ import torch
 DT = {"f32": torch.float32, "bf16": torch.bfloat16}
 HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}  # half a step, relative
 U = 2.0 ** -24
-CODE = np.log(2.0) / 2048  # half a step of a logit's code (1024 to a factor of two), relative in a probability
+CODE = np.log(2.0) * 32 / 65535  # half a step of a logit's code (65535 to 64 factors of two), relative in a probability
 
 
 def rand(shape, dtype, seed, scale=1.0, shift=0.0):

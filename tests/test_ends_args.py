@@ -94,10 +94,10 @@ def test_workspace_sizes():
     assert P.norm_backward_workspace_size(10, 12) == 0 and P.norm_backward_workspace_size(10, 16) > 0
     assert P.head_workspace_size(P.BF16, 10, 64, 0) == 0 and P.head_workspace_size(P.BF16, 10, 64, 100, top=2000) == 0
     assert P.head_workspace_size(P.E4M3, 10, 64, 100) == 0
-    # never the logits of a call at once: 16 bits for each of as many rows as fit 2 GiB
+    # never the logits of a call at once: 16 bits for each of as many rows as fit 4 GiB
     n, d, V = 1 << 17, 896, 151936
     size = P.head_workspace_size(P.BF16, n, d, V)
-    assert 0 < size < (2 << 30) + 4 * V * d + 2 * n * d + (1 << 30) < 2 * n * V
+    assert 0 < size < (4 << 30) + 4 * V * d + 2 * n * d + (1 << 30) < 2 * n * V
     assert P.head_workspace_size(P.BF16, n, d, V, gradients=False) < size
     # enough for the call without gradients
     for args in [(100, 64, 1003), (5000, 896, 151936), (1, 8, 1)]:

@@ -149,7 +149,7 @@ def test_a_bad_row_spoils_its_own_results(dev):
     assert bad["row_loss"][7].isnan() and bad["dh"][7].isnan().all() and bad["dw"].isnan().any()
 
 
-@pytest.mark.parametrize("dtype,n,V", [("bf16", 700, 1 << 21), ("f32", 300, (1 << 21) - 5), ("bf16", 1600, 700001)])
+@pytest.mark.parametrize("dtype,n,V", [("bf16", 1200, 1 << 21), ("f32", 600, (1 << 21) - 5), ("bf16", 3200, 700001)])
 @pytest.mark.parametrize("dw_type", ["same", "f32"])
 def test_rows_in_pieces(dev, dtype, n, V, dw_type):
     """More rows than fit one piece of the workspace. The reference is taken on the GPU in 64 bits, half the rows at a

@@ -7,7 +7,7 @@ from test_paged_dma_waits import WAIT_STATES, _listing
 
 
 def test_loads_into_lds_wait_for_their_operands(tmp_path):
-    kernel, waited, loads = "", None, 0
+    kernel, waited, moved, loads = "", None, 0, 0
     for line in _listing(tmp_path):
         name = re.match(r"^[0-9a-f]+ <(.+)>:", line)
         if name:
@@ -15,13 +15,16 @@ def test_loads_into_lds_wait_for_their_operands(tmp_path):
         words = line.split("//")[0].split()
         if "head_gemm_kernel" not in kernel or len(words) < 2:
             continue
-        if words[:2] == ["s_mov_b32", "m0,"]:
-            waited = 1
-        elif words[0] == "s_nop" and waited is not None:
+        # wait states since the block's first instruction, a move to m0; a block may hold two loads
+        if words[0] == "s_nop" and waited is not None:
             waited += int(words[1], 0) + 1
         elif words[0].startswith("buffer_load") and words[-1] == "lds":
             assert waited is not None and waited >= WAIT_STATES, f"{kernel}: {line.strip()} after {waited} wait states"
-            waited, loads = None, loads + 1
-        elif waited is not None:
-            waited += 1
+            assert moved >= 2, f"{kernel}: {line.strip()} right after its move to m0"
+            waited, loads = waited + 1, loads + 1
+        elif words[:2] == ["s_mov_b32", "m0,"]:
+            waited, moved = 1 if waited is None else waited + 1, 0
+        else:
+            waited = None
+        moved += 1 if words[0] != "s_nop" else int(words[1], 0) + 1
     assert loads > 0
