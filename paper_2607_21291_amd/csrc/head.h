@@ -16,6 +16,15 @@ constexpr int kHeadGrid = 256;  // workgroups of a product: one per CU
 constexpr int kHeadTile = 256;  // classes of a tile of the logits
 constexpr int kHeadMaxTop = 1024;
 
+// The codes, and dz after them (bf16), lie in blocks of 256 rows by 64 classes, rows of
+// 128 bytes: a block is what a product reads of them for one of its k-tiles (by
+// rows: four quarters of blocks), and an eighth of a wave's tile of logits. Rows
+// of all classes, 300 KB apart, had a CU read from 40 pages of 2 MB at a time.
+constexpr int kZRows = 256, kZClasses = 64, kZBlock = kZRows * kZClasses;
+__host__ __device__ inline int64_t head_z_at(int row, int c, int ldz) {
+  return (int64_t(row / kZRows) * (ldz / kZClasses) + c / kZClasses) * kZBlock + (row % kZRows) * kZClasses + c % kZClasses;
+}
+
 enum HeadMode { kHeadLogits = 0, kHeadDh = 1, kHeadDw = 2 };
 
 // One of a call's three products, over a piece of its active rows (bf16; fp32
@@ -23,8 +32,8 @@ enum HeadMode { kHeadLogits = 0, kHeadDh = 1, kHeadDw = 2 };
 struct HeadGemmArgs {
   const void* h;        // active rows of this piece [rows, d]
   const void* w;        // [V, d]
-  const void* z;        // dz [rows, ldz]
-  void* zout;           // codes (fp32: logits in units of log 2) [rows, ldz]; null: statistics alone
+  const void* z;        // dz of rows x ldz classes, in blocks (fp32: [rows, ldz])
+  void* zout;           // codes, in blocks (fp32: logits in units of log 2, [rows, ldz]); null: statistics alone
   float2* stats;        // bf16: [classes / 256][rows_ld] (maximum, sum)
   float* part;          // partial sums: of dh [splits][rows_ld][d], of dW's last round [kHeadGrid][256][256]
   const float* prev;    // dW so far, fp32 (nullable)

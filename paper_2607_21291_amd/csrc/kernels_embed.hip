@@ -17,7 +17,7 @@ namespace dsf {
 namespace {
 constexpr int kRange = 256;  // table rows of a workgroup of the sort
 constexpr int kWaves = 16;
-constexpr int kLong = 64;
+constexpr int kLong = 32;
 }  // namespace
 
 // out[i] = scale * table[tokens[i]], zeros for a token outside [0, V). A
@@ -56,16 +56,19 @@ __global__ __launch_bounds__(256) void embed_kernel(const int32_t* __restrict__ 
   }
 }
 
-// Positions sorted by token, those of one token ascending; start[v] = number
+// Positions sorted by token, those of one token ascending (and, for a gradient
+// written whole, the rows of absent tokens: zeros, `row_vecs` vectors of 16 bytes); start[v] = number
 // of positions whose token is in [0, v). A workgroup sorts the positions of
 // kRange tokens: it reads all tokens twice (they stay in L2), counts those
 // before its range, and each wave places the positions of its stretch, 64 at
 // a time, ranked among equals by ballots over the bits of the token.
 __global__ __launch_bounds__(64 * kWaves) void embed_order_kernel(const int32_t* __restrict__ tokens, int n, int V,
                                                                   int32_t* __restrict__ order,
-                                                                  int32_t* __restrict__ start) {
+                                                                  int32_t* __restrict__ start,
+                                                                  u32x4* __restrict__ out, int row_vecs) {
   __shared__ int hist[kWaves][kRange];
   __shared__ int part[kWaves];
+  __shared__ uint64_t absent[kRange / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t lo = int64_t(blockIdx.x) * kRange;
   const int size = int(std::min<int64_t>(kRange, V - lo));
@@ -111,6 +114,8 @@ __global__ __launch_bounds__(64 * kWaves) void embed_order_kernel(const int32_t*
   if (lane == 63) part[wave] = incl;
   __syncthreads();
   if (tid < kRange) {
+    const uint64_t none = __ballot(tid < size && all == 0);
+    if (lane == 0) absent[wave] = none;
     int at = base + incl - all;
     for (int w = 0; w < wave; ++w) at += part[w];
     if (tid < size) start[lo + tid] = at;
@@ -147,6 +152,13 @@ __global__ __launch_bounds__(64 * kWaves) void embed_order_kernel(const int32_t*
       __builtin_amdgcn_wave_barrier();
     }
   }
+  if (!out) return;
+  constexpr int kRows = kRange / kWaves;
+  uint32_t rows = uint32_t(absent[wave * kRows / 64] >> (wave * kRows % 64)) & ((1u << kRows) - 1u);
+  u32x4* p = out + (lo + wave * kRows) * row_vecs;
+  for (; rows; rows >>= 1, p += row_vecs)
+    if (rows & 1)
+      for (int c = lane; c < row_vecs; c += 64) p[c] = u32x4{0, 0, 0, 0};
 }
 
 struct EmbedSumArgs {
@@ -155,7 +167,7 @@ struct EmbedSumArgs {
   float* part;  // [pieces][2][d]: sums of a piece's positions for the token it goes on with, and for the one it begins
   int n, V, d, accumulate;
   float scale;
-  int sum_wgs, long_wgs, slabs;
+  int long_wgs, slabs;
 };
 
 constexpr int kSlab = 512;  // columns a wave sums at a time (8 a lane)
@@ -176,55 +188,43 @@ __device__ __forceinline__ void embed_store(TO* p, const float* v, float scale, 
 // which must be running; `in` (c < d) covers the loads alone.
 template <typename TI>
 __device__ __forceinline__ void embed_rows(const TI* dy, int d, int pos, int first, int count, int c, bool in, float* v) {
+  constexpr int U = 8;  // rows in flight
+  const int end = first + count;
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = 0.f;
-  for (int j = first; j < first + count; j += 4) {
-    int64_t at[4];
+  for (int j = first; j < end; j += U) {
+    int64_t at[U];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) at[u] = int64_t(__builtin_amdgcn_readlane(pos, std::min(j + u, first + count - 1))) * d;
-    float x[4][8];
+    for (int u = 0; u < U; ++u) at[u] = int64_t(__builtin_amdgcn_readlane(pos, std::min(j + u, end - 1))) * d;
     if (in) {
+      Raw8<TI> x[U];
+      // (past the end the last row again, which is not added)
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (j + u < first + count) load8(dy + at[u] + c, x[u]);
+      for (int u = 0; u < U; ++u)
+        if (u < 2 || j + u < end) x[u] = load_raw8(dy + at[u] + c);
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (j + u < first + count)
+      for (int u = 0; u < U; ++u)
+        if (j + u < end) {
+          float f[8];
+          unpack8(x[u], f);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] += x[u][e];
+          for (int e = 0; e < 8; ++e) v[e] += f[e];
+        }
     }
   }
 }
 
-// Workgroups [0, sum_wgs): a wave to a sorted place that begins a token of at
-// most kLong positions. Then long_wgs: a wave to a piece and slab, the sums of
-// longer ones. Then (gradients written whole) the rows of absent tokens.
+// Workgroups [0, long_wgs): a wave to a piece and slab, the sums of tokens of more
+// than kLong positions. The others: a wave to a slab and a sorted place that begins
+// a token of fewer.
 template <typename TI, typename TO>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedSumArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6));
-  int wg = blockIdx.x;
   const TI* dy = (const TI*)a.dy;
   TO* out = (TO*)a.out;
   const int n = a.start[a.V];  // positions that have a token
-  if (wg < a.sum_wgs) {
-    const int i = wg * 4 + wave;
-    if (i >= n) return;
-    const int t = a.tokens[a.order[i]];
-    if (a.start[t] != i) return;
-    const int m = a.start[t + 1] - i;
-    if (m > kLong) return;
-    const int pos = a.order[i + std::min(lane, m - 1)];
-    for (int c0 = 0; c0 < a.d; c0 += kSlab) {
-      const int c = c0 + lane * 8;
-      float v[8];
-      embed_rows(dy, a.d, pos, 0, m, c, c < a.d, v);
-      if (c < a.d) embed_store(out + int64_t(t) * a.d + c, v, a.scale, a.accumulate);
-    }
-    return;
-  }
-  wg -= a.sum_wgs;
-  if (wg < a.long_wgs) {
-    const int task = wg * 4 + wave, piece = task / a.slabs, c = (task - piece * a.slabs) * kSlab + lane * 8;
+  if (int(blockIdx.x) < a.long_wgs) {
+    const int task = int(blockIdx.x) * 4 + wave, piece = task / a.slabs, c = (task - piece * a.slabs) * kSlab + lane * 8;
     const int i0 = piece * kLong;
     if (i0 >= n) return;
     const int m = std::min(kLong, n - i0);
@@ -243,18 +243,16 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedSumArgs a) {
     }
     return;
   }
-  wg -= a.long_wgs;
-  // 64 rows a workgroup, 16 a wave
-  const int64_t r0 = int64_t(wg) * 64 + wave * 16;
-  const int64_t mine = r0 + std::min(lane, 15);
-  const bool none = lane < 16 && mine < a.V && a.start[mine] == a.start[mine + 1];
-  uint64_t rows = __ballot(none);
-  const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  while (rows) {
-    const int i = __builtin_ctzll(rows);
-    rows &= rows - 1;
-    for (int c = lane * 8; c < a.d; c += kSlab) store8(out + (r0 + i) * a.d + c, zero);
-  }
+  const int64_t task = (int64_t(blockIdx.x) - a.long_wgs) * 4 + wave;
+  const int i = int(task / a.slabs), c = int(task - int64_t(i) * a.slabs) * kSlab + lane * 8;
+  if (i >= n) return;
+  const int t = a.tokens[a.order[i]];
+  const int m = a.start[t + 1] - i;
+  if (a.start[t] != i || m > kLong) return;
+  const int pos = a.order[i + std::min(lane, m - 1)];
+  float v[8];
+  embed_rows(dy, a.d, pos, 0, m, c, c < a.d, v);
+  if (c < a.d) embed_store(out + int64_t(t) * a.d + c, v, a.scale, a.accumulate);
 }
 
 // The rows of tokens of more than kLong positions: a wave to the piece that a
@@ -326,12 +324,12 @@ hipError_t launch_embed_backward(const EmbedBackwardArgs& b, hipStream_t s) {
   a.accumulate = b.accumulate;
   a.scale = b.scale;
   a.slabs = (b.d + kSlab - 1) / kSlab;
-  a.sum_wgs = (b.n + 3) / 4;
   const int64_t tasks = b.n > kLong ? int64_t((b.n + kLong - 1) / kLong) * a.slabs : 0;
   a.long_wgs = int((tasks + 3) / 4);
-  const int zero_wgs = b.accumulate ? 0 : (b.V + 63) / 64;
-  embed_order_kernel<<<(b.V + kRange - 1) / kRange, 64 * kWaves, 0, s>>>(b.tokens, b.n, b.V, order, start);
-  const dim3 grid(uint32_t(a.sum_wgs + a.long_wgs + zero_wgs));
+  const int row_vecs = b.d * (b.dtable_type == DSF_F32 ? 4 : 2) / 16;
+  embed_order_kernel<<<(b.V + kRange - 1) / kRange, 64 * kWaves, 0, s>>>(b.tokens, b.n, b.V, order, start,
+                                                                         b.accumulate ? nullptr : (u32x4*)b.dtable, row_vecs);
+  const dim3 grid(uint32_t(a.long_wgs + (int64_t(b.n) * a.slabs + 3) / 4));
   const bool in32 = b.dtype == DSF_F32, out32 = b.dtable_type == DSF_F32;
   if (grid.x) {
     if (in32) embed_sum_kernel<float, float><<<grid, 256, 0, s>>>(a);

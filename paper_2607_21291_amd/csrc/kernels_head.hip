@@ -78,19 +78,29 @@ __global__ __launch_bounds__(256) void head_teacher_kernel(const int32_t* __rest
   }
 }
 
-// Shares of the classes for dh: each round of the grid costs its k-tiles and about
-// eight more, each share a partial sum written and read again (at some 3 MB a k-tile).
-__device__ __forceinline__ int head_dh_splits(int rows, int d, int ldz, bool f32, int most) {
+// Shares of the classes for dh, by a whole wave: each round of the grid costs its
+// k-tiles and about eight more, each share a partial sum written and read again
+// (at some 3 MB a k-tile). The fewest of the cheapest.
+__device__ __forceinline__ int head_dh_splits(int rows, int d, int ldz, bool f32, int most, int lane) {
   const int t = f32 ? 128 : 256, slots = f32 ? 512 : kHeadGrid;
   const int tiles = ((rows + t - 1) / t) * ((d + t - 1) / t);
   const float nk = float(ldz) / 64.f, join = float(rows) * float(d) * 8.f / (f32 ? 4e6f : 3e6f);
   int got = 1;
-  float best = 0.f;
-  for (int s = 1; s <= most; ++s) {
+  float best = INFINITY;
+  for (int s = 1 + lane; s <= most; s += 64) {
     const float cost = float((tiles * s + slots - 1) / slots) * (nk / float(s) + 8.f) + float(s) * join;
-    if (s == 1 || cost < best) {
+    if (cost < best) {
       best = cost;
       got = s;
+    }
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const float c = __shfl_xor(best, o, 64);
+    const int g = __shfl_xor(got, o, 64);
+    if (c < best || (c == best && g < got)) {
+      best = c;
+      got = g;
     }
   }
   return got;
@@ -167,8 +177,10 @@ __global__ __launch_bounds__(1024) void head_rows_kernel(HeadRowsArgs a) {
     }
   }
   if (a.splits)
-    for (int p = tid; p < a.pieces; p += 1024)
-      a.splits[p] = head_dh_splits(std::max(0, std::min(all - p * a.rows, a.rows)), a.d, a.ldz, a.f32 != 0, a.most);
+    for (int p = wave; p < a.pieces; p += 16) {
+      const int n = head_dh_splits(std::max(0, std::min(all - p * a.rows, a.rows)), a.d, a.ldz, a.f32 != 0, a.most, lane);
+      if (lane == 0) a.splits[p] = n;
+    }
   if (tid == 0) {
     *a.n_active = all;
     *a.wsum = sum;
@@ -345,64 +357,100 @@ __global__ __launch_bounds__(1024) void head_lse_kernel(HeadLseArgs a) {
   }
 }
 
-// dz / T in place of the logits: weight (p - q). A workgroup takes a row and a
-// range of its classes: p from all codes, then the target classes' entries
-// from their fp32 logits (p - sum of the q of a class, also where a list names
-// it twice).
+// dz / T in place of the logits: weight (p - q). A workgroup takes some rows and
+// a range of their classes: p from all codes (fp32: logits), then the target
+// classes' entries from their fp32 logits (p - sum of the q of a class, also
+// where a list names it twice).
 struct HeadProbsArgs {
   void* z; int ldz;
   const float2* stats; int rows_ld;  // bf16: the tiles' maxima
   const float* lse; const float* z2; const float* q;
   const float* weight; const int32_t* classes;
   const int32_t* act; const int32_t* n_active;
-  int row0, rows, k, V, cuts, cols;  // cols: classes of a range, a multiple of 2048
+  int row0, rows, k, V, cuts, cols;  // cols: classes of a range, a multiple of 2048 (bf16: 256)
 };
-template <typename T>
-__global__ __launch_bounds__(256) void head_probs_kernel(HeadProbsArgs a) {
-  constexpr int VEC = Elem<T>::kVec;
-  const int s = int(blockIdx.x) / a.cuts, c0 = (int(blockIdx.x) - s * a.cuts) * a.cols;
-  if (s >= std::min(*a.n_active - a.row0, a.rows)) return;
-  const int c1 = std::min(a.ldz, c0 + a.cols), g = a.row0 + s;
-  const float lse = a.lse[s];
-  const int row = a.act[g];
-  const float wt = a.weight ? a.weight[row] : 1.f;
-  T* z = (T*)a.z + int64_t(s) * a.ldz;
-  for (int c = c0 + int(threadIdx.x) * VEC; c < c1; c += 256 * VEC) {
-    float p[VEC];
-    if constexpr (sizeof(T) == 2) {
-      const float top = a.stats[int64_t(c / kHeadTile) * a.rows_ld + s].x - lse;
-      const u32x4 raw = *reinterpret_cast<const u32x4*>(z + c);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const uint32_t code = e ? raw[i] >> 16 : raw[i] & 0xffffu;
-          const float x = __builtin_amdgcn_exp2f(fmaf(float(code), -kHeadReach / 65535.f, top));
-          p[2 * i + e] = code == 0xffffu ? 0.f : wt * x;
-        }
-    } else {
-      load_vec(z + c, p);
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) p[i] = p[i] == -INFINITY ? 0.f : wt * exp2f(p[i] - lse);
-    }
-    store_vec(z + c, p);
-  }
-  __syncthreads();  // (with it the stores above have completed)
+// The entry of list place j of slot s, if its class lies in [c0, c1).
+template <typename F>
+__device__ __forceinline__ void head_probs_entry(const HeadProbsArgs& a, int s, int j, int c0, int c1, F store) {
+  const int g = a.row0 + s, row = a.act[g];
   const int32_t* cls = a.classes + int64_t(row) * a.k;
   const float* q = a.q ? a.q + int64_t(row) * a.k : nullptr;
-  const int hi = std::min(c1, a.V);
-  for (int j = threadIdx.x; j < a.k; j += 256) {
-    const int c = cls[j];
-    if (c < c0 || c >= hi) continue;
-    float sum = q ? q[j] : 1.f;
-    bool first = true;
-    for (int i = 0; i < a.k; ++i)
-      if (i != j && cls[i] == c) {
-        first = first && i > j;
-        sum += q ? q[i] : 1.f;
+  const int c = cls[j];
+  if (c < c0 || c >= std::min(c1, a.V)) return;
+  float sum = q ? q[j] : 1.f;
+  bool first = true;
+  for (int i = 0; i < a.k; ++i)
+    if (i != j && cls[i] == c) {
+      first = first && i > j;
+      sum += q ? q[i] : 1.f;
+    }
+  if (first) store(c, (a.weight ? a.weight[row] : 1.f) * (exp2f(a.z2[int64_t(g) * a.k + j] - a.lse[s]) - sum));
+}
+
+// bf16, in blocks: 32 rows, a thread to 16 bytes of a row of a block, then the
+// same of the next. Rows from the last that takes part to the next multiple of
+// 64 become zeros.
+constexpr int kProbsRows = 32;
+__global__ __launch_bounds__(256) void head_probs_kernel(HeadProbsArgs a) {
+  // the last rows first: their logits were written last
+  const int rows = std::min(*a.n_active - a.row0, a.rows), r = int(blockIdx.x) / a.cuts;
+  if (rows <= 0) return;
+  const int s0 = ((rows + 63) / 64 * 64 / kProbsRows - 1 - r) * kProbsRows, c0 = (int(blockIdx.x) - r * a.cuts) * a.cols;
+  if (s0 < 0) return;
+  const int c1 = std::min(a.ldz, c0 + a.cols), s = s0 + int(threadIdx.x >> 3);
+  const bool live = s < rows;
+  const float lse = live ? a.lse[s] : 0.f;
+  const float wt = !live ? 0.f : a.weight ? a.weight[a.act[a.row0 + s]] : 1.f;
+  u32x4* p = reinterpret_cast<u32x4*>((uint16_t*)a.z + head_z_at(s, c0, a.ldz) + (threadIdx.x & 7) * 8);
+  constexpr int kStep = kZBlock / 8;  // vectors of a block
+  auto probs = [&](u32x4& raw, float top) {
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t code = e ? raw[i] >> 16 : raw[i] & 0xffffu;
+        const float x = __builtin_amdgcn_exp2f(fmaf(float(code), -kHeadReach / 65535.f, top));
+        v[2 * i + e] = !live || code == 0xffffu ? 0.f : wt * x;
       }
-    if (first) z[c] = Elem<T>::from_f(wt * (exp2f(a.z2[int64_t(g) * a.k + j] - lse) - sum));
+    store_vec(reinterpret_cast<uint16_t*>(&raw), v);
+  };
+  for (int c = c0; c < c1; c += kHeadTile, p += 4 * kStep) {
+    const float top = live ? a.stats[int64_t(c / kHeadTile) * a.rows_ld + s].x - lse : 0.f;
+    u32x4 raw[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) raw[u] = p[u * kStep];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      probs(raw[u], top);
+      p[u * kStep] = raw[u];
+    }
   }
+  __syncthreads();  // (with it the stores above have completed)
+  for (int i = threadIdx.x; i < kProbsRows * a.k; i += 256) {
+    const int si = s0 + i / a.k;
+    if (si < rows)
+      head_probs_entry(a, si, i % a.k, c0, c1,
+                       [&](int c, float v) { ((uint16_t*)a.z)[head_z_at(si, c, a.ldz)] = f2bf(v); });
+  }
+}
+
+// fp32, a row.
+__global__ __launch_bounds__(256) void head_probs_f32_kernel(HeadProbsArgs a) {
+  const int s = int(blockIdx.x) / a.cuts, c0 = (int(blockIdx.x) - s * a.cuts) * a.cols;
+  if (s >= std::min(*a.n_active - a.row0, a.rows)) return;
+  const int c1 = std::min(a.ldz, c0 + a.cols);
+  const float lse = a.lse[s], wt = a.weight ? a.weight[a.act[a.row0 + s]] : 1.f;
+  float* z = (float*)a.z + int64_t(s) * a.ldz;
+  for (int c = c0 + int(threadIdx.x) * 4; c < c1; c += 1024) {
+    float p[4];
+    load_vec(z + c, p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = p[i] == -INFINITY ? 0.f : wt * exp2f(p[i] - lse);
+    store_vec(z + c, p);
+  }
+  __syncthreads();
+  for (int j = threadIdx.x; j < a.k; j += 256) head_probs_entry(a, s, j, c0, c1, [&](int c, float v) { z[c] = v; });
 }
 
 // dh of every row: scale times the sum of its partial sums, zeros for rows that
@@ -471,9 +519,10 @@ HeadPlan head_plan(int dtype, int n, int d, int V, int k, bool grads) {
   // shares of the classes for dh, at most
   const int64_t fit = int64_t(kDhPartBytes / (size_t(p.rows) * d * 4));
   p.most = int(std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(128, p.ldz / 256), fit)));
-  // ranges of a row for dz: about four workgroups per CU
-  p.cuts = std::max(1, std::min(p.ldz / 2048, (1024 + p.rows - 1) / p.rows));
-  p.cols = ((p.ldz + p.cuts - 1) / p.cuts + 2047) / 2048 * 2048;
+  // ranges of the classes for dz: some workgroups for each CU
+  const int unit = f32 ? 2048 : kHeadTile, groups = f32 ? p.rows : p.rows / kProbsRows;
+  p.cuts = std::max(1, std::min(p.ldz / unit, (2048 + groups - 1) / groups));
+  p.cols = ((p.ldz + p.cuts - 1) / p.cuts + unit - 1) / unit * unit;
   p.cuts = (p.ldz + p.cols - 1) / p.cols;
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -617,8 +666,8 @@ hipError_t launch_head_loss(const HeadLossArgs& a, hipStream_t s) {
     b.V = a.V;
     b.cuts = p.cuts;
     b.cols = p.cols;
-    if (f32) head_probs_kernel<float><<<g.rows * p.cuts, 256, 0, s>>>(b);
-    else head_probs_kernel<uint16_t><<<g.rows * p.cuts, 256, 0, s>>>(b);
+    if (f32) head_probs_f32_kernel<<<g.rows * p.cuts, 256, 0, s>>>(b);
+    else head_probs_kernel<<<(g.rows + 63) / 64 * 64 / kProbsRows * p.cuts, 256, 0, s>>>(b);
     DSF_TRY(hipGetLastError());
     if (a.dh) {
       DSF_TRY(product(kHeadDh));

@@ -1,6 +1,6 @@
 // The head's three products in fp32, on the fp32 matrix cores: the forms of
 // kernels_headgemm.hip on 128 x 128 tiles of four waves (64 x 64 each,
-// v_mfma_f32_32x32x2_f32), 16 of k in an LDS stage [k][x], whatever way an
+// v_mfma_f32_32x32x2_f32), 32 of k in an LDS stage [k][x], whatever way an
 // operand lies in memory; the next stage's values wait in registers. Logits are
 // stored as they are (in units of log 2), their statistics are a pass of their
 // own (kernels_head.hip).
@@ -10,7 +10,8 @@
 namespace dsf {
 
 namespace {
-constexpr int kT = 128, kBK = 16, kLD = 160;  // 160 = 32 mod 64 banks: a read's two k lie in different halves
+constexpr int kT = 128, kBK = 32, kLD = 132;
+constexpr int kVecs = kT * kBK / 4 / 256;  // 16-byte vectors of an operand a thread brings
 
 // COL false: element (x, k) at p[x ld + k]; COL true: at p[k ld + x]. Outside
 // [0, nx) x [0, nk) zeros (nx, nk, ld multiples of 4 on the contiguous side).
@@ -19,25 +20,25 @@ struct F32Op {
   const float* p;
   int64_t ld;
   int nx, nk;
-  f32x4 r[2];
-  // values of k0 .. k0 + 15, x0 .. x0 + 127: two vectors a thread
+  f32x4 r[kVecs];
+  // values of k0 .. k0 + 31, x0 .. x0 + 127
   __device__ __forceinline__ void load(int64_t x0, int k0, int tid) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int64_t x = COL ? x0 + 4 * (tid & 31) : x0 + (tid & 63) + 64 * u;
-      const int k = COL ? k0 + (tid >> 5) + 8 * u : k0 + 4 * (tid >> 6);
+    for (int u = 0; u < kVecs; ++u) {
+      const int64_t x = COL ? x0 + 4 * (tid & 31) : x0 + (tid & 63) + 64 * (u & 1);
+      const int k = COL ? k0 + (tid >> 5) + 8 * u : k0 + 4 * (tid >> 6) + 16 * (u >> 1);
       r[u] = x < nx && k < nk ? *reinterpret_cast<const f32x4*>(p + (COL ? k * ld + x : x * ld + k))
                               : f32x4{0.f, 0.f, 0.f, 0.f};
     }
   }
   __device__ __forceinline__ void store(float* lds, int tid) const {
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
+    for (int u = 0; u < kVecs; ++u) {
       if constexpr (COL) {
         *reinterpret_cast<f32x4*>(lds + ((tid >> 5) + 8 * u) * kLD + 4 * (tid & 31)) = r[u];
       } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) lds[(4 * (tid >> 6) + i) * kLD + (tid & 63) + 64 * u] = r[u][i];
+        for (int i = 0; i < 4; ++i) lds[(4 * (tid >> 6) + 16 * (u >> 1) + i) * kLD + (tid & 63) + 64 * (u & 1)] = r[u][i];
       }
     }
   }

@@ -63,23 +63,36 @@ __device__ __forceinline__ void head_dma2(u32x4 ra, uint32_t va, uint32_t at0, u
 // COL true: element (x, k) at p[k ld + x]; subtile l / 16 (128 columns) rows 4 (l % 16) .. + 3
 //   of k, 256 bytes each, chunk c of row r at c ^ key(r), key(r) = 2 ((r & 3) + 4 (r >> 3 & 1)): the
 //   sixteen rows of a transpose load, 32 bytes each, then cover the 64 banks twice, the minimum.
-// What lies past the operand's last row reads as zeros (the resource ends there).
-template <bool COL>
+// BLOCKS: dz in its blocks, rows being x (COL false) or k (COL true).
+// What lies past the operand's last row reads as zeros (the resource ends there);
+// of dz by rows of k the rows to the next multiple of 64 are zeros in memory.
+template <bool COL, bool BLOCKS>
 struct HeadOp {
   const char* base = nullptr;  // of the next k-tile to load
   uint32_t ld2 = 0;            // bytes of a row
   int rows = 0;                // COL: rows of k left; else rows of the tile
   uint32_t voff = 0;
+  int64_t step = 0;            // BLOCKS by rows of k: from a quarter of blocks to the next row of blocks
+  int quarter = 0;
   __device__ __forceinline__ void set(const void* p, int ld, int64_t nx, int64_t nk, int64_t x0, int kt, int wave,
                                       int lane) {
-    ld2 = uint32_t(ld) * 2u;
+    ld2 = BLOCKS ? uint32_t(kZClasses) * 2u : uint32_t(ld) * 2u;
     if constexpr (COL) {
-      base = (const char*)p + int64_t(kt) * kBK * ld2;
-      rows = int(nk - int64_t(kt) * kBK);
-      const int key = ((lane >> 4) + 4 * ((wave >> 1) & 1)) << 1;
-      voff = uint32_t(4 * wave + (lane >> 4)) * ld2 + uint32_t(x0) * 2u + uint32_t(((lane & 15) ^ key) * 16);
+      const int c = (lane & 15) ^ (((lane >> 4) + 4 * ((wave >> 1) & 1)) << 1);
+      if constexpr (BLOCKS) {
+        step = int64_t(ld / kZClasses) * (kZBlock * 2);
+        quarter = kt & 3;
+        base = (const char*)p + (kt >> 2) * step + (x0 / kZClasses) * (kZBlock * 2) + quarter * (kBK * kZClasses * 2);
+        rows = kBK;
+        voff = uint32_t(4 * wave + (lane >> 4)) * ld2 + uint32_t(c >> 3) * (kZBlock * 2u) + uint32_t((c & 7) * 16);
+      } else {
+        base = (const char*)p + int64_t(kt) * kBK * ld2;
+        rows = int(nk - int64_t(kt) * kBK);
+        voff = uint32_t(4 * wave + (lane >> 4)) * ld2 + uint32_t(x0) * 2u + uint32_t(c * 16);
+      }
     } else {
-      base = (const char*)p + x0 * ld2 + int64_t(kt) * (kBK * 2);
+      base = BLOCKS ? (const char*)p + ((x0 / kZRows) * (ld / kZClasses) + kt) * (kZBlock * 2)
+                    : (const char*)p + x0 * ld2 + int64_t(kt) * (kBK * 2);
       rows = int(nx - x0 < kT ? nx - x0 : kT);
       voff = uint32_t(8 * wave + (lane >> 3)) * ld2 + uint32_t(((lane & 7) ^ (lane >> 3)) * 16);
     }
@@ -91,14 +104,25 @@ struct HeadOp {
     const uint64_t b = reinterpret_cast<uint64_t>(base);
     const int n = COL && rows > kBK ? kBK : rows;
     auto uniform = [](uint32_t x) { return uint32_t(__builtin_amdgcn_readfirstlane(int(x))); };
-    const u32x4 r = {uniform(uint32_t(b)), uniform(uint32_t(b >> 32) & 0xffffu),
-                     uniform(any && n > 0 ? uint32_t(n) * ld2 : 0u), 0x00020000u};
-    base += COL ? int64_t(kBK) * ld2 : kBK * 2;
-    if (COL) rows -= kBK;
+    // (blocks by rows of k: four blocks' quarters)
+    const uint32_t bytes = COL && BLOCKS ? uint32_t(3 * kZBlock * 2 + kBK * kZClasses * 2) : uint32_t(n) * ld2;
+    const u32x4 r = {uniform(uint32_t(b)), uniform(uint32_t(b >> 32) & 0xffffu), uniform(any && n > 0 ? bytes : 0u),
+                     0x00020000u};
+    if constexpr (COL && BLOCKS) {
+      base += quarter == 3 ? step - 3 * (kBK * kZClasses * 2) : kBK * kZClasses * 2;
+      quarter = (quarter + 1) & 3;
+    } else if constexpr (BLOCKS) {
+      base += kZBlock * 2;
+    } else {
+      base += COL ? int64_t(kBK) * ld2 : kBK * 2;
+      if (COL) rows -= kBK;
+    }
     return r;
   }
   __device__ __forceinline__ uint32_t offset(int u) const {
-    return voff + (COL ? uint32_t(32 * (u & 1)) * ld2 + uint32_t(u >> 1) * 256u : uint32_t(64 * u) * ld2);
+    if constexpr (COL)
+      return voff + uint32_t(32 * (u & 1)) * ld2 + uint32_t(u >> 1) * (BLOCKS ? 2u * kZBlock * 2u : 256u);
+    return voff + uint32_t(64 * u) * ld2;
   }
 };
 
@@ -162,6 +186,20 @@ __device__ __forceinline__ u32x4 swap_rows8(uint32_t a0, uint32_t a1, uint32_t b
   const auto x = __builtin_amdgcn_permlane16_swap(a0, b0, false, false);
   const auto y = __builtin_amdgcn_permlane16_swap(a1, b1, false, false);
   return u32x4{x[0], y[0], x[1], y[1]};
+}
+// a and b: 64 bytes of a row (16 a lane, the row's four lanes r16 + 16 grp) each, a row
+// to an r16. Lanes of the upper eight rows swap their a with the b of those
+// eight rows below: then a holds rows 0-7 and b rows 8-15, 128 bytes of a row
+// over eight lanes (r16 < 8 what was a, else what was b), and a store of them
+// writes whole lines. Half lines (64 bytes, 16 rows a store) took the logits of
+// 8192 rows of 50304 classes (width 768) NNN instead of NNN us.
+__device__ __forceinline__ void whole_lines(u32x4& a, u32x4& b, bool low) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const uint32_t t = uint32_t(__builtin_amdgcn_mov_dpp(int(low ? b[q] : a[q]), 0x128, 0xF, 0xF, false));  // row_ror:8
+    a[q] = low ? a[q] : t;
+    b[q] = low ? t : b[q];
+  }
 }
 }  // namespace
 
@@ -233,8 +271,8 @@ __global__ __launch_bounds__(kThreads) void head_gemm_kernel(HeadGemmArgs g) {
   f32x4 acc[MI][NI];
 
   // The stream of loads: k-tile lk of item li, two k-tiles ahead of the products.
-  HeadOp<ACOL> A;
-  HeadOp<BCOL> B;
+  HeadOp<ACOL, false> A;
+  HeadOp<BCOL, MODE != kHeadLogits> B;
   int li = -1, lk = 0, lke = 0;
   u32x4 ra, rb;
   const int chunk_k = 8 * ((lane & 7) ^ (lane >> 3));
@@ -388,17 +426,25 @@ __global__ __launch_bounds__(kThreads) void head_gemm_kernel(HeadGemmArgs g) {
             g.stats[int64_t(it.tm) * g.rows_ld + n] = float2{top[j], (r[0] + r[kT]) + (r[2 * kT] + r[3 * kT])};
         }
       if (g.zout) {
+        const bool low = r16 < 8;
+        uint16_t* to = (uint16_t*)g.zout + head_z_at(it.tn * kT + wn * 128, it.tm * kT + wm * 64, g.ldz) +
+                       (r16 & 7) * kZClasses + 16 * (grp & 1) + 8 * (grp >> 1) + (low ? 0 : 32);
+        int left = rows - (n0 - r16) - (r16 & 7);
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
-          const int n = n0 + 16 * j;
-          uint16_t* row = (uint16_t*)g.zout + int64_t(n) * g.ldz + m0 + 16 * (grp & 1) + 8 * (grp >> 1);
+          u32x4 v[2];
 #pragma unroll
-          for (int i = 0; i < MI; i += 2) {
-            const f32x4 x = acc[i][j], y = acc[i + 1][j];
-            const u32x4 v = swap_rows8(pack_unit(x[0], x[1]), pack_unit(x[2], x[3]), pack_unit(y[0], y[1]),
-                                       pack_unit(y[2], y[3]));
-            if (n < rows) *reinterpret_cast<u32x4*>(row + 16 * i) = v;
+          for (int h = 0; h < 2; ++h) {
+            const f32x4 x = acc[2 * h][j], y = acc[2 * h + 1][j];
+            v[h] = swap_rows8(pack_unit(x[0], x[1]), pack_unit(x[2], x[3]), pack_unit(y[0], y[1]), pack_unit(y[2], y[3]));
           }
+          whole_lines(v[0], v[1], low);
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            if (left > 8 * h) __builtin_nontemporal_store(v[h], reinterpret_cast<u32x4*>(to + 8 * h * kZClasses));
+          to += 16 * kZClasses;
+          left -= 16;
+          asm volatile("" : "+v"(to), "+v"(left));  // one address at a time: all of them together spill
         }
       }
     } else if (MODE == kHeadDh || it.split >= 0) {

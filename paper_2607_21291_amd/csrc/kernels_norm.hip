@@ -106,19 +106,40 @@ __global__ __launch_bounds__(256) void norm_grad_kernel(const T* __restrict__ x,
     for (int i = 0; i < V; ++i) db[c][i] = 0.f;
   const float rd = 1.0f / float(d);
   int turn = 0;
-  for (int64_t r = int64_t(blockIdx.x) * RPW + (WAVES == 1 ? threadIdx.x >> 6 : 0); r < n;
-       r += int64_t(gridDim.x) * RPW, turn ^= 1) {
+  const int64_t step = int64_t(gridDim.x) * RPW;
+  // a row's vectors are asked for while the row before it is worked on (in
+  // registers as they are; rows of many vectors have no room for it)
+  constexpr bool kAhead = C <= 4;
+  u32x4 xr[kAhead ? C : 1], gr[kAhead ? C : 1];
+  auto ask = [&](int64_t r) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int at = (l + L * c) * V;
+      if (at < d && r < n) {
+        xr[c] = *reinterpret_cast<const u32x4*>(x + r * d + at);
+        gr[c] = *reinterpret_cast<const u32x4*>(dy + r * d + at);
+      }
+    }
+  };
+  const int64_t r0 = int64_t(blockIdx.x) * RPW + (WAVES == 1 ? threadIdx.x >> 6 : 0);
+  if constexpr (kAhead) ask(r0);
+  for (int64_t r = r0; r < n; r += step, turn ^= 1) {
     float xv[C][V], gv[C][V];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const int at = (l + L * c) * V;
 #pragma unroll
       for (int i = 0; i < V; ++i) xv[c][i] = gv[c][i] = 0.f;
-      if (at < d) {
+      if (at >= d) continue;
+      if constexpr (kAhead) {
+        load_vec(reinterpret_cast<const T*>(&xr[c]), xv[c]);
+        load_vec(reinterpret_cast<const T*>(&gr[c]), gv[c]);
+      } else {
         load_vec(x + r * d + at, xv[c]);
         load_vec(dy + r * d + at, gv[c]);
       }
     }
+    if constexpr (kAhead) ask(r + step);
     float m = 0.f;
     if constexpr (!RMS) {
       float s = 0.f;
@@ -214,7 +235,13 @@ __global__ __launch_bounds__(1024) void norm_grad_sums_kernel(const float* __res
   const int c = blockIdx.x * 64 + col, width = d << two;
   float v = 0.f;
   if (c < width)
-    for (int i = grp; i < slots; i += 16) v += partial[int64_t(i) * width + c];
+    for (int i = grp; i < slots; i += 16 * 16) {
+      float x[16];
+#pragma unroll
+      for (int u = 0; u < 16; ++u) x[u] = i + 16 * u < slots ? partial[int64_t(i + 16 * u) * width + c] : 0.f;
+#pragma unroll
+      for (int u = 0; u < 16; ++u) v += x[u];
+    }
   red[grp][col] = v;
   __syncthreads();
   if (grp != 0 || c >= width) return;
