@@ -585,24 +585,27 @@ def paged_attention(cache: PagedCache, batch: PagedBatch, q, out, window: int = 
 
 # ------------------------------------- the ends of a training step: embedding, norm, head
 
-def _dense(name: str, t, shape, dtypes, like):
-    """Pointer of a contiguous tensor of that shape, of one of the dtypes, on `like`'s device (None: null)."""
+def _dense(name: str, t, shape, dtype, index, other=None):
+    """Pointer of a contiguous tensor of that shape, of dtype (or `other`), on device `index` (None: null)."""
     if t is None:
         return None
-    if t.dtype not in dtypes:
-        raise ValueError(f"{name}: {' or '.join(str(d) for d in dtypes)} expected, got {t.dtype}")
-    if tuple(t.shape) != shape:
+    if t.dtype is dtype and t.is_contiguous() and t.get_device() == index and t.shape == shape:
+        return t.data_ptr()
+    if t.dtype not in (dtype, other):
+        raise ValueError(f"{name}: {dtype}{f' or {other}' if other else ''} expected, got {t.dtype}")
+    if t.shape != shape:
         raise ValueError(f"{name}: shape {list(shape)} expected, got {list(t.shape)}")
-    if t.get_device() != like.get_device():
-        raise ValueError(f"{name} lies on {t.device}, not on {like.device}")
+    if t.get_device() != index:
+        raise ValueError(f"{name} lies on {t.device}, the call's other tensors do not")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
 
 
-def _scratch(workspace, need: int, like, stream):
-    """Pointer, bytes and the tensor of a call's workspace: the caller's, or a new one."""
+def _scratch(workspace, size, like, stream):
+    """Pointer, bytes and the tensor of a call's workspace: the caller's, or a new one of size() bytes."""
     if workspace is None:
+        need = size()
         # on the stream that uses it, so that its memory is not handed on before that
         with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
             workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=like.device)
@@ -613,9 +616,8 @@ def _scratch(workspace, need: int, like, stream):
     return workspace.data_ptr(), workspace.nbytes, workspace
 
 
-def _call_on(name: str, like, stream, *args):
+def _call_on(name: str, like, index: int, stream, *args):
     """The C entry point `name` with the tensors' device current, on the given stream or that device's current one."""
-    index = like.get_device()
     if index < 0:
         raise ValueError(f"the tensors lie on {like.device}, not on a GPU")
     if stream is not None and stream.device.index != index:
@@ -630,19 +632,20 @@ def _call_on(name: str, like, stream, *args):
         _check(name, rc)
 
 
-_I32, _F32 = (torch.int32,), (torch.float32,)
+_I32, _F32 = torch.int32, torch.float32
+_CODES = {torch.float32: F32, torch.bfloat16: BF16}
 
 
 def embed_forward(tokens, table, out, scale: float = 1.0, stream=None):
     """out [..., d] = scale * table [n_classes, d] at tokens int32 [...]; zeros for tokens outside the table."""
-    dtype = _dtype_code(table)
-    if table.dim() != 2:
-        raise ValueError("table: [n_classes, d]")
-    V, d = table.shape
-    n = tokens.numel()
-    _call_on("dsf_embed_forward", table, stream, _dense("tokens", tokens, tuple(tokens.shape), _I32, table),
-             _dense("table", table, (V, d), (table.dtype,), table), dtype, n, V, d, float(scale),
-             _dense("out", out, (*tokens.shape, d), (table.dtype,), table))
+    t, shape, whole, at = table.dtype, tokens.shape, table.shape, table.get_device()
+    dtype = _CODES.get(t)
+    if len(whole) != 2 or dtype is None:
+        raise ValueError("table: [n_classes, d], float32 or bfloat16")
+    V, d = whole
+    _call_on("dsf_embed_forward", table, at, stream, _dense("tokens", tokens, shape, _I32, at),
+             _dense("table", table, whole, t, at), dtype, tokens.numel(), V, d, scale,
+             _dense("out", out, (*shape, d), t, at))
 
 
 def embed_backward_workspace_size(n_tokens: int, d: int, n_classes: int) -> int:
@@ -651,27 +654,28 @@ def embed_backward_workspace_size(n_tokens: int, d: int, n_classes: int) -> int:
 
 def embed_backward(tokens, dy, dtable, scale: float = 1.0, accumulate: bool = False, workspace=None, stream=None):
     """dtable [n_classes, d] (float32, or dy's dtype) = or += scale * the sums of dy [..., d] by token."""
-    dtype = _dtype_code(dy)
+    dtype, at = _dtype_code(dy), dy.get_device()
     if dtable.dim() != 2:
         raise ValueError("dtable: [n_classes, d]")
     V, d = dtable.shape
-    n = tokens.numel()
-    tp = _dense("tokens", tokens, tuple(tokens.shape), _I32, dy)
-    yp = _dense("dy", dy, (*tokens.shape, d), (dy.dtype,), dy)
-    gp = _dense("dtable", dtable, (V, d), (torch.float32, dy.dtype), dy)
-    wp, wb, keep = _scratch(workspace, embed_backward_workspace_size(n, d, V) if workspace is None else 0, dy, stream)
-    _call_on("dsf_embed_backward", dy, stream, tp, yp, dtype, n, V, d, float(scale), int(accumulate), gp,
+    n, shape = tokens.numel(), tokens.shape
+    tp, yp = _dense("tokens", tokens, shape, _I32, at), _dense("dy", dy, (*shape, d), dy.dtype, at)
+    gp = _dense("dtable", dtable, dtable.shape, dy.dtype, at, _F32)
+    wp, wb, keep = _scratch(workspace, lambda: embed_backward_workspace_size(n, d, V), dy, stream)
+    _call_on("dsf_embed_backward", dy, at, stream, tp, yp, dtype, n, V, d, scale, int(accumulate), gp,
              _dtype_code(dtable), wp, wb)
 
 
 def norm_forward(x, w, out, b=None, eps: float = 1e-5, rms: bool = False, stream=None):
     """out = LayerNorm (rms: RMSNorm) of x [..., d] with gain w [d] and bias b [d] or None. out may be x."""
-    dtype = _dtype_code(x)
-    d = x.shape[-1] if x.dim() else 0
+    t, at, shape = x.dtype, x.get_device(), x.shape
+    dtype = _CODES.get(t)
+    if dtype is None or not shape:
+        raise ValueError("x: [..., d], float32 or bfloat16")
+    d = shape[-1]
     n = x.numel() // d if d else 0
-    t = (x.dtype,)
-    _call_on("dsf_norm_forward", x, stream, _dense("x", x, tuple(x.shape), t, x), _dense("w", w, (d,), t, x),
-             _dense("b", b, (d,), t, x), dtype, n, d, float(eps), int(rms), _dense("out", out, tuple(x.shape), t, x))
+    _call_on("dsf_norm_forward", x, at, stream, _dense("x", x, shape, t, at), _dense("w", w, (d,), t, at),
+             _dense("b", b, (d,), t, at), dtype, n, d, eps, int(rms), _dense("out", out, shape, t, at))
 
 
 def norm_backward_workspace_size(n_rows: int, d: int) -> int:
@@ -681,17 +685,17 @@ def norm_backward_workspace_size(n_rows: int, d: int) -> int:
 def norm_backward(x, dy, w, dx, dw=None, db=None, add=None, eps: float = 1e-5, rms: bool = False, workspace=None,
                   stream=None):
     """dx [..., d] (or None) = add + the adjoint of norm_forward at dy; dw, db float32 [d] or None."""
-    dtype = _dtype_code(x)
-    d = x.shape[-1] if x.dim() else 0
+    dtype, at, shape = _dtype_code(x), x.get_device(), x.shape
+    d = shape[-1] if shape else 0
     n = x.numel() // d if d else 0
-    t, shape = (x.dtype,), tuple(x.shape)
-    ptrs = [_dense("x", x, shape, t, x), _dense("dy", dy, shape, t, x), _dense("w", w, (d,), t, x),
-            _dense("add", add, shape, t, x)]
-    outs = [_dense("dx", dx, shape, t, x), _dense("dw", dw, (d,), _F32, x), _dense("db", db, (d,), _F32, x)]
+    t = x.dtype
+    ptrs = [_dense("x", x, shape, t, at), _dense("dy", dy, shape, t, at), _dense("w", w, (d,), t, at),
+            _dense("add", add, shape, t, at)]
+    outs = [_dense("dx", dx, shape, t, at), _dense("dw", dw, (d,), _F32, at), _dense("db", db, (d,), _F32, at)]
     wp, wb, keep = None, 0, None
     if workspace is not None or dw is not None or db is not None:
-        wp, wb, keep = _scratch(workspace, norm_backward_workspace_size(n, d) if workspace is None else 0, x, stream)
-    _call_on("dsf_norm_backward", x, stream, *ptrs, dtype, n, d, float(eps), int(rms), *outs, wp, wb)
+        wp, wb, keep = _scratch(workspace, lambda: norm_backward_workspace_size(n, d), x, stream)
+    _call_on("dsf_norm_backward", x, at, stream, *ptrs, dtype, n, d, eps, int(rms), *outs, wp, wb)
 
 
 def head_workspace_size(dtype: int, n_rows: int, d: int, n_classes: int, top: int = 0, gradients: bool = True) -> int:
@@ -699,21 +703,21 @@ def head_workspace_size(dtype: int, n_rows: int, d: int, n_classes: int, top: in
 
 
 def _head(name: str, h, w, lists, middle, top, row_weight, row_loss, total, dh, dw, grad_scale, mean, workspace, stream):
-    dtype = _dtype_code(h)
+    dtype, at = _dtype_code(h), h.get_device()
     if h.dim() < 1 or w.dim() != 2:
         raise ValueError("h: [..., d], w: [n_classes, d]")
     V, d = w.shape
-    rows = tuple(h.shape[:-1])
+    rows = h.shape[:-1]
     n = h.numel() // d if d else 0
-    t = (h.dtype,)
-    hp, wp = _dense("h", h, (*rows, d), t, h), _dense("w", w, (V, d), t, h)
-    lp = [_dense(what, x, (*rows, *more), kind, h) for what, x, more, kind in lists]
-    rw, rl = _dense("row_weight", row_weight, rows, _F32, h), _dense("row_loss", row_loss, rows, _F32, h)
-    tp, dhp = _dense("total", total, (2,), _F32, h), _dense("dh", dh, (*rows, d), t, h)
-    dwp = _dense("dw", dw, (V, d), (torch.float32, h.dtype), h)
-    need = head_workspace_size(dtype, n, d, V, top, dh is not None or dw is not None) if workspace is None else 0
-    sp, sb, keep = _scratch(workspace, need, h, stream)
-    _call_on(name, h, stream, hp, wp, dtype, n, d, V, *lp, *middle, rw, float(grad_scale), int(mean), rl, tp, dhp, dwp,
+    t = h.dtype
+    hp, wp = _dense("h", h, (*rows, d), t, at), _dense("w", w, w.shape, t, at)
+    lp = [_dense(what, x, (*rows, *more), kind, at) for what, x, more, kind in lists]
+    rw, rl = _dense("row_weight", row_weight, rows, _F32, at), _dense("row_loss", row_loss, rows, _F32, at)
+    tp, dhp = _dense("total", total, (2,), _F32, at), _dense("dh", dh, h.shape, t, at)
+    dwp = _dense("dw", dw, w.shape, t, at, _F32)
+    grads = dh is not None or dw is not None
+    sp, sb, keep = _scratch(workspace, lambda: head_workspace_size(dtype, n, d, V, top, grads), h, stream)
+    _call_on(name, h, at, stream, hp, wp, dtype, n, d, V, *lp, *middle, rw, grad_scale, int(mean), rl, tp, dhp, dwp,
              _dtype_code(dw) if dw is not None else dtype, sp, sb)
 
 
@@ -732,7 +736,7 @@ def head_distill(h, w, top_classes, top_logits, temperature: float = 1.0, row_lo
     other numbers than classes are none. The rest as head_cross_entropy."""
     top = top_classes.shape[-1] if top_classes.dim() else 0
     _head("dsf_head_distill", h, w, [("top_classes", top_classes, (top,), _I32), ("top_logits", top_logits, (top,), _F32)],
-          (top, float(temperature)), top, row_weight, row_loss, total, dh, dw, grad_scale, mean, workspace, stream)
+          (top, temperature), top, row_weight, row_loss, total, dh, dw, grad_scale, mean, workspace, stream)
 
 
 def timing_enable(max_records: int, kinds: Optional[Sequence[str]] = None):

@@ -38,43 +38,58 @@ __device__ __forceinline__ double block_sum(double v, double* lds, int tid, int 
 
 // q[r][j], and plogp[r] = sum_j q_j log q_j; a row without an entry: live[r] = 0.
 // An entry counts if its class is in [0, V) and its logit is over -inf.
+// qsum[r][j]: the sum of the q of entry j's class where j is the first entry of
+// that class, -1 where it is not or its class is none. A wave to a row.
 __global__ __launch_bounds__(256) void head_teacher_kernel(const int32_t* __restrict__ top, const float* __restrict__ value,
                                                            int n, int k, int V, float c, float* __restrict__ q,
-                                                           float* __restrict__ plogp, int32_t* __restrict__ live) {
-  const int lane = threadIdx.x & 63, r = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (r >= n) return;
+                                                           float* __restrict__ qsum, float* __restrict__ plogp,
+                                                           int32_t* __restrict__ live) {
+  extern __shared__ float list[];  // k classes and k probabilities a wave
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = blockIdx.x * 4 + wave;
+  int32_t* cls = reinterpret_cast<int32_t*>(list) + wave * 2 * k;
+  float* prob = list + wave * 2 * k + k;
   const int64_t at = int64_t(r) * k;
-  auto logit = [&](int j) {
-    const float v = value[at + j];
-    return uint32_t(top[at + j]) < uint32_t(V) ? v * c : -INFINITY;
-  };
-  float m = -INFINITY;
+  float m = -INFINITY, sum = 0.f, h = 0.f;
   int any = 0;
-  for (int j = lane; j < k; j += 64) {
-    const float v = logit(j);
-    any |= !(v == -INFINITY);
-    m = fmaxf(m, v);
-  }
-  any = __any(any);
+  if (r < n) {
+    for (int j = lane; j < k; j += 64) {
+      const int t = top[at + j];
+      const float v = uint32_t(t) < uint32_t(V) ? value[at + j] * c : -INFINITY;
+      cls[j] = uint32_t(t) < uint32_t(V) ? t : -1;
+      prob[j] = v;
+      any |= !(v == -INFINITY);
+      m = fmaxf(m, v);
+    }
+    any = __any(any);
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-  float sum = 0.f;
-  for (int j = lane; j < k; j += 64) {
-    const float v = logit(j);
-    sum += v == -INFINITY ? 0.f : exp2f(v - m);
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    for (int j = lane; j < k; j += 64) sum += prob[j] == -INFINITY ? 0.f : exp2f(prob[j] - m);
+    sum = wave_sum(sum);
+    for (int j = lane; j < k; j += 64) {
+      const float v = prob[j];
+      const float p = v == -INFINITY ? 0.f : exp2f(v - m) / sum;
+      q[at + j] = p;
+      prob[j] = p;
+      if (!(p == 0.f)) h += p * ((v - m) - log2f(sum));
+    }
+    h = wave_sum(h);
+    if (lane == 0) {
+      plogp[r] = h * kLn2;
+      live[r] = any;
+    }
   }
-  sum = wave_sum(sum);
-  float h = 0.f;
+  __syncthreads();
+  if (r >= n) return;
   for (int j = lane; j < k; j += 64) {
-    const float v = logit(j);
-    const float p = v == -INFINITY ? 0.f : exp2f(v - m) / sum;
-    q[at + j] = p;
-    if (!(p == 0.f)) h += p * ((v - m) - log2f(sum));
-  }
-  h = wave_sum(h);
-  if (lane == 0) {
-    plogp[r] = h * kLn2;
-    live[r] = any;
+    const int t = cls[j];
+    float s = 0.f;
+    bool first = t >= 0;
+    for (int i = 0; i < k; ++i)
+      if (cls[i] == t) {
+        s += prob[i];
+        first = first && i >= j;
+      }
+    qsum[at + j] = first ? s : -1.f;
   }
 }
 
@@ -364,27 +379,21 @@ __global__ __launch_bounds__(1024) void head_lse_kernel(HeadLseArgs a) {
 struct HeadProbsArgs {
   void* z; int ldz;
   const float2* stats; int rows_ld;  // bf16: the tiles' maxima
-  const float* lse; const float* z2; const float* q;
+  const float* lse; const float* z2; const float* qsum;  // qsum null: cross entropy
   const float* weight; const int32_t* classes;
   const int32_t* act; const int32_t* n_active;
   int row0, rows, k, V, cuts, cols;  // cols: classes of a range, a multiple of 2048 (bf16: 256)
 };
-// The entry of list place j of slot s, if its class lies in [c0, c1).
+// The entry of list place j of slot s, if its class lies in [c0, c1) and is not named before.
 template <typename F>
 __device__ __forceinline__ void head_probs_entry(const HeadProbsArgs& a, int s, int j, int c0, int c1, F store) {
   const int g = a.row0 + s, row = a.act[g];
-  const int32_t* cls = a.classes + int64_t(row) * a.k;
-  const float* q = a.q ? a.q + int64_t(row) * a.k : nullptr;
-  const int c = cls[j];
+  const int64_t at = int64_t(row) * a.k + j;
+  const int c = a.classes[at];
   if (c < c0 || c >= std::min(c1, a.V)) return;
-  float sum = q ? q[j] : 1.f;
-  bool first = true;
-  for (int i = 0; i < a.k; ++i)
-    if (i != j && cls[i] == c) {
-      first = first && i > j;
-      sum += q ? q[i] : 1.f;
-    }
-  if (first) store(c, (a.weight ? a.weight[row] : 1.f) * (exp2f(a.z2[int64_t(g) * a.k + j] - a.lse[s]) - sum));
+  const float sum = a.qsum ? a.qsum[at] : 1.f;
+  if (sum == -1.f) return;
+  store(c, (a.weight ? a.weight[row] : 1.f) * (exp2f(a.z2[int64_t(g) * a.k + j] - a.lse[s]) - sum));
 }
 
 // bf16, in blocks: 32 rows, a thread to 16 bytes of a row of a block, then the
@@ -494,7 +503,7 @@ __global__ __launch_bounds__(256) void head_dh_kernel(const float* __restrict__ 
 namespace {
 struct HeadPlan {
   int ldz, rows, pieces, tiles, most, cuts, cols;
-  size_t splits, act, slot, live, scalars, q, plogp, z2, hc, lse, stats, partial, z, part, acc, total;
+  size_t splits, act, slot, live, scalars, q, qsum, plogp, z2, hc, lse, stats, partial, z, part, acc, total;
 };
 
 size_t up(size_t v) { return (v + 255) & ~size_t(255); }
@@ -537,6 +546,7 @@ HeadPlan head_plan(int dtype, int n, int d, int V, int k, bool grads) {
   p.live = take(size_t(n) * 4);
   p.plogp = take(size_t(n) * 4);
   p.q = take(size_t(n) * k * 4);
+  p.qsum = take(size_t(n) * k * 4);
   p.z2 = take(size_t(n) * std::max(k, 1) * 4);
   p.lse = take(size_t(p.rows) * 4);
   p.partial = take(size_t(p.pieces) * ((p.rows + kLseRows - 1) / kLseRows) * 8);
@@ -575,8 +585,9 @@ hipError_t launch_head_loss(const HeadLossArgs& a, hipStream_t s) {
   hipError_t e;
 #define DSF_TRY(x) do { if ((e = (x)) != hipSuccess) return e; } while (0)
   if (distill) {
-    head_teacher_kernel<<<(a.n + 3) / 4, 256, 0, s>>>(a.classes, a.value, a.n, k, a.V, z_scale, q, (float*)(ws + p.plogp),
-                                                      (int32_t*)(ws + p.live));
+    head_teacher_kernel<<<(a.n + 3) / 4, 256, 8 * k * sizeof(float), s>>>(a.classes, a.value, a.n, k, a.V, z_scale, q,
+                                                                          (float*)(ws + p.qsum), (float*)(ws + p.plogp),
+                                                                          (int32_t*)(ws + p.live));
     DSF_TRY(hipGetLastError());
   }
   int32_t* splits = (int32_t*)(ws + p.splits);
@@ -655,7 +666,7 @@ hipError_t launch_head_loss(const HeadLossArgs& a, hipStream_t s) {
     b.rows_ld = p.rows;
     b.lse = lse;
     b.z2 = z2;
-    b.q = q;
+    b.qsum = distill ? (const float*)(ws + p.qsum) : nullptr;
     b.weight = a.weight;
     b.classes = a.classes;
     b.act = act;

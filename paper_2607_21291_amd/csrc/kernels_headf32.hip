@@ -93,18 +93,27 @@ __global__ __launch_bounds__(256, 2) void head_f32_kernel(HeadGemmArgs g) {
     }
     const float* at = smem[s][0] + hi * kLD + wm * 64 + r32;
     const float* bt = smem[s][1] + hi * kLD + wn * 64 + r32;
-#pragma unroll
-    for (int k = 0; k < kBK; k += 2) {
-      float a[2], b[2];
+    // the fragments of two k are read while the two before them are multiplied
+    float af[2][2], bf[2][2];
+    auto read = [&](int set, int k) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        a[i] = at[k * kLD + 32 * i];
-        b[i] = bt[k * kLD + 32 * i];
+        af[set][i] = at[k * kLD + 32 * i];
+        bf[set][i] = bt[k * kLD + 32 * i];
       }
+    };
+    read(0, 0);
+#pragma unroll
+    for (int k = 0; k < kBK; k += 2) {
+      const int set = (k >> 1) & 1;
+      if (k + 2 < kBK) read(set ^ 1, k + 2);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[j], acc[i][j], 0, 0, 0);
+        for (int j = 0; j < 2; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(af[set][i], bf[set][j], acc[i][j], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
     }
     if (kt + 1 < ke) {  // the other stage was read before this iteration's barrier
       A.store(smem[s ^ 1][0], tid);

@@ -191,8 +191,10 @@ __device__ __forceinline__ u32x4 swap_rows8(uint32_t a0, uint32_t a1, uint32_t b
 // to an r16. Lanes of the upper eight rows swap their a with the b of those
 // eight rows below: then a holds rows 0-7 and b rows 8-15, 128 bytes of a row
 // over eight lanes (r16 < 8 what was a, else what was b), and a store of them
-// writes whole lines. Half lines (64 bytes, 16 rows a store) took the logits of
-// 8192 rows of 50304 classes (width 768) NNN instead of NNN us.
+// writes whole lines. They are written past the L2, which holds the operands: a
+// round of tiles, 4 MB an XCD, would push all of them out (8192 rows of width 768
+// over 50304 classes: logits 807 -> 638 us; dW of 256 rows of width 1536 over 151936
+// classes 195 -> 157 us; half lines 4 % slower).
 __device__ __forceinline__ void whole_lines(u32x4& a, u32x4& b, bool low) {
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
@@ -205,7 +207,8 @@ __device__ __forceinline__ void whole_lines(u32x4& a, u32x4& b, bool low) {
 
 // MODE 0: logits (A = W along k, B = h along k); 1: dh (A = W by rows of k, B = dz along k);
 // 2: dW (A = h by rows of k, B = dz by rows of k).
-template <int MODE>
+// HALF: the last tile of m is at most half full.
+template <int MODE, bool HALF>
 __global__ __launch_bounds__(kThreads) void head_gemm_kernel(HeadGemmArgs g) {
   constexpr bool ACOL = MODE != kHeadLogits, BCOL = MODE == kHeadDw;
   constexpr int MI = 4, NI = 8;
@@ -257,6 +260,8 @@ __global__ __launch_bounds__(kThreads) void head_gemm_kernel(HeadGemmArgs g) {
         it.split = MODE == kHeadDh ? share : -1;
       }
     }
+    // bands of four tile rows, column by column, share both operands in the L2s (row by
+    // row: dW of 4096 rows of width 3584 over 151936 classes 3597 us, so 3474)
     const GemmTile t = gemm_tile(tile, outer, inner, 4);
     it.tm = t.tn;
     it.tn = t.tm;  // out[n][m]: rows of the tile order are n
@@ -361,14 +366,31 @@ __global__ __launch_bounds__(kThreads) void head_gemm_kernel(HeadGemmArgs g) {
     // One k-tile. All its fragments are in registers by the middle, where the
     // barrier publishes the next k-tile and frees this one's stage. (Past the
     // stream's end zeros are loaded and read; nothing uses them.)
-    for (int kt = it.kb; kt < it.ke; ++kt) {
-      substep(std::integral_constant<int, 0>(), 1, 0, 0);
+    auto middle = [&]() DSF_INLINE {
       const uint32_t past = start();
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
       fa.at ^= kStage;
       fb.at ^= kStage;
-      substep(std::integral_constant<int, 1>(), 0, cur, past);
-      cur ^= kStage;
+      return past;
+    };
+    if (!HALF || it.tm * kT + wm * 64 < g.d) {
+      for (int kt = it.kb; kt < it.ke; ++kt) {
+        substep(std::integral_constant<int, 0>(), 1, 0, 0);
+        const uint32_t past = middle();
+        substep(std::integral_constant<int, 1>(), 0, cur, past);
+        cur ^= kStage;
+      }
+    } else {
+      // No column for this wave, one of a SIMD's two: its loads alone, and the next
+      // item's first fragments.
+      for (int kt = it.kb; kt < it.ke; ++kt) {
+        const uint32_t past = middle();
+#pragma unroll
+        for (int u = 0; u < 4; ++u) issue(cur, u, past);
+        cur ^= kStage;
+      }
+#pragma unroll
+      for (int n = 0; n < R; ++n) read_n(0, 0, n);
     }
     // lane holds out[n = 16 j + r16][m = 16 i + 4 grp + e] of its wave's part
     const int m0 = it.tm * kT + wm * 64, n0 = it.tn * kT + wn * 128 + r16;
@@ -460,11 +482,13 @@ __global__ __launch_bounds__(kThreads) void head_gemm_kernel(HeadGemmArgs g) {
             *reinterpret_cast<f32x4*>(out + int64_t(16 * j) * ld + 16 * i + 4 * grp) = acc[i][j];
     } else {
       const float scale = *g.scale;
+      const bool low = r16 < 8;
 #pragma unroll
       for (int j = 0; j < NI; ++j) {
         const int n = n0 + 16 * j;
         const bool in = n < g.V;
         const int64_t row = int64_t(n) * g.d;
+        u32x4 v16[2];
 #pragma unroll
         for (int i = 0; i < MI; i += 2) {
           f32x4 v[2];
@@ -473,18 +497,24 @@ __global__ __launch_bounds__(kThreads) void head_gemm_kernel(HeadGemmArgs g) {
             const int m = m0 + 16 * (i + ii) + 4 * grp;
             v[ii] = acc[i + ii][j] * scale;
             if (g.prev && in && m < g.d) v[ii] += *reinterpret_cast<const f32x4*>(g.prev + row + m);
-            if (g.out32 && in && m < g.d) *reinterpret_cast<f32x4*>(g.out32 + row + m) = v[ii];
+            if (g.out32 && in && m < g.d) __builtin_nontemporal_store(v[ii], reinterpret_cast<f32x4*>(g.out32 + row + m));
           }
-          if (!g.out16) continue;
           uint32_t pk[2][2];
 #pragma unroll
           for (int ii = 0; ii < 2; ++ii)
 #pragma unroll
             for (int q = 0; q < 2; ++q)
               pk[ii][q] = uint32_t(f2bf(v[ii][2 * q])) | uint32_t(f2bf(v[ii][2 * q + 1])) << 16;
-          const u32x4 u = swap_rows8(pk[0][0], pk[0][1], pk[1][0], pk[1][1]);
-          const int m = m0 + 16 * (i + (grp & 1)) + 8 * (grp >> 1);
-          if (in && m < g.d) *reinterpret_cast<u32x4*>(g.out16 + row + m) = u;
+          v16[i >> 1] = swap_rows8(pk[0][0], pk[0][1], pk[1][0], pk[1][1]);
+        }
+        if (!g.out16) continue;
+        whole_lines(v16[0], v16[1], low);
+        const int m = m0 + 16 * (grp & 1) + 8 * (grp >> 1) + (low ? 0 : 32);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int to = n - r16 + 8 * h + (r16 & 7);
+          if (to < g.V && m < g.d) __builtin_nontemporal_store(v16[h], reinterpret_cast<u32x4*>(g.out16 + int64_t(to) * g.d + m));
+          __builtin_amdgcn_sched_barrier(0);  // one address after another
         }
       }
     }
@@ -533,12 +563,16 @@ hipError_t launch_head_gemm(int mode, const HeadGemmArgs& g, hipStream_t s) {
   const int64_t tr = (g.rows + kT - 1) / kT, tv = (g.V + kT - 1) / kT, td = (g.d + kT - 1) / kT;
   auto grid = [](int64_t items) { return dim3(uint32_t(std::min<int64_t>(kHeadGrid, (items + kXcds - 1) / kXcds * kXcds))); };
   if (mode == kHeadLogits) {
-    head_gemm_kernel<kHeadLogits><<<grid(tr * tv), kThreads, 0, s>>>(g);
+    head_gemm_kernel<kHeadLogits, false><<<grid(tr * tv), kThreads, 0, s>>>(g);
   } else if (mode == kHeadDh) {
-    head_gemm_kernel<kHeadDh><<<kHeadGrid, kThreads, 0, s>>>(g);
+    head_gemm_kernel<kHeadDh, false><<<kHeadGrid, kThreads, 0, s>>>(g);
   } else {
     const int nt = int(tv * td), left = nt % kHeadGrid;
-    head_gemm_kernel<kHeadDw><<<kHeadGrid, kThreads, 0, s>>>(g);
+    // Leaving out the products past a width like 896 takes registers, 3 % of whole tiles' time, and
+    // is worth it where a workgroup has some of either kind (6554 rows, 151936 classes: dW 1648 ->
+    // 1560 us; dh, whose workgroups have few, gains nothing).
+    if ((g.d - 1) % kT < kT / 2) head_gemm_kernel<kHeadDw, true><<<kHeadGrid, kThreads, 0, s>>>(g);
+    else head_gemm_kernel<kHeadDw, false><<<kHeadGrid, kThreads, 0, s>>>(g);
     if (left && 2 * left <= kHeadGrid) head_dw_join_kernel<<<left * 8, 256, 0, s>>>(g, kHeadGrid);
   }
   return hipGetLastError();
