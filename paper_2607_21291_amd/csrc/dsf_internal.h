@@ -356,6 +356,14 @@ struct PagedAttnArgs {
 size_t paged_attention_workspace_bytes(int dtype, int Hq, const PagedPool& pool, const PagedBatch& pb);
 hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t s);
 
+// Grids of any number of workgroups: one dimension holds less than 2^32 work items.
+// Kernels count them with wide_index() and end past their last one.
+inline dim3 wide_grid(int64_t workgroups) {
+  constexpr int64_t kRow = 1 << 20;
+  return workgroups <= kRow ? dim3(uint32_t(workgroups)) : dim3(uint32_t(kRow), uint32_t((workgroups + kRow - 1) / kRow));
+}
+__device__ __forceinline__ int64_t wide_index() { return int64_t(blockIdx.y) * gridDim.x + blockIdx.x; }
+
 // ---- embedding (kernels_embed.hip) ----
 hipError_t launch_embed(int dtype, const int32_t* tokens, const void* table, int n, int V, int d, float scale, void* out,
                         hipStream_t s);

@@ -27,7 +27,7 @@ __global__ __launch_bounds__(256) void embed_kernel(const int32_t* __restrict__ 
                                                     int n, int V, int d, float scale, T* __restrict__ out) {
   constexpr int VEC = Elem<T>::kVec;
   const uint32_t nv = uint32_t(d) / VEC;
-  const int64_t base = int64_t(blockIdx.x) * 1024, all = int64_t(n) * nv;
+  const int64_t base = wide_index() * 1024, all = int64_t(n) * nv;
   const int64_t row0 = base / nv;
   const uint32_t rem = uint32_t(base - row0 * nv);
   u32x4 raw[4];
@@ -223,8 +223,9 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedSumArgs a) {
   const TI* dy = (const TI*)a.dy;
   TO* out = (TO*)a.out;
   const int n = a.start[a.V];  // positions that have a token
-  if (int(blockIdx.x) < a.long_wgs) {
-    const int task = int(blockIdx.x) * 4 + wave, piece = task / a.slabs, c = (task - piece * a.slabs) * kSlab + lane * 8;
+  const int64_t wg = wide_index();
+  if (wg < a.long_wgs) {
+    const int task = int(wg) * 4 + wave, piece = task / a.slabs, c = (task - piece * a.slabs) * kSlab + lane * 8;
     const int i0 = piece * kLong;
     if (i0 >= n) return;
     const int m = std::min(kLong, n - i0);
@@ -243,9 +244,9 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedSumArgs a) {
     }
     return;
   }
-  const int64_t task = (int64_t(blockIdx.x) - a.long_wgs) * 4 + wave;
+  const int64_t task = (wg - a.long_wgs) * 4 + wave;
+  if (task >= int64_t(n) * a.slabs) return;
   const int i = int(task / a.slabs), c = int(task - int64_t(i) * a.slabs) * kSlab + lane * 8;
-  if (i >= n) return;
   const int t = a.tokens[a.order[i]];
   const int m = a.start[t + 1] - i;
   if (a.start[t] != i || m > kLong) return;
@@ -260,7 +261,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedSumArgs a) {
 template <typename TO>
 __global__ __launch_bounds__(256) void embed_join_kernel(EmbedSumArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6));
-  const int task = int(blockIdx.x) * 4 + wave, piece = task / a.slabs;
+  const int task = int(wide_index()) * 4 + wave, piece = task / a.slabs;
   const int c = (task - piece * a.slabs) * kSlab + lane * 8;
   const int n = a.start[a.V], i0 = piece * kLong;
   if (i0 >= n) return;
@@ -292,7 +293,7 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedSumArgs a) {
 hipError_t launch_embed(int dtype, const int32_t* tokens, const void* table, int n, int V, int d, float scale, void* out,
                         hipStream_t s) {
   const int64_t nv = int64_t(n) * d / (dtype == DSF_F32 ? 4 : 8);
-  const dim3 grid(uint32_t((nv + 1023) / 1024));
+  const dim3 grid = wide_grid((nv + 1023) / 1024);
   if (dtype == DSF_F32)
     embed_kernel<float><<<grid, 256, 0, s>>>(tokens, (const float*)table, n, V, d, scale, (float*)out);
   else
@@ -329,7 +330,7 @@ hipError_t launch_embed_backward(const EmbedBackwardArgs& b, hipStream_t s) {
   const int row_vecs = b.d * (b.dtable_type == DSF_F32 ? 4 : 2) / 16;
   embed_order_kernel<<<(b.V + kRange - 1) / kRange, 64 * kWaves, 0, s>>>(b.tokens, b.n, b.V, order, start,
                                                                          b.accumulate ? nullptr : (u32x4*)b.dtable, row_vecs);
-  const dim3 grid(uint32_t(a.long_wgs + (int64_t(b.n) * a.slabs + 3) / 4));
+  const dim3 grid = wide_grid(a.long_wgs + (int64_t(b.n) * a.slabs + 3) / 4);
   const bool in32 = b.dtype == DSF_F32, out32 = b.dtable_type == DSF_F32;
   if (grid.x) {
     if (in32) embed_sum_kernel<float, float><<<grid, 256, 0, s>>>(a);
@@ -337,8 +338,8 @@ hipError_t launch_embed_backward(const EmbedBackwardArgs& b, hipStream_t s) {
     else embed_sum_kernel<uint16_t, uint16_t><<<grid, 256, 0, s>>>(a);
   }
   if (a.long_wgs) {
-    if (out32) embed_join_kernel<float><<<a.long_wgs, 256, 0, s>>>(a);
-    else embed_join_kernel<uint16_t><<<a.long_wgs, 256, 0, s>>>(a);
+    if (out32) embed_join_kernel<float><<<wide_grid(a.long_wgs), 256, 0, s>>>(a);
+    else embed_join_kernel<uint16_t><<<wide_grid(a.long_wgs), 256, 0, s>>>(a);
   }
   return hipGetLastError();
 }

@@ -216,9 +216,9 @@ __global__ __launch_bounds__(256) void head_gather_kernel(const T* __restrict__ 
   constexpr int VEC = Elem<T>::kVec;
   const int lane = threadIdx.x & 63;
   const int groups = (k + kDots - 1) / kDots;
-  const int64_t task = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  const int64_t task = wide_index() * 4 + (threadIdx.x >> 6);
+  if (task >= int64_t(*n_active) * groups) return;
   const int s = int(task / groups), g = int(task - int64_t(s) * groups);
-  if (s >= *n_active) return;
   const int row = act[s];
   const T* src = h + int64_t(row) * d;
   const T* wr[kDots];
@@ -597,7 +597,7 @@ hipError_t launch_head_loss(const HeadLossArgs& a, hipStream_t s) {
   head_rows_kernel<<<1, 1024, 0, s>>>(r);
   DSF_TRY(hipGetLastError());
   const int64_t tasks = int64_t(a.n) * ((k + kDots - 1) / kDots);
-  const dim3 gg(uint32_t((tasks + 3) / 4));
+  const dim3 gg = wide_grid((tasks + 3) / 4);
   if (f32)
     head_gather_kernel<float><<<gg, 256, 0, s>>>((const float*)a.h, (const float*)a.w, a.classes, k, a.V, a.d, act,
                                                  n_active, z_scale, (float*)(ws + p.hc), z2);

@@ -1,7 +1,8 @@
 // The head's three products in fp32, on the fp32 matrix cores: the forms of
 // kernels_headgemm.hip on 128 x 128 tiles of four waves (64 x 64 each,
-// v_mfma_f32_32x32x2_f32), 32 of k in an LDS stage [k][x], whatever way an
-// operand lies in memory; the next stage's values wait in registers. Logits are
+// v_mfma_f32_32x32x2_f32), 16 of k in an LDS stage [k][x], whatever way an
+// operand lies in memory; the next stage's values wait in registers, and four
+// workgroups to a CU cover each other's barriers. Logits are
 // stored as they are (in units of log 2), their statistics are a pass of their
 // own (kernels_head.hip).
 #include "dsf_device.h"
@@ -10,8 +11,12 @@
 namespace dsf {
 
 namespace {
-constexpr int kT = 128, kBK = 32, kLD = 132;
+constexpr int kT = 128, kBK = 16;
 constexpr int kVecs = kT * kBK / 4 / 256;  // 16-byte vectors of an operand a thread brings
+
+// Value (x, k) of a stage. Odd k have the halves of their 64 banks swapped: a read's two k
+// then cover all banks.
+__device__ __forceinline__ int f32_at(int x, int k) { return k * kT + (x ^ ((k & 1) << 5)); }
 
 // COL false: element (x, k) at p[x ld + k]; COL true: at p[k ld + x]. Outside
 // [0, nx) x [0, nk) zeros (nx, nk, ld multiples of 4 on the contiguous side).
@@ -21,7 +26,7 @@ struct F32Op {
   int64_t ld;
   int nx, nk;
   f32x4 r[kVecs];
-  // values of k0 .. k0 + 31, x0 .. x0 + 127
+  // values of k0 .. k0 + 15, x0 .. x0 + 127
   __device__ __forceinline__ void load(int64_t x0, int k0, int tid) {
 #pragma unroll
     for (int u = 0; u < kVecs; ++u) {
@@ -35,10 +40,10 @@ struct F32Op {
 #pragma unroll
     for (int u = 0; u < kVecs; ++u) {
       if constexpr (COL) {
-        *reinterpret_cast<f32x4*>(lds + ((tid >> 5) + 8 * u) * kLD + 4 * (tid & 31)) = r[u];
+        *reinterpret_cast<f32x4*>(lds + f32_at(4 * (tid & 31), (tid >> 5) + 8 * u)) = r[u];
       } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) lds[(4 * (tid >> 6) + 16 * (u >> 1) + i) * kLD + (tid & 63) + 64 * (u & 1)] = r[u][i];
+        for (int i = 0; i < 4; ++i) lds[f32_at((tid & 63) + 64 * (u & 1), 4 * (tid >> 6) + 16 * (u >> 1) + i)] = r[u][i];
       }
     }
   }
@@ -46,9 +51,9 @@ struct F32Op {
 }  // namespace
 
 template <int MODE>
-__global__ __launch_bounds__(256, 2) void head_f32_kernel(HeadGemmArgs g) {
+__global__ __launch_bounds__(256, 4) void head_f32_kernel(HeadGemmArgs g) {
   constexpr bool ACOL = MODE != kHeadLogits, BCOL = MODE == kHeadDw;
-  __shared__ __attribute__((aligned(16))) float smem[2][2][kBK * kLD];
+  __shared__ __attribute__((aligned(16))) float smem[2][2][kBK * kT];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wm = wave >> 1, wn = wave & 1, r32 = lane & 31, hi = lane >> 5;
   int rows = *g.n_active - g.row0;
@@ -91,15 +96,15 @@ __global__ __launch_bounds__(256, 2) void head_f32_kernel(HeadGemmArgs g) {
       A.load(xm, (kt + 1) * kBK, tid);
       B.load(xn, (kt + 1) * kBK, tid);
     }
-    const float* at = smem[s][0] + hi * kLD + wm * 64 + r32;
-    const float* bt = smem[s][1] + hi * kLD + wn * 64 + r32;
+    const float* at[2] = {smem[s][0] + f32_at(wm * 64 + r32, hi), smem[s][0] + f32_at(wm * 64 + 32 + r32, hi)};
+    const float* bt[2] = {smem[s][1] + f32_at(wn * 64 + r32, hi), smem[s][1] + f32_at(wn * 64 + 32 + r32, hi)};
     // the fragments of two k are read while the two before them are multiplied
     float af[2][2], bf[2][2];
     auto read = [&](int set, int k) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        af[set][i] = at[k * kLD + 32 * i];
-        bf[set][i] = bt[k * kLD + 32 * i];
+        af[set][i] = at[i][k * kT];
+        bf[set][i] = bt[i][k * kT];
       }
     };
     read(0, 0);
