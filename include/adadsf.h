@@ -707,8 +707,8 @@ int dsf_norm_backward(const void* x, const void* dy, const void* w, const void* 
 /* Workspace bytes of the head's losses: top = 0 for dsf_head_cross_entropy, the
  * entries of a row for dsf_head_distill; gradients != 0 if dh or dw are wanted
  * (also enough for calls without). It holds 16 bits (fp32: 32) for each logit of
- * as many rows as fit 4 GiB, and for calls of more rows than that the sum of dw
- * in fp32; never the logits of a call at once. 0 on a bad argument. */
+ * as many rows as fit 4 GiB (calls of more take them in pieces), and for
+ * calls of several pieces the sum of dw in fp32. 0 on a bad argument. */
 size_t dsf_head_workspace_size(int dtype, int64_t n_rows, int d, int n_classes, int top, int gradients);
 
 /* Cross entropy of a linear head. For rows h[i] and logits z_i = h[i] W^T over
@@ -725,7 +725,8 @@ size_t dsf_head_workspace_size(int dtype, int64_t n_rows, int d, int n_classes, 
  * d] of type dw_type: DSF_F32, or dtype. All are overwritten. With mean and
  * weights that sum to 0 the gradients are 0.
  * bf16: the products' operands are bf16; of the gradient at the logits,
- * weight (p - q), that is the one rounding (2^-8) but for a relative 2^-11 of p.
+ * weight (p - q), that is the one rounding (2^-8) but for a relative 2^-11 of p,
+ * and p below 2^-64 of the greatest among 256 neighbouring classes, which is 0.
  * Logits, log-sums and accumulation are fp32, total is summed in 64 bits.
  * d a multiple of 8, at most 16384; n_classes at most 2^21, n_rows at most 2^24.
  * Equal calls give equal bits. Workspace (256-byte aligned) as above. */
@@ -744,7 +745,8 @@ int dsf_head_cross_entropy(const void* h, const void* w, int dtype, int64_t n_ro
  * with both entries. A row without entries, or of weight 0, takes no part. L,
  * the outputs and the other arguments are dsf_head_cross_entropy's.
  * top_classes int32, top_logits float, [n_rows, top], top from 1 to 1024;
- * temperature positive and finite. */
+ * temperature from 1e-6 to 1e6 (a loss, a difference of terms in fp32, is off by
+ * some 1e-6 temperature^2). */
 int dsf_head_distill(const void* h, const void* w, int dtype, int64_t n_rows, int d, int n_classes,
                      const int32_t* top_classes, const float* top_logits, int top, float temperature,
                      const float* row_weight, float grad_scale, int mean, float* row_loss, float* total, void* dh,

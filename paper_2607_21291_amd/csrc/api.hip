@@ -1891,7 +1891,7 @@ extern "C" int dsf_norm_backward(const void* x, const void* dy, const void* w, c
   if (rc) return rc;
   rc = check_norm(n_rows, d, eps);
   if (rc) return rc;
-  DSF_CHECK(dx || dw || db, DSF_EINVAL, "no output");
+  DSF_CHECK(n_rows == 0 || dx || dw || db, DSF_EINVAL, "no output");
   DSF_CHECK(!(rms && db), DSF_EINVAL, "an RMSNorm has no bias: db must be null");
   DSF_CHECK(n_rows == 0 || (x && dy && w), DSF_EINVAL, "null pointer");
   DSF_CHECK(aligned16(x) && aligned16(dy) && aligned16(w) && aligned16(add) && aligned16(dx) && aligned16(dw) &&
@@ -1939,7 +1939,7 @@ static int head_loss(const HeadLossArgs& a, int64_t n_rows, int dw_type, size_t 
   DSF_CHECK(((uintptr_t(a.classes) | uintptr_t(a.value) | uintptr_t(a.weight) | uintptr_t(a.row_loss) |
               uintptr_t(a.total)) & 3u) == 0,
             DSF_EINVAL, "targets, weights and losses must be 4-byte aligned");
-  DSF_CHECK(a.row_loss || a.total || a.dh || a.dw, DSF_EINVAL, "no output");
+  DSF_CHECK(n_rows == 0 || a.row_loss || a.total || a.dh || a.dw, DSF_EINVAL, "no output");
   const size_t need = n_rows == 0 ? 0 : head_workspace_bytes(a.dtype, a.n, a.d, a.V, a.value ? a.k : 0, a.dh || a.dw);
   rc = check_workspace(a.workspace, workspace_bytes, need);
   if (rc) return rc;
@@ -1975,7 +1975,7 @@ extern "C" int dsf_head_distill(const void* h, const void* w, int dtype, int64_t
   int rc = check_head(dtype, n_rows, d, n_classes, top);
   if (rc) return rc;
   DSF_CHECK(top >= 1, DSF_EINVAL, "top must be at least 1");
-  DSF_CHECK(temperature > 0.f && std::isfinite(temperature), DSF_EINVAL, "temperature must be positive and finite");
+  DSF_CHECK(temperature >= 1e-6f && temperature <= 1e6f, DSF_EINVAL, "temperature must be from 1e-6 to 1e6");
   DSF_CHECK(n_rows == 0 || top_logits, DSF_EINVAL, "null pointer");
   static const float none = 0.f;
   const HeadLossArgs a{dtype, h, w, int(n_rows), d, n_classes, top_classes, n_rows ? top_logits : &none, top, temperature,

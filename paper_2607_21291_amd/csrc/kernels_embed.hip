@@ -70,7 +70,8 @@ __global__ __launch_bounds__(64 * kWaves) void embed_order_kernel(const int32_t*
   __shared__ int part[kWaves];
   __shared__ uint64_t absent[kRange / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t lo = int64_t(blockIdx.x) * kRange;
+  const int64_t lo = wide_index() * kRange;
+  if (lo >= V) return;
   const int size = int(std::min<int64_t>(kRange, V - lo));
   const int seg = ((n + kWaves - 1) / kWaves + 63) / 64 * 64;
   const int b = std::min(int64_t(n), int64_t(wave) * seg), e = std::min(int64_t(n), int64_t(b) + seg);
@@ -328,8 +329,8 @@ hipError_t launch_embed_backward(const EmbedBackwardArgs& b, hipStream_t s) {
   const int64_t tasks = b.n > kLong ? int64_t((b.n + kLong - 1) / kLong) * a.slabs : 0;
   a.long_wgs = int((tasks + 3) / 4);
   const int row_vecs = b.d * (b.dtable_type == DSF_F32 ? 4 : 2) / 16;
-  embed_order_kernel<<<(b.V + kRange - 1) / kRange, 64 * kWaves, 0, s>>>(b.tokens, b.n, b.V, order, start,
-                                                                         b.accumulate ? nullptr : (u32x4*)b.dtable, row_vecs);
+  embed_order_kernel<<<wide_grid((int64_t(b.V) + kRange - 1) / kRange), 64 * kWaves, 0, s>>>(
+      b.tokens, b.n, b.V, order, start, b.accumulate ? nullptr : (u32x4*)b.dtable, row_vecs);
   const dim3 grid = wide_grid(a.long_wgs + (int64_t(b.n) * a.slabs + 3) / 4);
   const bool in32 = b.dtype == DSF_F32, out32 = b.dtable_type == DSF_F32;
   if (grid.x) {

@@ -37,7 +37,9 @@ __device__ __forceinline__ double block_sum(double v, double* lds, int tid, int 
 }  // namespace
 
 // q[r][j], and plogp[r] = sum_j q_j log q_j; a row without an entry: live[r] = 0.
-// An entry counts if its class is in [0, V) and its logit is over -inf.
+// An entry counts if its class is in [0, V) and its logit is over -inf; c is
+// log2(e) / T (for differences of logits: the lowest finite one, which masks
+// use, times c would be -inf).
 // qsum[r][j]: the sum of the q of entry j's class where j is the first entry of
 // that class, -1 where it is not or its class is none. A wave to a row.
 __global__ __launch_bounds__(256) void head_teacher_kernel(const int32_t* __restrict__ top, const float* __restrict__ value,
@@ -54,7 +56,7 @@ __global__ __launch_bounds__(256) void head_teacher_kernel(const int32_t* __rest
   if (r < n) {
     for (int j = lane; j < k; j += 64) {
       const int t = top[at + j];
-      const float v = uint32_t(t) < uint32_t(V) ? value[at + j] * c : -INFINITY;
+      const float v = uint32_t(t) < uint32_t(V) ? value[at + j] : -INFINITY;
       cls[j] = uint32_t(t) < uint32_t(V) ? t : -1;
       prob[j] = v;
       any |= !(v == -INFINITY);
@@ -63,14 +65,14 @@ __global__ __launch_bounds__(256) void head_teacher_kernel(const int32_t* __rest
     any = __any(any);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-    for (int j = lane; j < k; j += 64) sum += prob[j] == -INFINITY ? 0.f : exp2f(prob[j] - m);
+    for (int j = lane; j < k; j += 64) sum += prob[j] == -INFINITY ? 0.f : exp2f((prob[j] - m) * c);
     sum = wave_sum(sum);
     for (int j = lane; j < k; j += 64) {
       const float v = prob[j];
-      const float p = v == -INFINITY ? 0.f : exp2f(v - m) / sum;
+      const float p = v == -INFINITY ? 0.f : exp2f((v - m) * c) / sum;
       q[at + j] = p;
       prob[j] = p;
-      if (!(p == 0.f)) h += p * ((v - m) - log2f(sum));
+      if (!(p == 0.f)) h += p * ((v - m) * c - log2f(sum));
     }
     h = wave_sum(h);
     if (lane == 0) {
@@ -435,7 +437,7 @@ __global__ __launch_bounds__(256) void head_probs_kernel(HeadProbsArgs a) {
       p[u * kStep] = raw[u];
     }
   }
-  __syncthreads();  // (with it the stores above have completed)
+  __syncthreads();  // (the stores below come after those above)
   for (int i = threadIdx.x; i < kProbsRows * a.k; i += 256) {
     const int si = s0 + i / a.k;
     if (si < rows)

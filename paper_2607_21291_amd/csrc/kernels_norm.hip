@@ -44,11 +44,10 @@ __device__ __forceinline__ void put_vec(T* p, const float* v, bool past) {
 }
 }  // namespace
 
-// C vectors of 16 bytes a lane. WAVES 1: four rows a workgroup; 4: one.
+// C vectors of 16 bytes a lane. WAVES 1: four rows a workgroup; 4: one. out may be x.
 template <typename T, int C, int WAVES, bool RMS>
-__global__ __launch_bounds__(256) void norm_rows_kernel(const T* __restrict__ x, const T* __restrict__ w,
-                                                        const T* __restrict__ b, int64_t n, int d, float eps,
-                                                        T* __restrict__ out) {
+__global__ __launch_bounds__(256) void norm_rows_kernel(const T* x, const T* __restrict__ w, const T* __restrict__ b,
+                                                        int64_t n, int d, float eps, T* out) {
   constexpr int V = Elem<T>::kVec, L = 64 * WAVES;
   __shared__ float red[2][4];
   const int l = WAVES == 1 ? int(threadIdx.x & 63) : int(threadIdx.x);
@@ -96,12 +95,11 @@ __global__ __launch_bounds__(256) void norm_rows_kernel(const T* __restrict__ x,
   }
 }
 
-// SUMS: also partial[workgroup][0] = sum dy xh, [1] = sum dy over its rows.
+// SUMS: also partial[workgroup][0] = sum dy xh, [1] = sum dy over its rows. dx may be dy or add.
 template <typename T, int C, int WAVES, bool RMS, bool SUMS>
-__global__ __launch_bounds__(256) void norm_grad_kernel(const T* __restrict__ x, const T* __restrict__ dy,
-                                                        const T* __restrict__ w, const T* __restrict__ add, int64_t n,
-                                                        int d, float eps, T* __restrict__ dx,
-                                                        float* __restrict__ partial) {
+__global__ __launch_bounds__(256) void norm_grad_kernel(const T* __restrict__ x, const T* dy,
+                                                        const T* __restrict__ w, const T* add, int64_t n, int d,
+                                                        float eps, T* dx, float* __restrict__ partial) {
   constexpr int V = Elem<T>::kVec, L = 64 * WAVES, RPW = 4 / WAVES;  // rows of a workgroup at a time
   __shared__ float red[2][4][4];
   const int l = WAVES == 1 ? int(threadIdx.x & 63) : int(threadIdx.x);
@@ -236,8 +234,8 @@ __global__ __launch_bounds__(256) void norm_grad_kernel(const T* __restrict__ x,
   }
 }
 
-// dw[c] (and db[c]) = sum over the partial sums: 16 columns of a workgroup, 16
-// threads to a column's partial sums.
+// dw[c] (and db[c]) = sum over the partial sums: 64 columns of a workgroup, a
+// column's partial sums in 16 groups, then the groups in order.
 __global__ __launch_bounds__(1024) void norm_grad_sums_kernel(const float* __restrict__ partial, int slots, int d, int two,
                                                               float* __restrict__ dw, float* __restrict__ db) {
   __shared__ float red[16][64];

@@ -64,7 +64,7 @@ BAD = {
           (dict(kind=P.BF16, dtype=P.F32), 2), (dict(loss=None, total=None, dh=None, dw=None), 1), (dict(ws=None), 3),
           (dict(ws=FAKE + 128), 1), (dict(nbytes=4096), 3)],
     _distill: [(dict(k=0), 1), (dict(k=-1), 2), (dict(k=1025), 2), (dict(T=0.0), 1), (dict(T=-1.0), 1), (dict(T=NAN), 1),
-               (dict(T=INF), 1), (dict(top=None), 1), (dict(value=None), 1), (dict(value=FAKE + 2), 1), (dict(h=None), 1),
+               (dict(T=INF), 1), (dict(T=1e-7), 1), (dict(T=2e6), 1), (dict(top=None), 1), (dict(value=None), 1), (dict(value=FAKE + 2), 1), (dict(h=None), 1),
                (dict(nbytes=4096), 3), (dict(dtype=9), 2)],
 }
 
@@ -87,6 +87,10 @@ def test_empty_calls_need_no_gpu():
     assert _norm_grad(n=0, x=None, dy=None, w=None, dw=None, db=None) == 0
     assert _ce(n=0, h=None, w=None, targets=None, total=None, dw=None, ws=None, nbytes=0) == 0
     assert _distill(n=0, h=None, w=None, top=None, value=None, total=None, dw=None, ws=None, nbytes=0) == 0
+    # a tensor without elements has no address: its output is not told from none
+    none = dict(dh=None, dw=None, loss=None, total=None, ws=None, nbytes=0)
+    assert _ce(n=0, h=None, w=None, targets=None, **none) == 0 and _distill(n=0, h=None, top=None, value=None, **none) == 0
+    assert _norm_grad(n=0, x=None, dy=None, dx=None, dw=None, db=None) == 0
 
 
 def test_workspace_sizes():

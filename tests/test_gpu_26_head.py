@@ -231,3 +231,36 @@ def test_differences(dev):
                       for s in (-0.05, 0.05))
             want = (f64(out["dh"]) * f64(dh)).sum() + (f64(out["dw"]) * f64(dw)).sum()
             assert abs((hi - lo) / 0.1 - want) < n * 4e-3
+
+
+@pytest.mark.parametrize("T", [0.5, 1.0, 3.0])
+def test_teacher_logits_of_the_lowest_value(dev, T):
+    """Masks of the type's lowest value are logits: alone in a list they share it, beside others they weigh nothing."""
+    n, d, V, k = 4, 64, 300, 5
+    h, w = _inputs(n, d, V, "f32")
+    top = torch.arange(n * k).view(n, k).int()
+    value = torch.full((n, k), torch.finfo(torch.float32).min)
+    value[1, 2], value[2, :2], value[3, 1:] = 4.0, torch.tensor([3.0e38, 1.0]), -float("inf")
+    announce(f"lowest logits {T}")
+    out = _run(dev, P.head_distill, h, w, top, value, temperature=T)
+    ref = E.distill(f64(h), f64(w), top.numpy(), value.numpy(), temperature=T)
+    assert ref["live"].all()
+    _check(out, ref, h, w, "f32", w.dtype, lists=k)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,d,V", [(37, 72, 257), (300, 128, 1003)])
+def test_workspaces_of_any_contents(dev, dtype, n, d, V):
+    """What a workspace holds before a call (here every bit set, NaN in both types) has no effect."""
+    h, w = (x.to(dev) for x in _inputs(n, d, V, dtype))
+    t = _targets(n, V, 0.3, 4).to(dev)
+    top = torch.stack([t, t.roll(1), t.roll(2)], 1).contiguous()
+    value = torch.randn(n, 3, device=dev)
+    for call, lists, k in [(P.head_cross_entropy, (t,), 0), (P.head_distill, (top, value), 3)]:
+        ws = torch.zeros(P.head_workspace_size(P.F32 if dtype == "f32" else P.BF16, n, d, V, top=k), dtype=torch.uint8,
+                         device=dev)
+        got = []
+        for fill in (0, 255):
+            ws.fill_(fill)
+            got.append(_run(dev, call, h, w, *lists, workspace=ws, mean=True))
+        assert all(torch.equal(got[0][x], got[1][x]) and got[0][x].isfinite().all() for x in got[0])
