@@ -56,14 +56,16 @@ __global__ __launch_bounds__(256) void embed_kernel(const int32_t* __restrict__ 
   }
 }
 
-// Positions sorted by token, those of one token ascending (and, for a gradient
-// written whole, the rows of absent tokens: zeros, `row_vecs` vectors of 16 bytes); start[v] = number
-// of positions whose token is in [0, v). A workgroup sorts the positions of
+// Positions sorted by token (order, and the tokens in key), those of one token
+// ascending (and, for a gradient written whole, the rows of absent tokens: zeros,
+// `row_vecs` vectors of 16 bytes); start[v] = number of positions whose token is
+// in [0, v). A workgroup sorts the positions of
 // kRange tokens: it reads all tokens twice (they stay in L2), counts those
 // before its range, and each wave places the positions of its stretch, 64 at
 // a time, ranked among equals by ballots over the bits of the token.
 __global__ __launch_bounds__(64 * kWaves) void embed_order_kernel(const int32_t* __restrict__ tokens, int n, int V,
                                                                   int32_t* __restrict__ order,
+                                                                  int32_t* __restrict__ key,
                                                                   int32_t* __restrict__ start,
                                                                   u32x4* __restrict__ out, int row_vecs) {
   __shared__ int hist[kWaves][kRange];
@@ -148,6 +150,7 @@ __global__ __launch_bounds__(64 * kWaves) void embed_order_kernel(const int32_t*
         const int rank = __popcll(same & ((uint64_t(1) << lane) - 1));
         const int at = hist[wave][r];
         order[at + rank] = i + 64 * u + lane;
+        key[at + rank] = t[u];
         if (rank == 0) hist[wave][r] = at + __popcll(same);
       }
       __builtin_amdgcn_wave_barrier();
@@ -163,7 +166,7 @@ __global__ __launch_bounds__(64 * kWaves) void embed_order_kernel(const int32_t*
 }
 
 struct EmbedSumArgs {
-  const int32_t* tokens; const int32_t* order; const int32_t* start;
+  const int32_t* order; const int32_t* key; const int32_t* start;
   const void* dy; void* out;
   float* part;  // [pieces][2][d]: sums of a piece's positions for the token it goes on with, and for the one it begins
   int n, V, d, accumulate;
@@ -223,7 +226,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedSumArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6));
   const TI* dy = (const TI*)a.dy;
   TO* out = (TO*)a.out;
-  const int n = a.start[a.V];  // positions that have a token
+  const int n = a.start[a.V];  // positions that have a token (from there on order and key hold nothing)
   const int64_t wg = wide_index();
   if (wg < a.long_wgs) {
     const int task = int(wg) * 4 + wave, piece = task / a.slabs, c = (task - piece * a.slabs) * kSlab + lane * 8;
@@ -231,7 +234,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedSumArgs a) {
     if (i0 >= n) return;
     const int m = std::min(kLong, n - i0);
     const int pos = a.order[i0 + std::min(lane, m - 1)];
-    const int t = a.tokens[pos];
+    const int t = a.key[i0 + std::min(lane, m - 1)];
     const int s = a.start[t];
     const bool is_long = a.start[t + 1] - s > kLong;
     // lanes of the long token that began before the piece, and of one that begins in it
@@ -246,12 +249,15 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedSumArgs a) {
     return;
   }
   const int64_t task = (wg - a.long_wgs) * 4 + wave;
-  if (task >= int64_t(n) * a.slabs) return;
   const int i = int(task / a.slabs), c = int(task - int64_t(i) * a.slabs) * kSlab + lane * 8;
-  const int t = a.tokens[a.order[i]];
-  const int m = a.start[t + 1] - i;
-  if (a.start[t] != i || m > kLong) return;
-  const int pos = a.order[i + std::min(lane, m - 1)];
+  // the places from i - 1 on, a lane to each: the token's are those from i to the next other's
+  // (read beside n, not after it)
+  const int here = a.key[std::max(0, std::min(i - 1 + lane, a.n - 1))], pos = a.order[std::min(i + lane, a.n - 1)];
+  if (i >= n) return;
+  const int last = std::min(i + kLong, n - 1);
+  const int t = __builtin_amdgcn_readlane(here, 1);
+  const int m = __popcll(__ballot(here == t && lane >= 1 && i - 1 + lane <= last));
+  if ((i > 0 && __builtin_amdgcn_readfirstlane(here) == t) || m > kLong) return;
   float v[8];
   embed_rows(dy, a.d, pos, 0, m, c, c < a.d, v);
   if (c < a.d) embed_store(out + int64_t(t) * a.d + c, v, a.scale, a.accumulate);
@@ -267,7 +273,7 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedSumArgs a) {
   const int n = a.start[a.V], i0 = piece * kLong;
   if (i0 >= n) return;
   const int m = std::min(kLong, n - i0);
-  const int t = a.tokens[a.order[i0 + std::min(lane, m - 1)]];
+  const int t = a.key[i0 + std::min(lane, m - 1)];
   const int s = a.start[t], e1 = a.start[t + 1];
   const uint64_t begins = __ballot(lane < m && e1 - s > kLong && s >= i0);
   if (begins == 0) return;
@@ -306,16 +312,17 @@ static size_t up256b(size_t v) { return (v + 255) & ~size_t(255); }
 
 size_t embed_backward_workspace_bytes(int n, int d, int V) {
   const size_t pieces = n > kLong ? size_t(n + kLong - 1) / kLong : 0;
-  return up256b(size_t(n) * 4) + up256b((size_t(V) + 1) * 4) + up256b(pieces * 2 * d * 4);
+  return 2 * up256b(size_t(n) * 4) + up256b((size_t(V) + 1) * 4) + up256b(pieces * 2 * d * 4);
 }
 
 hipError_t launch_embed_backward(const EmbedBackwardArgs& b, hipStream_t s) {
   char* ws = (char*)b.workspace;
   EmbedSumArgs a{};
   int32_t* order = (int32_t*)ws;
-  int32_t* start = (int32_t*)(ws + up256b(size_t(b.n) * 4));
-  a.part = (float*)(ws + up256b(size_t(b.n) * 4) + up256b((size_t(b.V) + 1) * 4));
-  a.tokens = b.tokens;
+  int32_t* key = (int32_t*)(ws + up256b(size_t(b.n) * 4));
+  int32_t* start = (int32_t*)(ws + 2 * up256b(size_t(b.n) * 4));
+  a.part = (float*)(ws + 2 * up256b(size_t(b.n) * 4) + up256b((size_t(b.V) + 1) * 4));
+  a.key = key;
   a.order = order;
   a.start = start;
   a.dy = b.dy;
@@ -330,7 +337,7 @@ hipError_t launch_embed_backward(const EmbedBackwardArgs& b, hipStream_t s) {
   a.long_wgs = int((tasks + 3) / 4);
   const int row_vecs = b.d * (b.dtable_type == DSF_F32 ? 4 : 2) / 16;
   embed_order_kernel<<<wide_grid((int64_t(b.V) + kRange - 1) / kRange), 64 * kWaves, 0, s>>>(
-      b.tokens, b.n, b.V, order, start, b.accumulate ? nullptr : (u32x4*)b.dtable, row_vecs);
+      b.tokens, b.n, b.V, order, key, start, b.accumulate ? nullptr : (u32x4*)b.dtable, row_vecs);
   const dim3 grid = wide_grid(a.long_wgs + (int64_t(b.n) * a.slabs + 3) / 4);
   const bool in32 = b.dtype == DSF_F32, out32 = b.dtable_type == DSF_F32;
   if (grid.x) {

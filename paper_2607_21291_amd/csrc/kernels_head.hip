@@ -256,36 +256,46 @@ __global__ __launch_bounds__(256) void head_gather_kernel(const T* __restrict__ 
 }
 
 // fp32: (maximum, sum of 2^(z - maximum)) of a row of logits, stats[row].
-__global__ __launch_bounds__(256) void head_stats_f32_kernel(const float* __restrict__ z, int ldz, int row0, int rows_max,
+__global__ __launch_bounds__(1024) void head_stats_f32_kernel(const float* __restrict__ z, int ldz, int row0, int rows_max,
                                                              const int32_t* __restrict__ n_active,
                                                              float2* __restrict__ stats) {
-  __shared__ float red[8];
-  const int rows = std::min(*n_active - row0, rows_max), s = blockIdx.x;
+  __shared__ float red[2][16];
+  const int rows = std::min(*n_active - row0, rows_max), s = int(wide_index());
   if (s >= rows) return;
   const float* p = z + int64_t(s) * ldz;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  // four vectors of a thread in flight: a call of few rows has a workgroup a CU at most
+  auto each = [&](auto f) {
+    for (int c = threadIdx.x * 4; c < ldz; c += 4 * 4096) {
+      float v[4][4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        v[u][0] = v[u][1] = v[u][2] = v[u][3] = -INFINITY;
+        if (c + 4096 * u < ldz) load_vec(p + c + 4096 * u, v[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) f(v[u]);
+    }
+  };
   float m = -INFINITY;
-  for (int c = threadIdx.x * 4; c < ldz; c += 1024) {
-    float v[4];
-    load_vec(p + c, v);
-    m = fmaxf(fmaxf(fmaxf(m, v[0]), fmaxf(v[1], v[2])), v[3]);
-  }
+  each([&](const float* v) { m = fmaxf(fmaxf(fmaxf(m, v[0]), fmaxf(v[1], v[2])), v[3]); });
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-  if (lane == 0) red[wave] = m;
+  if (lane == 0) red[0][wave] = m;
   __syncthreads();
-  m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+#pragma unroll
+  for (int i = 0; i < 16; ++i) m = fmaxf(m, red[0][i]);
   const float ref = m == -INFINITY ? 0.f : m;
   float sum = 0.f;
-  for (int c = threadIdx.x * 4; c < ldz; c += 1024) {
-    float v[4];
-    load_vec(p + c, v);
-    sum += (exp2f(v[0] - ref) + exp2f(v[1] - ref)) + (exp2f(v[2] - ref) + exp2f(v[3] - ref));
-  }
+  each([&](const float* v) { sum += (exp2f(v[0] - ref) + exp2f(v[1] - ref)) + (exp2f(v[2] - ref) + exp2f(v[3] - ref)); });
   sum = wave_sum(sum);
-  if (lane == 0) red[4 + wave] = sum;
+  if (lane == 0) red[1][wave] = sum;
   __syncthreads();
-  if (threadIdx.x == 0) stats[s] = float2{m, (red[4] + red[5]) + (red[6] + red[7])};
+  if (threadIdx.x == 0) {
+    sum = 0.f;
+    for (int i = 0; i < 16; ++i) sum += red[1][i];
+    stats[s] = float2{m, sum};
+  }
 }
 
 // lse[s] from the tiles' statistics, the row's loss, and the sum of weight x
@@ -482,15 +492,21 @@ __global__ __launch_bounds__(256) void head_dh_kernel(const float* __restrict__ 
       if (row0 != 0) continue;
     } else {
       if (s < 0 || s >= rows) continue;
-      for (int sp = 0; sp < splits; ++sp) {
-        const float* p = part + (int64_t(sp) * rows_ld + s) * d + c;
+      // (few rows have many partial sums: kPart of them in flight, added in order)
+      constexpr int kPart = 16;
+      const float* p = part + int64_t(s) * d + c;
+      for (int sp = 0; sp < splits; sp += kPart) {
+        float x[kPart][VEC];
 #pragma unroll
-        for (int e = 0; e < VEC; e += 4) {
-          float x[4];
-          load_vec(p + e, x);
+        for (int u = 0; u < kPart; ++u)
+          if (sp + u < splits)
 #pragma unroll
-          for (int b = 0; b < 4; ++b) v[e + b] += x[b];
-        }
+            for (int e = 0; e < VEC; e += 4) load_vec(p + int64_t(sp + u) * rows_ld * d + e, &x[u][e]);
+#pragma unroll
+        for (int u = 0; u < kPart; ++u)
+          if (sp + u < splits)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) v[e] += x[u][e];
       }
       const float f = *scale;
 #pragma unroll
@@ -631,7 +647,7 @@ hipError_t launch_head_loss(const HeadLossArgs& a, hipStream_t s) {
     auto product = [&](int mode) { return f32 ? launch_head_gemm_f32(mode, g, s) : launch_head_gemm(mode, g, s); };
     DSF_TRY(product(kHeadLogits));
     if (f32) {
-      head_stats_f32_kernel<<<g.rows, 256, 0, s>>>((const float*)g.z, p.ldz, g.row0, g.rows, n_active, stats);
+      head_stats_f32_kernel<<<wide_grid(g.rows), 1024, 0, s>>>((const float*)g.z, p.ldz, g.row0, g.rows, n_active, stats);
       DSF_TRY(hipGetLastError());
     }
     HeadLseArgs l{};
