@@ -725,8 +725,9 @@ size_t dsf_head_workspace_size(int dtype, int64_t n_rows, int d, int n_classes, 
  * d] of type dw_type: DSF_F32, or dtype. All are overwritten. With mean and
  * weights that sum to 0 the gradients are 0.
  * bf16: the products' operands are bf16; of the gradient at the logits,
- * weight (p - q), that is the one rounding (2^-8) but for a relative 2^-11 of p,
- * and p below 2^-64 of the greatest among 256 neighbouring classes, which is 0.
+ * weight (p - q), that is the one rounding (2^-8; in calls of at most 128 rows
+ * that take part 2^-16) but for a relative 2^-11 of p, and p below 2^-64 of the
+ * greatest among 256 neighbouring classes, which is 0.
  * Logits, log-sums and accumulation are fp32, total is summed in 64 bits.
  * d a multiple of 8, at most 16384; n_classes at most 2^21, n_rows at most 2^24.
  * Equal calls give equal bits. Workspace (256-byte aligned) as above. */

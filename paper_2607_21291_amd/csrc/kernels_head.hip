@@ -195,7 +195,8 @@ __global__ __launch_bounds__(1024) void head_rows_kernel(HeadRowsArgs a) {
   }
   if (a.splits)
     for (int p = wave; p < a.pieces; p += 16) {
-      const int n = head_dh_splits(std::max(0, std::min(all - p * a.rows, a.rows)), a.d, a.ldz, a.f32 != 0, a.most, lane);
+      const int here = std::max(0, std::min(all - p * a.rows, a.rows));
+      const int n = head_dh_splits(a.f32 ? here : head_dz_rows(all, here), a.d, a.ldz, a.f32 != 0, a.most, lane);
       if (lane == 0) a.splits[p] = n;
     }
   if (tid == 0) {
@@ -206,7 +207,7 @@ __global__ __launch_bounds__(1024) void head_rows_kernel(HeadRowsArgs a) {
   }
 }
 
-// hc[slot] = h[act[slot]], and z2[slot][j] = <h, W[class j]> z_scale for the row's
+// hc[slot] = h[act[slot]] (bf16, few rows: again for dz's second terms), and z2[slot][j] = <h, W[class j]> z_scale for the row's
 // classes (0 for those outside [0, V)). A wave takes a row and kDots classes.
 constexpr int kDots = 4;
 template <typename T>
@@ -219,7 +220,9 @@ __global__ __launch_bounds__(256) void head_gather_kernel(const T* __restrict__ 
   const int lane = threadIdx.x & 63;
   const int groups = (k + kDots - 1) / kDots;
   const int64_t task = wide_index() * 4 + (threadIdx.x >> 6);
-  if (task >= int64_t(*n_active) * groups) return;
+  const int n = *n_active;
+  if (task >= int64_t(n) * groups) return;
+  const bool twin = sizeof(T) == 2 && head_dz_rows(n, n) > n;
   const int s = int(task / groups), g = int(task - int64_t(s) * groups);
   const int row = act[s];
   const T* src = h + int64_t(row) * d;
@@ -235,7 +238,10 @@ __global__ __launch_bounds__(256) void head_gather_kernel(const T* __restrict__ 
   float acc[kDots] = {0.f, 0.f, 0.f, 0.f};
   for (int c = lane * VEC; c < d; c += 64 * VEC) {
     const u32x4 raw = *reinterpret_cast<const u32x4*>(src + c);
-    if (hc && g == 0) *reinterpret_cast<u32x4*>(hc + int64_t(s) * d + c) = raw;
+    if (g == 0) {
+      *reinterpret_cast<u32x4*>(hc + int64_t(s) * d + c) = raw;
+      if (twin) *reinterpret_cast<u32x4*>(hc + int64_t(n + s) * d + c) = raw;
+    }
     float x[VEC];
     load_vec(src + c, x);
 #pragma unroll
@@ -409,23 +415,26 @@ __device__ __forceinline__ void head_probs_entry(const HeadProbsArgs& a, int s, 
 }
 
 // bf16, in blocks: 32 rows, a thread to 16 bytes of a row of a block, then the
-// same of the next. Rows from the last that takes part to the next multiple of
-// 64 become zeros.
+// same of the next; few rows' second terms with the first. Rows from the last to
+// the next multiple of 64 become zeros.
 constexpr int kProbsRows = 32;
 __global__ __launch_bounds__(256) void head_probs_kernel(HeadProbsArgs a) {
   // the last rows first: their logits were written last
-  const int rows = std::min(*a.n_active - a.row0, a.rows), r = int(blockIdx.x) / a.cuts;
+  const int active = *a.n_active, rows = std::min(active - a.row0, a.rows), r = int(blockIdx.x) / a.cuts;
   if (rows <= 0) return;
-  const int s0 = ((rows + 63) / 64 * 64 / kProbsRows - 1 - r) * kProbsRows, c0 = (int(blockIdx.x) - r * a.cuts) * a.cols;
+  const int all = head_dz_rows(active, rows);
+  const int s0 = ((all + 63) / 64 * 64 / kProbsRows - 1 - r) * kProbsRows, c0 = (int(blockIdx.x) - r * a.cuts) * a.cols;
   if (s0 < 0) return;
   const int c1 = std::min(a.ldz, c0 + a.cols), s = s0 + int(threadIdx.x >> 3);
-  const bool live = s < rows;
+  const bool live = s < rows, twin = live && all > rows;
   const float lse = live ? a.lse[s] : 0.f;
   const float wt = !live ? 0.f : a.weight ? a.weight[a.act[a.row0 + s]] : 1.f;
   u32x4* p = reinterpret_cast<u32x4*>((uint16_t*)a.z + head_z_at(s, c0, a.ldz) + (threadIdx.x & 7) * 8);
+  // (the second terms' rows lie in the same blocks of 256)
+  u32x4* const p2 = p + int64_t(rows) * (kZClasses / 8);
   constexpr int kStep = kZBlock / 8;  // vectors of a block
-  auto probs = [&](u32x4& raw, float top) {
-    float v[8];
+  auto probs = [&](u32x4& raw, u32x4& rest, float top) {
+    float v[8], w[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -435,24 +444,35 @@ __global__ __launch_bounds__(256) void head_probs_kernel(HeadProbsArgs a) {
         v[2 * i + e] = !live || code == 0xffffu ? 0.f : wt * x;
       }
     store_vec(reinterpret_cast<uint16_t*>(&raw), v);
-  };
-  for (int c = c0; c < c1; c += kHeadTile, p += 4 * kStep) {
-    const float top = live ? a.stats[int64_t(c / kHeadTile) * a.rows_ld + s].x - lse : 0.f;
-    u32x4 raw[4];
+    if (twin) {
+      load_vec(reinterpret_cast<const uint16_t*>(&raw), w);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) raw[u] = p[u * kStep];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      probs(raw[u], top);
-      p[u * kStep] = raw[u];
+      for (int i = 0; i < 8; ++i) v[i] -= w[i];
+      store_vec(reinterpret_cast<uint16_t*>(&rest), v);
     }
-  }
+  };
+  if (live || s >= all)  // (the others are second terms)
+    for (int c = c0, at = 0; c < c1; c += kHeadTile, at += 4 * kStep) {
+      const float top = live ? a.stats[int64_t(c / kHeadTile) * a.rows_ld + s].x - lse : 0.f;
+      u32x4 raw[4], rest;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) raw[u] = p[at + u * kStep];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        probs(raw[u], rest, top);
+        p[at + u * kStep] = raw[u];
+        if (twin) p2[at + u * kStep] = rest;
+      }
+    }
   __syncthreads();  // (the stores below come after those above)
   for (int i = threadIdx.x; i < kProbsRows * a.k; i += 256) {
     const int si = s0 + i / a.k;
     if (si < rows)
-      head_probs_entry(a, si, i % a.k, c0, c1,
-                       [&](int c, float v) { ((uint16_t*)a.z)[head_z_at(si, c, a.ldz)] = f2bf(v); });
+      head_probs_entry(a, si, i % a.k, c0, c1, [&](int c, float v) {
+        const uint16_t first = f2bf(v);
+        ((uint16_t*)a.z)[head_z_at(si, c, a.ldz)] = first;
+        if (all > rows) ((uint16_t*)a.z)[head_z_at(rows + si, c, a.ldz)] = f2bf(v - bf2f(first));
+      });
   }
 }
 
@@ -475,14 +495,21 @@ __global__ __launch_bounds__(256) void head_probs_f32_kernel(HeadProbsArgs a) {
 }
 
 // dh of every row: scale times the sum of its partial sums, zeros for rows that
-// do not take part (written with the first piece).
+// do not take part (written with the first piece). `groups` lanes of a wave (a
+// power of two) share a vector's partial sums, which are then added in order: 64
+// rows of width 896, 64 shares of two terms, one lane 18 us, eight 8.3.
 template <typename T>
-__global__ __launch_bounds__(256) void head_dh_kernel(const float* __restrict__ part, const int32_t* __restrict__ n_splits, int rows_ld, int d,
+__global__ __launch_bounds__(256) void head_dh_kernel(const float* __restrict__ part, const int32_t* __restrict__ n_splits,
+                                                      const int32_t* __restrict__ n_active, int rows_ld, int d,
                                                       const int32_t* __restrict__ slot, int n, int row0, int rows,
-                                                      const float* __restrict__ scale, T* __restrict__ dh) {
-  constexpr int VEC = Elem<T>::kVec;
-  const int nv = d / VEC, splits = *n_splits;
-  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < int64_t(n) * nv; i += int64_t(gridDim.x) * 256) {
+                                                      const float* __restrict__ scale, T* __restrict__ dh, int groups) {
+  constexpr int VEC = Elem<T>::kVec, kPart = 16;  // partial sums in flight
+  const int nv = d / VEC, splits = *n_splits, active = *n_active;
+  // (few rows: dz's second terms' sums lie `active` rows on)
+  const int terms = sizeof(T) == 2 && head_dz_rows(active, 1) == 2 ? 2 : 1, sums = splits * terms;
+  const int lane = threadIdx.x & 63, per = 64 / groups, grp = lane / per;
+  const int64_t wave = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  for (int64_t i = wave * per + lane % per; i < int64_t(n) * nv; i += int64_t(gridDim.x) * 4 * per) {
     const int r = int(i / nv), c = int(i - int64_t(r) * nv) * VEC;
     const int s = slot[r] - row0;
     float v[VEC];
@@ -492,27 +519,31 @@ __global__ __launch_bounds__(256) void head_dh_kernel(const float* __restrict__ 
       if (row0 != 0) continue;
     } else {
       if (s < 0 || s >= rows) continue;
-      // (few rows have many partial sums: kPart of them in flight, added in order)
-      constexpr int kPart = 16;
       const float* p = part + int64_t(s) * d + c;
-      for (int sp = 0; sp < splits; sp += kPart) {
+      for (int q = grp * kPart; q < sums; q += groups * kPart) {
         float x[kPart][VEC];
 #pragma unroll
         for (int u = 0; u < kPart; ++u)
-          if (sp + u < splits)
+          if (q + u < sums) {
+            const int sp = (q + u) / terms, row = (q + u) % terms * active;
 #pragma unroll
-            for (int e = 0; e < VEC; e += 4) load_vec(p + int64_t(sp + u) * rows_ld * d + e, &x[u][e]);
+            for (int e = 0; e < VEC; e += 4) load_vec(p + (int64_t(sp) * rows_ld + row) * d + e, &x[u][e]);
+          }
 #pragma unroll
         for (int u = 0; u < kPart; ++u)
-          if (sp + u < splits)
+          if (q + u < sums)
 #pragma unroll
             for (int e = 0; e < VEC; ++e) v[e] += x[u][e];
       }
+      // (a vector's lanes have come the same way)
+      for (int o = per; o < 64; o <<= 1)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[e] += __shfl_xor(v[e], o, 64);
       const float f = *scale;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) v[e] *= f;
     }
-    store_vec(dh + int64_t(r) * d + c, v);
+    if (grp == 0) store_vec(dh + int64_t(r) * d + c, v);
   }
 }
 
@@ -520,7 +551,7 @@ __global__ __launch_bounds__(256) void head_dh_kernel(const float* __restrict__ 
 
 namespace {
 struct HeadPlan {
-  int ldz, rows, pieces, tiles, most, cuts, cols;
+  int ldz, rows, pieces, tiles, most, dz_rows, cuts, cols;  // dz_rows: of dz (with second terms), at most
   size_t splits, act, slot, live, scalars, q, qsum, plogp, z2, hc, lse, stats, partial, z, part, acc, total;
 };
 
@@ -547,7 +578,9 @@ HeadPlan head_plan(int dtype, int n, int d, int V, int k, bool grads) {
   const int64_t fit = int64_t(kDhPartBytes / (size_t(p.rows) * d * 4));
   p.most = int(std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(128, p.ldz / 256), fit)));
   // ranges of the classes for dz: some workgroups for each CU
-  const int unit = f32 ? 2048 : kHeadTile, groups = f32 ? p.rows : p.rows / kProbsRows;
+  p.dz_rows = std::min(p.rows, n);
+  if (!f32) p.dz_rows = (std::max(p.dz_rows, 2 * std::min(n, kHeadTwin)) + 63) / 64 * 64;
+  const int unit = f32 ? 2048 : kHeadTile, groups = f32 ? p.dz_rows : p.dz_rows / kProbsRows;
   p.cuts = std::max(1, std::min(p.ldz / unit, (2048 + groups - 1) / groups));
   p.cols = ((p.ldz + p.cuts - 1) / p.cuts + unit - 1) / unit * unit;
   p.cuts = (p.ldz + p.cols - 1) / p.cols;
@@ -569,7 +602,7 @@ HeadPlan head_plan(int dtype, int n, int d, int V, int k, bool grads) {
   p.lse = take(size_t(p.rows) * 4);
   p.partial = take(size_t(p.pieces) * ((p.rows + kLseRows - 1) / kLseRows) * 8);
   p.stats = take(size_t(p.tiles) * p.rows * sizeof(float2));
-  p.hc = take(size_t(n) * d * eb);
+  p.hc = take(size_t(f32 ? n : std::max(n, 2 * std::min(n, kHeadTwin))) * d * eb);
   if (grads || f32) p.z = take(size_t(p.rows) * p.ldz * eb);
   if (grads) {
     p.part = take(std::max(size_t(p.most) * p.rows * d * 4, size_t(kHeadGrid) * kHeadTile * kHeadTile * 4));
@@ -696,18 +729,20 @@ hipError_t launch_head_loss(const HeadLossArgs& a, hipStream_t s) {
     b.cuts = p.cuts;
     b.cols = p.cols;
     if (f32) head_probs_f32_kernel<<<g.rows * p.cuts, 256, 0, s>>>(b);
-    else head_probs_kernel<<<(g.rows + 63) / 64 * 64 / kProbsRows * p.cuts, 256, 0, s>>>(b);
+    else head_probs_kernel<<<p.dz_rows / kProbsRows * p.cuts, 256, 0, s>>>(b);
     DSF_TRY(hipGetLastError());
     if (a.dh) {
       DSF_TRY(product(kHeadDh));
       const int64_t nv = int64_t(a.n) * a.d / (f32 ? 4 : 8);
-      const dim3 grid(uint32_t(std::min<int64_t>((nv + 255) / 256, 8192)));
+      int groups = 1;  // lanes of a vector: some workgroups for each CU
+      while (groups < 8 && nv * groups < (1 << 17)) groups *= 2;
+      const dim3 grid(uint32_t(std::min<int64_t>((nv * groups + 255) / 256, 8192)));
       if (f32)
-        head_dh_kernel<float><<<grid, 256, 0, s>>>(g.part, g.splits, p.rows, a.d, slot, a.n, g.row0, g.rows, scale,
-                                                   (float*)a.dh);
+        head_dh_kernel<float><<<grid, 256, 0, s>>>(g.part, g.splits, n_active, p.rows, a.d, slot, a.n, g.row0, g.rows, scale,
+                                                   (float*)a.dh, groups);
       else
-        head_dh_kernel<uint16_t><<<grid, 256, 0, s>>>(g.part, g.splits, p.rows, a.d, slot, a.n, g.row0, g.rows, scale,
-                                                      (uint16_t*)a.dh);
+        head_dh_kernel<uint16_t><<<grid, 256, 0, s>>>(g.part, g.splits, n_active, p.rows, a.d, slot, a.n, g.row0, g.rows, scale,
+                                                      (uint16_t*)a.dh, groups);
       DSF_TRY(hipGetLastError());
     }
     if (a.dw) {

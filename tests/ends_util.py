@@ -48,7 +48,8 @@ def head_bounds(ref, h, w, dtype, half_out, dw_half):
     A logit is a sum of d products: chains of d / 32 additions of the matrix core's own sums of 32 (fp32: d / 2 of 2),
     scaled to log2 and by 1 / T: 4 u of itself. A dot product at a target is shorter. lse: the logits' error, exp2 and
     the sums (16 in a lane, 6 across lanes and waves, the tiles' in 16 chains and 16 more; fp32: V / 1024 and 16 more) and
-    the logarithm's. p: those of z and lse, the code (bf16), 4 u. dz is rounded to dtype. Products with dz: chains as
+    the logarithm's. p: those of z and lse, the code (bf16), 4 u. dz is rounded to dtype, in two terms where at most 128 rows take part
+    (bf16). Products with dz: chains as
     above over classes or rows (plus 128 partial sums), then scale and rounding."""
     n, d = h.shape
     V, T, live = w.shape[0], ref["temperature"], ref["live"]
@@ -66,9 +67,10 @@ def head_bounds(ref, h, w, dtype, half_out, dw_half):
     rp = np.expm1((ez + elogs + 8 * U * (spread + 1)) + (CODE if dtype == "bf16" else 0.0))[:, None]
     wt = np.abs(ref["weight"])[:, None]
     edz = wt * (ref["p"] * rp + (0 if ref["lists"] is None else 64 * U) + 4 * U) * live[:, None]
-    edz = edz + HALF[dtype] * (np.abs(ref["dz"]) + edz)
+    twin = dtype == "bf16" and live.sum() <= 128
+    edz = edz + (HALF[dtype] ** 2 if twin else HALF[dtype]) * (np.abs(ref["dz"]) + edz)
     s = abs(ref["scale"])
-    k1, k2 = V / step + step + 130, n / step + step + 4
+    k1, k2 = V / step + step + (260 if twin else 130), (2 if twin else 1) * n / step + step + 4
     adz = np.abs(ref["dz"]) + edz
     dh = s * (edz @ np.abs(w) + 2 * k1 * U * (adz @ np.abs(w))) * (1 + 4 * U)
     dw = s * (edz.T @ np.abs(h) + 2 * k2 * U * (adz.T @ np.abs(h))) * (1 + 4 * U)

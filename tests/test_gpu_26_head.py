@@ -98,6 +98,26 @@ def test_distill(dev, n, d, V, dtype, k, T):
     _check(out, ref, h, w, dtype, w.dtype, lists=k)
 
 
+@pytest.mark.parametrize("n,d,V", [(33, 8, 65), (64, 136, 1000), (65, 72, 129), (100, 904, 3001), (128, 64, 64), (129, 64, 300), (250, 72, 999)])
+@pytest.mark.parametrize("dw_type", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("masked", [0.0, 0.5])
+def test_few_rows(dev, n, d, V, dw_type, masked):
+    """dz has two terms up to 128 rows that take part: one large entry's rounding is not a row's error."""
+    h, w = _inputs(n, d, V, "bf16", n)
+    t = _targets(n, V, masked, 8)
+    h[(t < 0) | (t >= V)] = NAN
+    announce(f"few rows {n} {d} {V} {dw_type} {masked}")
+    weight = 0.5 + torch.rand(n, generator=torch.Generator().manual_seed(n))
+    out = _run(dev, P.head_cross_entropy, h, w, t, dw_type=dw_type, mean=True, row_weight=weight.to(dev))
+    ref = E.cross_entropy(np.nan_to_num(f64(h)), f64(w), t.numpy(), mean=True, weight=weight.numpy())
+    _check(out, ref, h, w, "bf16", dw_type)
+    teacher = torch.stack([t, t.roll(1)], 1).contiguous()
+    value = torch.randn(n, 2, generator=torch.Generator().manual_seed(n))
+    h = torch.nan_to_num(h)
+    out = _run(dev, P.head_distill, h, w, teacher, value, temperature=2.0, dw_type=dw_type)
+    _check(out, E.distill(f64(h), f64(w), teacher.numpy(), value.numpy(), temperature=2.0), h, w, "bf16", dw_type, lists=2)
+
+
 def test_one_entry_at_temperature_one_is_cross_entropy(dev):
     h, w = _inputs(70, 128, 900, "bf16")
     t = _targets(70, 900, 0.2, 1)
