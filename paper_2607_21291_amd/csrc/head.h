@@ -34,6 +34,13 @@ __host__ __device__ inline int64_t head_z_at(int row, int c, int ldz) {
 constexpr int kHeadTwin = 128;
 __host__ __device__ inline int head_dz_rows(int n_active, int rows) { return n_active <= kHeadTwin ? 2 * rows : rows; }
 
+// fp32: rows of a tile of the logits and of dh. Of few rows 64 where that pads them less
+// (F32FEW).
+constexpr int kHeadF32Few = 320;
+__host__ __device__ inline int head_f32_rows(int rows) {
+  return rows <= kHeadF32Few && (rows + 127) / 128 * 128 - rows >= 64 ? 64 : 128;
+}
+
 enum HeadMode { kHeadLogits = 0, kHeadDh = 1, kHeadDw = 2 };
 
 // One of a call's three products, over a piece of its active rows (bf16; fp32

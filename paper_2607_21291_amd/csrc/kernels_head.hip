@@ -99,8 +99,8 @@ __global__ __launch_bounds__(256) void head_teacher_kernel(const int32_t* __rest
 // k-tiles and about eight more, each share a partial sum written and read again
 // (at some 3 MB a k-tile). The fewest of the cheapest.
 __device__ __forceinline__ int head_dh_splits(int rows, int d, int ldz, bool f32, int most, int lane) {
-  const int t = f32 ? 128 : 256, slots = f32 ? 512 : kHeadGrid;
-  const int tiles = ((rows + t - 1) / t) * ((d + t - 1) / t);
+  const int t = f32 ? 128 : 256, tr = f32 ? head_f32_rows(rows) : 256, slots = f32 ? 512 : kHeadGrid;
+  const int tiles = ((rows + tr - 1) / tr) * ((d + t - 1) / t);
   const float nk = float(ldz) / 64.f, join = float(rows) * float(d) * 8.f / (f32 ? 4e6f : 3e6f);
   int got = 1;
   float best = INFINITY;

@@ -118,6 +118,19 @@ def test_few_rows(dev, n, d, V, dw_type, masked):
     _check(out, E.distill(f64(h), f64(w), teacher.numpy(), value.numpy(), temperature=2.0), h, w, "bf16", dw_type, lists=2)
 
 
+@pytest.mark.parametrize("n", [1, 63, 64, 65, 130, 192, 193, 300, 321, 400])
+@pytest.mark.parametrize("masked", [0.0, 0.4])
+def test_few_rows_in_fp32(dev, n, masked):
+    """Either side of the tiles' choices, by the rows that take part."""
+    d, V = 136, 1400
+    h, w = _inputs(n, d, V, "f32", n)
+    t = _targets(n, V, masked, 8)
+    h[(t < 0) | (t >= V)] = NAN
+    announce(f"few rows, fp32 {n} {masked}")
+    out = _run(dev, P.head_cross_entropy, h, w, t, mean=True)
+    _check(out, E.cross_entropy(np.nan_to_num(f64(h)), f64(w), t.numpy(), mean=True), h, w, "f32", w.dtype)
+
+
 def test_one_entry_at_temperature_one_is_cross_entropy(dev):
     h, w = _inputs(70, 128, 900, "bf16")
     t = _targets(70, 900, 0.2, 1)
