@@ -17,6 +17,12 @@
 // A workgroup per CU walks its tiles with one stream of k-tiles: the loads run
 // two k-tiles ahead, into the next tile while this one ends, so that only its
 // epilogue is between two tiles' products.
+//
+// 8192 rows of width 3584 over 151936 classes: logits 7.1 ms, dh 6.6-6.9, dW 6.7-6.95
+// (1.25-1.35 PFLOP/s), at the card's power limit: the clock falls to 1.8 GHz, of
+// which the matrix cores are busy 63-68 %. Width 768 over 50304: 740, 590, 540 us, the
+// logits' epilogue (two reductions over the tile's rows, an exponential and a code a logit)
+// being a quarter of theirs: accumulators fill the registers, so it stands alone.
 #include <algorithm>
 #include <type_traits>
 

@@ -6,7 +6,9 @@
 // Rows stay in registers between their one read and their write; one wave or
 // one workgroup to a row. The adjoint's workgroups walk the rows with the
 // gradients of gain and bias in registers; their partial sums are added in a
-// second launch, in an order that the number of rows fixes.
+// second launch, in an order that the number of rows fixes. Memory bounds both:
+// 8192 rows of width 2048 (bf16) 14 us, 4.8 TB/s, what a copy reaches; the adjoint
+// of 32768 of width 3584 170 us, 4.1 TB/s of three streams, and 6 for the sums.
 #include <algorithm>
 #include <type_traits>
 
@@ -95,14 +97,15 @@ __global__ __launch_bounds__(256) void norm_rows_kernel(const T* x, const T* __r
   }
 }
 
-// SUMS: also partial[workgroup][0] = sum dy xh, [1] = sum dy over its rows. dx may be dy or add.
-template <typename T, int C, int WAVES, bool RMS, bool SUMS>
+// A workgroup to a row. SUMS: also partial[workgroup][0] = sum dy xh, [1] = sum dy over its rows.
+// dx may be dy or add.
+template <typename T, int C, bool RMS, bool SUMS>
 __global__ __launch_bounds__(256) void norm_grad_kernel(const T* __restrict__ x, const T* dy,
                                                         const T* __restrict__ w, const T* add, int64_t n, int d,
                                                         float eps, T* dx, float* __restrict__ partial) {
-  constexpr int V = Elem<T>::kVec, L = 64 * WAVES, RPW = 4 / WAVES;  // rows of a workgroup at a time
+  constexpr int V = Elem<T>::kVec, WAVES = 4, L = 64 * WAVES;
   __shared__ float red[2][4][4];
-  const int l = WAVES == 1 ? int(threadIdx.x & 63) : int(threadIdx.x);
+  const int l = int(threadIdx.x);
   float dw[SUMS ? C : 1][V], db[SUMS && !RMS ? C : 1][V];
 #pragma unroll
   for (int c = 0; c < (SUMS ? C : 1); ++c)
@@ -114,7 +117,6 @@ __global__ __launch_bounds__(256) void norm_grad_kernel(const T* __restrict__ x,
     for (int i = 0; i < V; ++i) db[c][i] = 0.f;
   const float rd = 1.0f / float(d);
   int turn = 0;
-  const int64_t step = int64_t(gridDim.x) * RPW;
   // a row's vectors are asked for while the row before it is worked on (in
   // registers as they are; rows of many vectors have no room for it)
   constexpr bool kAhead = C <= 4;
@@ -129,9 +131,8 @@ __global__ __launch_bounds__(256) void norm_grad_kernel(const T* __restrict__ x,
       }
     }
   };
-  const int64_t r0 = int64_t(blockIdx.x) * RPW + (WAVES == 1 ? threadIdx.x >> 6 : 0);
-  if constexpr (kAhead) ask(r0);
-  for (int64_t r = r0; r < n; r += step, turn ^= 1) {
+  if constexpr (kAhead) ask(blockIdx.x);
+  for (int64_t r = blockIdx.x; r < n; r += gridDim.x, turn ^= 1) {
     float xv[C][V], gv[C][V];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
@@ -147,7 +148,7 @@ __global__ __launch_bounds__(256) void norm_grad_kernel(const T* __restrict__ x,
         load_vec(dy + r * d + at, gv[c]);
       }
     }
-    if constexpr (kAhead) ask(r + step);
+    if constexpr (kAhead) ask(r + gridDim.x);
     float m = 0.f;
     if constexpr (!RMS) {
       float s = 0.f;
@@ -177,23 +178,21 @@ __global__ __launch_bounds__(256) void norm_grad_kernel(const T* __restrict__ x,
     q = wave_sum_fast(q);
     sgx = wave_sum_fast(sgx);
     if constexpr (!RMS) sg = wave_sum_fast(sg);
-    if constexpr (WAVES > 1) {
-      const int wv = threadIdx.x >> 6;
-      if ((threadIdx.x & 63) == 0) {
-        red[turn][1][wv] = q;
-        red[turn][2][wv] = sgx;
-        red[turn][3][wv] = sg;
-      }
-      __syncthreads();
-      q = red[turn][1][0];
-      sgx = red[turn][2][0];
-      sg = red[turn][3][0];
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) {
+      red[turn][1][wave] = q;
+      red[turn][2][wave] = sgx;
+      red[turn][3][wave] = sg;
+    }
+    __syncthreads();
+    q = red[turn][1][0];
+    sgx = red[turn][2][0];
+    sg = red[turn][3][0];
 #pragma unroll
-      for (int i = 1; i < WAVES; ++i) {
-        q += red[turn][1][i];
-        sgx += red[turn][2][i];
-        sg += red[turn][3][i];
-      }
+    for (int i = 1; i < WAVES; ++i) {
+      q += red[turn][1][i];
+      sgx += red[turn][2][i];
+      sg += red[turn][3][i];
     }
     const float rstd = 1.0f / sqrtf(q * rd + eps);
     const float mgx = sgx * rd * rstd * rstd, mg = RMS ? 0.f : sg * rd;  // mean(g xh) r, mean g
@@ -218,9 +217,7 @@ __global__ __launch_bounds__(256) void norm_grad_kernel(const T* __restrict__ x,
     }
   }
   if constexpr (SUMS) {
-    // WAVES 1: the workgroup's four waves hold rows of their own, each a partial sum
-    const int64_t slot = WAVES == 1 ? int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6) : int64_t(blockIdx.x);
-    float* p = partial + slot * (RMS ? 1 : 2) * d;
+    float* p = partial + int64_t(blockIdx.x) * (RMS ? 1 : 2) * d;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const int at = (l + L * c) * V;
@@ -260,20 +257,14 @@ __global__ __launch_bounds__(1024) void norm_grad_sums_kernel(const float* __res
 }
 
 namespace {
-// (vectors a lane, waves a row) by the row's 16-byte vectors
+// vectors a lane of four waves to a row, by the row's 16-byte vectors
 template <typename F>
-bool norm_shape(int nv, bool many, F f) {
-  auto go = [&](auto Cc, auto Wc) { f(Cc, Wc); return true; };
-#define DSF_SHAPE(c, w) go(std::integral_constant<int, c>(), std::integral_constant<int, w>())
-  if (many && nv <= 64) return DSF_SHAPE(1, 1);
-  if (many && nv <= 128) return DSF_SHAPE(2, 1);
-  if (nv <= 256) return DSF_SHAPE(1, 4);
-  if (nv <= 512) return DSF_SHAPE(2, 4);
-  if (nv <= 1024) return DSF_SHAPE(4, 4);
-  if (nv <= 2048) return DSF_SHAPE(8, 4);
-  if (nv <= 4096) return DSF_SHAPE(16, 4);
-#undef DSF_SHAPE
-  return false;
+void norm_shape(int nv, F f) {
+  if (nv <= 256) f(std::integral_constant<int, 1>());
+  else if (nv <= 512) f(std::integral_constant<int, 2>());
+  else if (nv <= 1024) f(std::integral_constant<int, 4>());
+  else if (nv <= 2048) f(std::integral_constant<int, 8>());
+  else f(std::integral_constant<int, 16>());
 }
 }  // namespace
 
@@ -283,32 +274,43 @@ hipError_t launch_norm_rows(int dtype, bool rms, const void* x, const void* w, c
                             void* out, hipStream_t s) {
   auto run = [&](auto Tz) {
     using T = decltype(Tz);
-    norm_shape(d / Elem<T>::kVec, n >= 1024, [&](auto Cc, auto Wc) {
+    const int nv = d / Elem<T>::kVec;
+    auto go = [&](auto Cc, auto Wc) {
       constexpr int C = decltype(Cc)::value, W = decltype(Wc)::value;
       const dim3 grid = wide_grid(W == 1 ? (n + 3) / 4 : n);
       if (rms) norm_rows_kernel<T, C, W, true><<<grid, 256, 0, s>>>((const T*)x, (const T*)w, (const T*)b, n, d, eps, (T*)out);
       else norm_rows_kernel<T, C, W, false><<<grid, 256, 0, s>>>((const T*)x, (const T*)w, (const T*)b, n, d, eps, (T*)out);
-    });
+    };
+    // Many narrow rows: a wave to a row, so that its lanes have loads enough (width 768, bf16: 16384 rows
+    // 12.6 -> 9.7 us, 4096 4.5 -> 3.9; 1024 2.3 -> 2.7).
+    using One = std::integral_constant<int, 1>;
+    if (n >= 2048 && nv <= 64) go(One(), One());
+    else if (n >= 2048 && nv <= 128) go(std::integral_constant<int, 2>(), One());
+    else norm_shape(nv, [&](auto Cc) { go(Cc, std::integral_constant<int, 4>()); });
   };
   if (dtype == DSF_F32) run(float());
   else run(uint16_t());
   return hipGetLastError();
 }
 
-// partial sums: up to four a workgroup
+// partial sums: one a workgroup at most
 size_t norm_backward_workspace_bytes(int64_t n, int d) {
-  return size_t(std::min<int64_t>((n + 3) / 4, kBwdWgs)) * 4 * 2 * d * sizeof(float);
+  return size_t(std::min<int64_t>(n, kBwdWgs)) * 2 * d * sizeof(float);
 }
 
 hipError_t launch_norm_backward(const NormBackwardArgs& a, hipStream_t s) {
   auto run = [&](auto Tz) {
     using T = decltype(Tz);
-    norm_shape(a.d / Elem<T>::kVec, a.n >= 1024, [&](auto Cc, auto Wc) {
-      constexpr int C = decltype(Cc)::value, W = decltype(Wc)::value;
-      const int wgs = int(std::min<int64_t>(W == 1 ? (a.n + 3) / 4 : a.n, kBwdWgs));
+    // (a workgroup to a row also where rows are narrow: a wave to each leaves four times the partial
+    // sums, 4096 rows of width 768 14.1 -> 27.3 us, 16384 29.4 -> 35.0)
+    norm_shape(a.d / Elem<T>::kVec, [&](auto Cc) {
+      constexpr int C = decltype(Cc)::value;
+      // two rows or more for each partial sum once every CU has a workgroup (1024 rows of width 3584 on 1024
+      // workgroups 16.9 us, on 512 13.1); up to 1024 (16384 rows: on 512 125 us, 1024 91, 2048 97)
+      const int wgs = int(std::min<int64_t>(a.n, std::min<int64_t>(kBwdWgs, std::max<int64_t>(256, (a.n + 1) / 2))));
       const bool sums = a.dw || a.db;
       auto go = [&](auto R, auto S) {
-        norm_grad_kernel<T, C, W, decltype(R)::value, decltype(S)::value><<<wgs, 256, 0, s>>>(
+        norm_grad_kernel<T, C, decltype(R)::value, decltype(S)::value><<<wgs, 256, 0, s>>>(
             (const T*)a.x, (const T*)a.dy, (const T*)a.w, (const T*)a.add, a.n, a.d, a.eps, (T*)a.dx, (float*)a.workspace);
       };
       using Y = std::true_type;
@@ -318,9 +320,8 @@ hipError_t launch_norm_backward(const NormBackwardArgs& a, hipStream_t s) {
       else if (sums) go(N(), Y());
       else go(N(), N());
       if (!sums) return;
-      const int slots = W == 1 ? wgs * 4 : wgs, width = a.d * (a.rms ? 1 : 2);
-      norm_grad_sums_kernel<<<(width + 63) / 64, 1024, 0, s>>>((const float*)a.workspace, slots, a.d, a.rms ? 0 : 1, a.dw,
-                                                              a.db);
+      const int width = a.d * (a.rms ? 1 : 2);
+      norm_grad_sums_kernel<<<(width + 63) / 64, 1024, 0, s>>>((const float*)a.workspace, wgs, a.d, a.rms ? 0 : 1, a.dw, a.db);
     });
   };
   if (a.dtype == DSF_F32) run(float());

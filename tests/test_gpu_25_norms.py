@@ -11,7 +11,7 @@ from oracle import ends_oracle as E
 pytestmark = pytest.mark.gpu
 
 SHAPES = [(1, 8), (1, 896), (3, 768), (16, 3584), (5, 2056), (2, 16384), (7, 8200), (1023, 64), (1024, 64), (1025, 520),
-          (1500, 1024), (2050, 72), (1030, 3584), (4100, 1032)]
+          (1500, 1024), (2050, 72), (1030, 3584), (4100, 1032), (2100, 1000)]
 
 
 def _inputs(n, d, dtype, seed=0):
