@@ -697,7 +697,7 @@ size_t dsf_norm_backward_workspace_size(int64_t n_rows, int d);
  *   dx = add + r (g - mean g - xh mean(g xh))   (rms: without mean g),
  *   dw = sum over rows of dy xh,  db = sum over rows of dy.
  * dx [n_rows, d] in dtype, nullable; add nullable, in dtype (the gradient that
- * goes past the norm); dx may be dy or add. dw, db: device float [d], nullable,
+ * goes past the norm); dx may be x, dy or add. dw, db: device float [d], nullable,
  * overwritten (zeros for n_rows == 0); db null with rms. Statistics are taken
  * from x again. Sums in an order that n_rows and d fix. The workspace as above. */
 int dsf_norm_backward(const void* x, const void* dy, const void* w, const void* add, int dtype, int64_t n_rows, int d,
@@ -707,8 +707,11 @@ int dsf_norm_backward(const void* x, const void* dy, const void* w, const void* 
 /* Workspace bytes of the head's losses: top = 0 for dsf_head_cross_entropy, the
  * entries of a row for dsf_head_distill; gradients != 0 if dh or dw are wanted
  * (also enough for calls without). It holds 16 bits (fp32: 32) for each logit of
- * as many rows as fit 4 GiB (calls of more take them in pieces), and for
- * calls of several pieces the sum of dw in fp32. 0 on a bad argument. */
+ * as many rows as fit 4 GiB (calls of more take them in pieces), a copy of the
+ * rows of h that take part, three values an entry of the lists, with gradients
+ * fp32 partial sums (64 MiB at least; of dh for a piece's rows as many as fit 512
+ * MiB, one at least), and for calls of several pieces the sum of dw in fp32. 0 on
+ * a bad argument. */
 size_t dsf_head_workspace_size(int dtype, int64_t n_rows, int d, int n_classes, int top, int gradients);
 
 /* Cross entropy of a linear head. For rows h[i] and logits z_i = h[i] W^T over
@@ -722,8 +725,9 @@ size_t dsf_head_workspace_size(int dtype, int64_t n_rows, int d, int n_classes, 
  * [n_rows]; row_weight float [n_rows], null: ones. row_loss (nullable, float
  * [n_rows]): loss_i. total (nullable, float [2]): sum_i weight_i loss_i, and
  * sum_i weight_i (both 0 without rows). dh [n_rows, d] in dtype; dw [n_classes,
- * d] of type dw_type: DSF_F32, or dtype. All are overwritten. With mean and
- * weights that sum to 0 the gradients are 0.
+ * d] of type dw_type: DSF_F32, or dtype. All are overwritten; dh may be h, no
+ * other output may share memory with an input. With mean and weights that sum to
+ * 0 the gradients are 0.
  * bf16: the products' operands are bf16; of the gradient at the logits,
  * weight (p - q), that is the one rounding (2^-8; in calls of at most 128 rows
  * that take part 2^-16) but for a relative 2^-11 of p, and p below 2^-64 of the

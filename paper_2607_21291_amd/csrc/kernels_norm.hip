@@ -98,9 +98,9 @@ __global__ __launch_bounds__(256) void norm_rows_kernel(const T* x, const T* __r
 }
 
 // A workgroup to a row. SUMS: also partial[workgroup][0] = sum dy xh, [1] = sum dy over its rows.
-// dx may be dy or add.
+// dx may be x, dy or add: a row's are read before it is written, by the threads that write it.
 template <typename T, int C, bool RMS, bool SUMS>
-__global__ __launch_bounds__(256) void norm_grad_kernel(const T* __restrict__ x, const T* dy,
+__global__ __launch_bounds__(256) void norm_grad_kernel(const T* x, const T* dy,
                                                         const T* __restrict__ w, const T* add, int64_t n, int d,
                                                         float eps, T* dx, float* __restrict__ partial) {
   constexpr int V = Elem<T>::kVec, WAVES = 4, L = 64 * WAVES;

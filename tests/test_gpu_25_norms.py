@@ -129,3 +129,23 @@ def test_replays(dev):
             g.replay()
             torch.cuda.synchronize()
             assert all(torch.equal(p, q) for p, q in zip(got, want))
+
+
+@pytest.mark.parametrize("n,d", [(5, 2056), (1500, 1024), (2050, 72), (7, 8200), (3, 16384)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rms", [False, True])
+def test_adjoint_in_place(dev, n, d, dtype, rms):
+    """dx in the place of x, of dy or of add."""
+    x, w, _ = (t.to(dev) for t in _inputs(n, d, dtype))
+    dy, add = rand((n, d), dtype, 1).to(dev), rand((n, d), dtype, 2).to(dev)
+
+    def call(x, dy, add, dx):
+        dw = torch.empty(d, device=dev)
+        P.norm_backward(x, dy, w, dx, dw=dw, add=add, rms=rms)
+        return dx, dw
+
+    announce(f"adjoint in place {n} {d} {dtype} {rms}")
+    want = call(x, dy, add, torch.empty_like(x))
+    for i in range(3):
+        t = [x.clone(), dy.clone(), add.clone()]
+        assert all(torch.equal(a, b) for a, b in zip(call(*t, t[i]), want))

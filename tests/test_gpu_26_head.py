@@ -297,3 +297,16 @@ def test_workspaces_of_any_contents(dev, dtype, n, d, V):
             ws.fill_(fill)
             got.append(_run(dev, call, h, w, *lists, workspace=ws, mean=True))
         assert all(torch.equal(got[0][x], got[1][x]) and got[0][x].isfinite().all() for x in got[0])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,d,V", [(37, 72, 257), (300, 128, 1003)])
+def test_dh_in_the_place_of_h(dev, dtype, n, d, V):
+    h, w = (x.to(dev) for x in _inputs(n, d, V, dtype))
+    t = _targets(n, V, 0.3, 4).to(dev)
+    want = _run(dev, P.head_cross_entropy, h, w, t, mean=True)
+    total, row_loss, dw, dh = torch.empty(2, device=dev), torch.empty(n, device=dev), torch.empty_like(w), h.clone()
+    announce(f"dh in the place of h {dtype} {n} {d} {V}")
+    P.head_cross_entropy(dh, w, t, row_loss=row_loss, total=total, dh=dh, dw=dw, mean=True)
+    got = {"row_loss": row_loss, "total": total, "dh": dh, "dw": dw}
+    assert all(torch.equal(got[x], want[x]) for x in want)
