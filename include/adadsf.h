@@ -732,7 +732,9 @@ size_t dsf_head_workspace_size(int dtype, int64_t n_rows, int d, int n_classes, 
  * weight (p - q), that is the one rounding (2^-8; in calls of at most 128 rows
  * that take part 2^-16) but for a relative 2^-11 of p, and p below 2^-64 of the
  * greatest among 256 neighbouring classes, which is 0.
- * Logits, log-sums and accumulation are fp32, total is summed in 64 bits.
+ * Logits, log-sums and accumulation are fp32, total is summed in 64 bits. Where p of
+ * a target is next to 1, the loss and p - 1 are off by the rounding of 1 (8 x 2^-24), not
+ * by that of a logit.
  * d a multiple of 8, at most 16384; n_classes at most 2^21, n_rows at most 2^24.
  * Equal calls give equal bits. Workspace (256-byte aligned) as above. */
 int dsf_head_cross_entropy(const void* h, const void* w, int dtype, int64_t n_rows, int d, int n_classes,

@@ -5,10 +5,16 @@
 // one class, q = 1). With z = h W^T / T, in units of log 2, lse = log2 sum 2^z:
 //   loss = T^2 sum_j q_j (log q_j - ln 2 (z_j - lse)),  dz = T (p - q).
 // Steps: the teacher's q; the rows that take part (a target, a weight), counted
-// and listed in order; their h, gathered; z at the targets by dot products in
-// fp32; then for pieces of those rows the logits' tiles, lse and losses, dz in
-// place of the logits' codes, dh and dW. Only the listed rows cost products,
-// and what lies in the others (NaN too) has no effect.
+// and listed in order; their h, gathered; z at the targets; then for pieces of
+// those rows the logits' tiles, lse and losses, dz in place of the logits' codes,
+// dh and dW. Only the listed rows cost products, and what lies in the others (NaN
+// too) has no effect.
+//
+// A row that is sure of its target has z = lse but for e^-z: both have to come from the
+// same sums, or the loss and p - 1 are a logit's rounding (6e-5 at 45 and width 3584).
+// z at the targets is the product's own, bit by bit (bf16: the same matrix
+// instructions in the same order; fp32: read back), and lse stays in two terms, the
+// greatest logit and log2 of the sum relative to it: z - maximum is taken first.
 //
 // 16 bits per logit of a piece are all that is kept: with them the backward
 // needs no second product for the logits (three products, not four; 25 % of the
@@ -207,60 +213,71 @@ __global__ __launch_bounds__(1024) void head_rows_kernel(HeadRowsArgs a) {
   }
 }
 
-// hc[slot] = h[act[slot]] (bf16, few rows: again for dz's second terms), and
-// z2[slot][j] = <h, W[class j]> z_scale for the row's classes (0 for those outside
-// [0, V)). A wave takes a row and kDots classes (6554 rows of width 896 with lists
-// of 64: 126 us, 6.0 TB/s with what the caches hold).
-constexpr int kDots = 4;
-template <typename T>
-__global__ __launch_bounds__(256) void head_gather_kernel(const T* __restrict__ h, const T* __restrict__ w,
-                                                          const int32_t* __restrict__ classes, int k, int V, int d,
-                                                          const int32_t* __restrict__ act,
-                                                          const int32_t* __restrict__ n_active, float z_scale,
-                                                          T* __restrict__ hc, float* __restrict__ z2) {
-  constexpr int VEC = Elem<T>::kVec;
-  const int lane = threadIdx.x & 63;
-  const int groups = (k + kDots - 1) / kDots;
-  const int64_t task = wide_index() * 4 + (threadIdx.x >> 6);
+// The rows that take part, and (bf16) their logits at their lists' classes:
+// hc[slot] = h[act[slot]] (few rows: again for dz's second terms), z2[slot][j] = <h, W[class j]>,
+// 0 for a class outside [0, V).
+//
+// bf16: a wave to sixteen entries of the lists one after another, entry x being list place
+// x % k of slot x / k: A's rows are the entries' rows of W, B's their rows of h, and
+// the products' diagonal is z2. k goes up by the 32 of an instruction, from the same zeros and in
+// the same lanes as in a tile of logits, so that the sums have the same bits. A slot's first
+// entry copies its row. (One wave a workgroup: 8192 rows of one class are 512, 34 us at width
+// 3584, eight operands in flight 37; 6554 rows of width 896 with lists of 64 124 us, 6.1 TB/s
+// with what the caches hold.)
+constexpr int kDots = 16;
+__global__ __launch_bounds__(64) void head_gather_kernel(const uint16_t* __restrict__ h, const uint16_t* __restrict__ w,
+                                                         const int32_t* __restrict__ classes, int k, int V, int d,
+                                                         const int32_t* __restrict__ act,
+                                                         const int32_t* __restrict__ n_active, uint16_t* __restrict__ hc,
+                                                         float* __restrict__ z2) {
+  constexpr int U = 16;  // products whose operands are in flight
+  const int lane = threadIdx.x & 63, r16 = lane & 15, grp = lane >> 4;
   const int n = *n_active;
-  if (task >= int64_t(n) * groups) return;
-  const bool twin = sizeof(T) == 2 && head_dz_rows(n, n) > n;
-  const int s = int(task / groups), g = int(task - int64_t(s) * groups);
-  const int row = act[s];
-  const T* src = h + int64_t(row) * d;
-  const T* wr[kDots];
-  bool in[kDots];
+  const int64_t x0 = wide_index() * kDots, all = int64_t(n) * k, x = x0 + r16;
+  if (x0 >= all) return;
+  const bool in = x < all;
+  const int s = in ? int(x / k) : 0, j = in ? int(x - int64_t(s) * k) : 0, row = act[s];
+  const int c = in ? classes[int64_t(row) * k + j] : -1;
+  const bool some = uint32_t(c) < uint32_t(V), first = in && j == 0;
+  const bool twin = first && head_dz_rows(n, n) > n;
+  const uint16_t* const hr = h + int64_t(row) * d;
+  const uint16_t* const wr = w + int64_t(some ? c : 0) * d;
+  uint16_t* const to = hc + int64_t(s) * d;
+  uint16_t* const to2 = hc + int64_t(n + s) * d;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int k0 = 0; k0 < d; k0 += 32 * U) {
+    u32x4 a[U], b[U];
 #pragma unroll
-  for (int u = 0; u < kDots; ++u) {
-    const int j = g * kDots + u;
-    const int c = j < k ? classes[int64_t(row) * k + j] : -1;
-    in[u] = uint32_t(c) < uint32_t(V);
-    wr[u] = w + int64_t(in[u] ? c : 0) * d;
-  }
-  float acc[kDots] = {0.f, 0.f, 0.f, 0.f};
-  for (int c = lane * VEC; c < d; c += 64 * VEC) {
-    const u32x4 raw = *reinterpret_cast<const u32x4*>(src + c);
-    if (g == 0) {
-      *reinterpret_cast<u32x4*>(hc + int64_t(s) * d + c) = raw;
-      if (twin) *reinterpret_cast<u32x4*>(hc + int64_t(n + s) * d + c) = raw;
+    for (int u = 0; u < U; ++u) {
+      const int at = k0 + 32 * u + 8 * grp;
+      a[u] = b[u] = u32x4{0, 0, 0, 0};
+      if (in && at < d) b[u] = *reinterpret_cast<const u32x4*>(hr + at);
+      if (some && at < d) a[u] = *reinterpret_cast<const u32x4*>(wr + at);
     }
-    float x[VEC];
-    load_vec(src + c, x);
 #pragma unroll
-    for (int u = 0; u < kDots; ++u) {
-      float y[VEC];
-      if (in[u]) {
-        load_vec(wr[u] + c, y);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) acc[u] = fmaf(x[i], y[i], acc[u]);
-      }
+    for (int u = 0; u < U; ++u) {
+      const int at = k0 + 32 * u + 8 * grp;
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[u]), __builtin_bit_cast(bf16x8, b[u]), acc,
+                                                    0, 0, 0);
+      if (first && at < d) *reinterpret_cast<u32x4*>(to + at) = b[u];
+      if (twin && at < d) *reinterpret_cast<u32x4*>(to2 + at) = b[u];
     }
   }
-#pragma unroll
-  for (int u = 0; u < kDots; ++u) {
-    const float v = wave_sum(acc[u]);
-    if (lane == 0 && g * kDots + u < k) z2[int64_t(s) * k + g * kDots + u] = v * z_scale;
-  }
+  // lane holds out[n = r16][m = 4 grp + e]
+  const float v = r16 & 2 ? (r16 & 1 ? acc[3] : acc[2]) : (r16 & 1 ? acc[1] : acc[0]);
+  if (in && grp == r16 >> 2) z2[x] = some ? v : 0.f;
+}
+
+// fp32: the rows alone, a wave to a row (z at the targets is read back from the product).
+__global__ __launch_bounds__(256) void head_rows_f32_kernel(const float* __restrict__ h, int d,
+                                                            const int32_t* __restrict__ act,
+                                                            const int32_t* __restrict__ n_active, float* __restrict__ hc) {
+  const int lane = threadIdx.x & 63;
+  const int64_t s = wide_index() * 4 + (threadIdx.x >> 6);
+  if (s >= *n_active) return;
+  const u32x4* src = reinterpret_cast<const u32x4*>(h + int64_t(act[s]) * d);
+  u32x4* to = reinterpret_cast<u32x4*>(hc + s * d);
+  for (int c = lane; c < d / 4; c += 64) to[c] = src[c];
 }
 
 // fp32: (maximum, sum of 2^(z - maximum)) of kStatCols of a row's logits, which stay in
@@ -306,16 +323,20 @@ __global__ __launch_bounds__(1024) void head_stats_f32_kernel(const float* __res
   }
 }
 
-// lse[s] from the tiles' statistics, the row's loss, and the sum of weight x
+// lse[s] = (greatest logit, log2 of the sum of 2^(z - greatest)) from the tiles'
+// statistics, the row's loss, and the sum of weight x
 // loss: a partial sum of each workgroup, added in order by the last of the
 // call's to finish. 16 rows by 64 groups of tiles; then a wave to a row's list.
+// fp32: z at the list's classes comes from the logits, and goes to z2.
 struct HeadLseArgs {
   const float2* stats; int tiles, rows_ld;
-  const float* z2; const float* q; const float* plogp;  // q null: one class, q = 1
+  float* z2; const float* q; const float* plogp;  // q null: one class, q = 1
+  float z_scale;  // of z2: to units of log 2
+  const float* z; int ldz; const int32_t* classes; int V;  // z: fp32 logits, or null
   const float* weight;
   const int32_t* act; const int32_t* n_active;
   const double* wsum;
-  float* lse; float* row_loss; float* total; double* partial; uint32_t* count;
+  float2* lse; float* row_loss; float* total; double* partial; uint32_t* count;
   int row0, rows, k, first, workgroups;  // first: index of this launch's first partial sum; workgroups of the call
   float T;
 };
@@ -351,20 +372,29 @@ __global__ __launch_bounds__(1024) void head_lse_kernel(HeadLseArgs a) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
   const float ref = M == -INFINITY ? 0.f : M;
-  const float lse = ref + log2f(wave_sum(mine.y * exp2f(mine.x - ref)));
+  const float logs = log2f(wave_sum(mine.y * exp2f(mine.x - ref)));
   const int row = in ? a.act[g] : 0;
   // sum_j q_j (lse - z_j)
   float x = 0.f;
   if (in)
     for (int j = lane; j < a.k; j += 64) {
       const float q = a.q ? a.q[int64_t(row) * a.k + j] : 1.f;
-      if (!(q == 0.f)) x += q * (lse - a.z2[int64_t(g) * a.k + j]);
+      float z;
+      if (a.z) {
+        const int c = a.classes[int64_t(row) * a.k + j];
+        a.z2[int64_t(g) * a.k + j] = z = uint32_t(c) < uint32_t(a.V) ? a.z[int64_t(s) * a.ldz + c] : 0.f;
+      } else {
+        z = a.z2[int64_t(g) * a.k + j];
+      }
+      // (a probability is at most 1: what the sum's rounding leaves below 0 is 0; NaN stays)
+      const float below = fmaf(-a.z_scale, z, ref) + logs;
+      if (!(q == 0.f)) x += q * (below < 0.f ? 0.f : below);
     }
   x = wave_sum(x);
   if (lane == 0) {
     double wl = 0.0;
     if (in) {
-      a.lse[s] = lse;
+      a.lse[s] = float2{ref, logs};
       const float loss = a.T * a.T * ((a.q ? a.plogp[row] : 0.f) + kLn2 * x);
       if (a.row_loss) a.row_loss[row] = loss;
       wl = (a.weight ? double(a.weight[row]) : 1.0) * double(loss);
@@ -399,7 +429,8 @@ __global__ __launch_bounds__(1024) void head_lse_kernel(HeadLseArgs a) {
 struct HeadProbsArgs {
   void* z; int ldz;
   const float2* stats; int rows_ld;  // bf16: the tiles' maxima
-  const float* lse; const float* z2; const float* qsum;  // qsum null: cross entropy
+  const float2* lse; const float* z2; float z_scale;  // as above
+  const float* qsum;  // null: cross entropy
   const float* weight; const int32_t* classes;
   const int32_t* act; const int32_t* n_active;
   int row0, rows, k, V, cuts, cols;  // cols: classes of a range, a multiple of 2048 (bf16: 256)
@@ -413,7 +444,9 @@ __device__ __forceinline__ void head_probs_entry(const HeadProbsArgs& a, int s, 
   if (c < c0 || c >= std::min(c1, a.V)) return;
   const float sum = a.qsum ? a.qsum[at] : 1.f;
   if (sum == -1.f) return;
-  store(c, (a.weight ? a.weight[row] : 1.f) * (exp2f(a.z2[int64_t(g) * a.k + j] - a.lse[s]) - sum));
+  const float2 lse = a.lse[s];
+  const float z = fmaf(a.z_scale, a.z2[int64_t(g) * a.k + j], -lse.x) - lse.y;
+  store(c, (a.weight ? a.weight[row] : 1.f) * (exp2f(z > 0.f ? 0.f : z) - sum));
 }
 
 // bf16, in blocks: 32 rows, a thread to 16 bytes of a row of a block, then the
@@ -430,7 +463,7 @@ __global__ __launch_bounds__(256) void head_probs_kernel(HeadProbsArgs a) {
   if (s0 < 0) return;
   const int c1 = std::min(a.ldz, c0 + a.cols), s = s0 + int(threadIdx.x >> 3);
   const bool live = s < rows, twin = live && all > rows;
-  const float lse = live ? a.lse[s] : 0.f;
+  const float2 lse = live ? a.lse[s] : float2{0.f, 0.f};
   const float wt = !live ? 0.f : a.weight ? a.weight[a.act[a.row0 + s]] : 1.f;
   u32x4* p = reinterpret_cast<u32x4*>((uint16_t*)a.z + head_z_at(s, c0, a.ldz) + (threadIdx.x & 7) * 8);
   // (the second terms' rows lie in the same blocks of 256)
@@ -456,7 +489,7 @@ __global__ __launch_bounds__(256) void head_probs_kernel(HeadProbsArgs a) {
   };
   if (live || s >= all)  // (the others are second terms)
     for (int c = c0, at = 0; c < c1; c += kHeadTile, at += 4 * kStep) {
-      const float top = live ? a.stats[int64_t(c / kHeadTile) * a.rows_ld + s].x - lse : 0.f;
+      const float top = live ? (a.stats[int64_t(c / kHeadTile) * a.rows_ld + s].x - lse.x) - lse.y : 0.f;
       u32x4 raw[4], rest;
 #pragma unroll
       for (int u = 0; u < 4; ++u) raw[u] = p[at + u * kStep];
@@ -484,13 +517,14 @@ __global__ __launch_bounds__(256) void head_probs_f32_kernel(HeadProbsArgs a) {
   const int s = int(blockIdx.x) / a.cuts, c0 = (int(blockIdx.x) - s * a.cuts) * a.cols;
   if (s >= std::min(*a.n_active - a.row0, a.rows)) return;
   const int c1 = std::min(a.ldz, c0 + a.cols);
-  const float lse = a.lse[s], wt = a.weight ? a.weight[a.act[a.row0 + s]] : 1.f;
+  const float2 lse = a.lse[s];
+  const float wt = a.weight ? a.weight[a.act[a.row0 + s]] : 1.f;
   float* z = (float*)a.z + int64_t(s) * a.ldz;
   for (int c = c0 + int(threadIdx.x) * 4; c < c1; c += 1024) {
     float p[4];
     load_vec(z + c, p);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) p[i] = p[i] == -INFINITY ? 0.f : wt * exp2f(p[i] - lse);
+    for (int i = 0; i < 4; ++i) p[i] = p[i] == -INFINITY ? 0.f : wt * exp2f((p[i] - lse.x) - lse.y);
     store_vec(z + c, p);
   }
   __syncthreads();
@@ -602,7 +636,7 @@ HeadPlan head_plan(int dtype, int n, int d, int V, int k, bool grads) {
   p.q = take(size_t(n) * k * 4);
   p.qsum = take(size_t(n) * k * 4);
   p.z2 = take(size_t(n) * std::max(k, 1) * 4);
-  p.lse = take(size_t(p.rows) * 4);
+  p.lse = take(size_t(p.rows) * sizeof(float2));
   p.partial = take(size_t(p.pieces) * ((p.rows + kLseRows - 1) / kLseRows) * 8);
   p.stats = take(size_t(p.tiles) * p.rows * sizeof(float2));
   p.hc = take(size_t(f32 ? n : std::max(n, 2 * std::min(n, kHeadTwin))) * d * eb);
@@ -633,7 +667,7 @@ hipError_t launch_head_loss(const HeadLossArgs& a, hipStream_t s) {
   int32_t* slot = (int32_t*)(ws + p.slot);
   float* q = distill ? (float*)(ws + p.q) : nullptr;
   float* z2 = (float*)(ws + p.z2);
-  float* lse = (float*)(ws + p.lse);
+  float2* lse = (float2*)(ws + p.lse);
   float2* stats = (float2*)(ws + p.stats);
   const float z_scale = kLog2e / a.temperature;
   hipError_t e;
@@ -650,14 +684,12 @@ hipError_t launch_head_loss(const HeadLossArgs& a, hipStream_t s) {
                        a.dh ? splits : nullptr, p.pieces, p.rows, a.d, p.ldz, p.most, f32};
   head_rows_kernel<<<1, 1024, 0, s>>>(r);
   DSF_TRY(hipGetLastError());
-  const int64_t tasks = int64_t(a.n) * ((k + kDots - 1) / kDots);
-  const dim3 gg = wide_grid((tasks + 3) / 4);
   if (f32)
-    head_gather_kernel<float><<<gg, 256, 0, s>>>((const float*)a.h, (const float*)a.w, a.classes, k, a.V, a.d, act,
-                                                 n_active, z_scale, (float*)(ws + p.hc), z2);
+    head_rows_f32_kernel<<<wide_grid((int64_t(a.n) + 3) / 4), 256, 0, s>>>((const float*)a.h, a.d, act, n_active,
+                                                                           (float*)(ws + p.hc));
   else
-    head_gather_kernel<uint16_t><<<gg, 256, 0, s>>>((const uint16_t*)a.h, (const uint16_t*)a.w, a.classes, k, a.V, a.d,
-                                                    act, n_active, z_scale, (uint16_t*)(ws + p.hc), z2);
+    head_gather_kernel<<<wide_grid((int64_t(a.n) * k + kDots - 1) / kDots), 64, 0, s>>>(
+        (const uint16_t*)a.h, (const uint16_t*)a.w, a.classes, k, a.V, a.d, act, n_active, (uint16_t*)(ws + p.hc), z2);
   DSF_TRY(hipGetLastError());
   const int lse_wgs = (p.rows + kLseRows - 1) / kLseRows;
   for (int i = 0; i < p.pieces; ++i) {
@@ -692,6 +724,11 @@ hipError_t launch_head_loss(const HeadLossArgs& a, hipStream_t s) {
     l.tiles = p.tiles;
     l.rows_ld = p.rows;
     l.z2 = z2;
+    l.z_scale = f32 ? 1.f : z_scale;
+    l.z = f32 ? (const float*)g.z : nullptr;
+    l.ldz = p.ldz;
+    l.classes = a.classes;
+    l.V = a.V;
     l.q = q;
     l.plogp = (const float*)(ws + p.plogp);
     l.weight = a.weight;
@@ -721,6 +758,7 @@ hipError_t launch_head_loss(const HeadLossArgs& a, hipStream_t s) {
     b.rows_ld = p.rows;
     b.lse = lse;
     b.z2 = z2;
+    b.z_scale = l.z_scale;
     b.qsum = distill ? (const float*)(ws + p.qsum) : nullptr;
     b.weight = a.weight;
     b.classes = a.classes;
