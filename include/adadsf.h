@@ -673,8 +673,9 @@ size_t dsf_embed_backward_workspace_size(int64_t n_tokens, int d, int n_classes)
  * occur are not touched), for a table that is the head's as well. Positions
  * whose token lies outside [0, n_classes) have no effect, whatever their dy.
  * dy [n_tokens, d] in dtype; dtable [n_classes, d] of type dtable_type: DSF_F32,
- * or dtype. Sums are fp32, in an order that tokens fix: equal calls give equal
- * bits. n_tokens below 2^30. The workspace (256-byte aligned) needs no
+ * or dtype. Sums are fp32 for up to 256 positions,
+ * those of more add such sums in 64 bits, in an order that tokens fix: equal calls
+ * give equal bits. n_tokens below 2^30. The workspace (256-byte aligned) needs no
  * initialisation; calls that overlap in time, and graphs whose replays may, need
  * separate ones. */
 int dsf_embed_backward(const int32_t* tokens, const void* dy, int dtype, int64_t n_tokens, int n_classes, int d,
