@@ -632,6 +632,13 @@ def _call_on(name: str, like, index: int, stream, *args):
         _check(name, rc)
 
 
+def _ints(**sizes):
+    """Refuses sizes that the C entry points' 32-bit integers would take the lower halves of."""
+    for name, value in sizes.items():
+        if not -2**31 <= value < 2**31:
+            raise ValueError(f"{name} must be below 2^31, got {value}")
+
+
 _I32, _F32 = torch.int32, torch.float32
 _CODES = {torch.float32: F32, torch.bfloat16: BF16}
 
@@ -643,12 +650,15 @@ def embed_forward(tokens, table, out, scale: float = 1.0, stream=None):
     if len(whole) != 2 or dtype is None:
         raise ValueError("table: [n_classes, d], float32 or bfloat16")
     V, d = whole
+    if (V | d) >> 31:
+        _ints(n_classes=V, d=d)
     _call_on("dsf_embed_forward", table, at, stream, _dense("tokens", tokens, shape, _I32, at),
              _dense("table", table, whole, t, at), dtype, tokens.numel(), V, d, scale,
              _dense("out", out, (*shape, d), t, at))
 
 
 def embed_backward_workspace_size(n_tokens: int, d: int, n_classes: int) -> int:
+    _ints(d=d, n_classes=n_classes)
     return lib().dsf_embed_backward_workspace_size(n_tokens, d, n_classes)
 
 
@@ -658,6 +668,8 @@ def embed_backward(tokens, dy, dtable, scale: float = 1.0, accumulate: bool = Fa
     if dtable.dim() != 2:
         raise ValueError("dtable: [n_classes, d]")
     V, d = dtable.shape
+    if (V | d) >> 31:
+        _ints(n_classes=V, d=d)
     n, shape = tokens.numel(), tokens.shape
     tp, yp = _dense("tokens", tokens, shape, _I32, at), _dense("dy", dy, (*shape, d), dy.dtype, at)
     gp = _dense("dtable", dtable, dtable.shape, dy.dtype, at, _F32)
@@ -673,12 +685,15 @@ def norm_forward(x, w, out, b=None, eps: float = 1e-5, rms: bool = False, stream
     if dtype is None or not shape:
         raise ValueError("x: [..., d], float32 or bfloat16")
     d = shape[-1]
+    if d >> 31:
+        _ints(d=d)
     n = x.numel() // d if d else 0
     _call_on("dsf_norm_forward", x, at, stream, _dense("x", x, shape, t, at), _dense("w", w, (d,), t, at),
              _dense("b", b, (d,), t, at), dtype, n, d, eps, int(rms), _dense("out", out, shape, t, at))
 
 
 def norm_backward_workspace_size(n_rows: int, d: int) -> int:
+    _ints(d=d)
     return lib().dsf_norm_backward_workspace_size(n_rows, d)
 
 
@@ -687,6 +702,8 @@ def norm_backward(x, dy, w, dx, dw=None, db=None, add=None, eps: float = 1e-5, r
     """dx [..., d] (or None) = add + the adjoint of norm_forward at dy; dw, db float32 [d] or None."""
     dtype, at, shape = _dtype_code(x), x.get_device(), x.shape
     d = shape[-1] if shape else 0
+    if d >> 31:
+        _ints(d=d)
     n = x.numel() // d if d else 0
     t = x.dtype
     ptrs = [_dense("x", x, shape, t, at), _dense("dy", dy, shape, t, at), _dense("w", w, (d,), t, at),
@@ -699,6 +716,7 @@ def norm_backward(x, dy, w, dx, dw=None, db=None, add=None, eps: float = 1e-5, r
 
 
 def head_workspace_size(dtype: int, n_rows: int, d: int, n_classes: int, top: int = 0, gradients: bool = True) -> int:
+    _ints(d=d, n_classes=n_classes, top=top)
     return lib().dsf_head_workspace_size(dtype, n_rows, d, n_classes, top, int(gradients))
 
 
@@ -707,6 +725,8 @@ def _head(name: str, h, w, lists, middle, top, row_weight, row_loss, total, dh, 
     if h.dim() < 1 or w.dim() != 2:
         raise ValueError("h: [..., d], w: [n_classes, d]")
     V, d = w.shape
+    if (V | d | top) >> 31:
+        _ints(n_classes=V, d=d, top=top)
     rows = h.shape[:-1]
     n = h.numel() // d if d else 0
     t = h.dtype

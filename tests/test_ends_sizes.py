@@ -1,0 +1,48 @@
+"""Sizes of the embedding, norms and head losses that pass the integers of the C entry points are refused by the binding:
+they would arrive as their lower halves, 2^32 + 8 as 8. On tensors without memory; nothing here needs a GPU."""
+import pytest
+import torch
+
+import paper_2607_21291_amd as P
+
+BIG = (1 << 32) + 8
+SIGNED = 1 << 31
+
+
+def _meta(*shape, dtype=torch.bfloat16):
+    return torch.empty(shape, dtype=dtype, device="meta")
+
+
+@pytest.mark.parametrize("V,d", [(BIG, 8), (8, BIG), (SIGNED, 8), (8, SIGNED)])
+def test_tables_past_32_bits(V, d):
+    tok, table, rows = _meta(3, dtype=torch.int32), _meta(V, d), _meta(3, d)
+    calls = [lambda: P.embed_forward(tok, table, rows), lambda: P.embed_backward(tok, rows, table),
+             lambda: P.head_cross_entropy(rows, table, tok, row_loss=_meta(3, dtype=torch.float32)),
+             lambda: P.head_distill(rows, table, _meta(3, 2, dtype=torch.int32), _meta(3, 2, dtype=torch.float32), dh=rows)]
+    for call in calls:
+        with pytest.raises(ValueError, match="2\\^31"):
+            call()
+
+
+@pytest.mark.parametrize("d", [BIG, SIGNED])
+def test_rows_past_32_bits(d):
+    x, w = _meta(3, d), _meta(d)
+    for call in (lambda: P.norm_forward(x, w, x), lambda: P.norm_backward(x, x, w, x)):
+        with pytest.raises(ValueError, match="2\\^31"):
+            call()
+
+
+def test_lists_past_32_bits():
+    rows, table = _meta(1, 8), _meta(9, 8)
+    with pytest.raises(ValueError, match="2\\^31"):
+        P.head_distill(rows, table, _meta(1, BIG, dtype=torch.int32), _meta(1, BIG, dtype=torch.float32), dh=rows)
+
+
+@pytest.mark.parametrize("big", [BIG, SIGNED, -BIG])
+def test_workspace_sizes_past_32_bits(big):
+    for call in (lambda: P.embed_backward_workspace_size(10, big, 100), lambda: P.embed_backward_workspace_size(10, 64, big),
+                 lambda: P.norm_backward_workspace_size(10, big), lambda: P.head_workspace_size(P.BF16, 10, big, 100),
+                 lambda: P.head_workspace_size(P.BF16, 10, 64, big),
+                 lambda: P.head_workspace_size(P.BF16, 10, 64, 100, top=big)):
+        with pytest.raises(ValueError, match="2\\^31"):
+            call()
