@@ -1932,7 +1932,8 @@ extern "C" size_t dsf_head_workspace_size(int dtype, int64_t n_rows, int d, int 
 static int head_loss(const HeadLossArgs& a, int64_t n_rows, int dw_type, size_t workspace_bytes, hipStream_t stream) {
   int rc = check_grad_type("dw_type", dw_type, a.dtype);
   if (rc) return rc;
-  DSF_CHECK(std::isfinite(a.grad_scale), DSF_EINVAL, "grad_scale must be finite");
+  DSF_CHECK(std::isfinite(a.grad_scale) && std::isfinite(a.grad_scale * a.temperature), DSF_EINVAL,
+            "grad_scale must be finite, also times the temperature");
   DSF_CHECK(n_rows == 0 || (a.h && a.w && a.classes), DSF_EINVAL, "null pointer");
   DSF_CHECK(aligned16(a.h) && aligned16(a.w) && aligned16(a.dh) && aligned16(a.dw), DSF_EINVAL,
             "h, w, dh and dw must be 16-byte aligned");

@@ -46,3 +46,13 @@ def test_workspace_sizes_past_32_bits(big):
                  lambda: P.head_workspace_size(P.BF16, 10, 64, 100, top=big)):
         with pytest.raises(ValueError, match="2\\^31"):
             call()
+
+
+def test_a_gradient_scale_that_overflows_with_the_temperature_is_refused():
+    """dz is scaled by grad_scale x temperature in fp32: infinity there would make NaN of every gradient that is 0."""
+    def call(scale, T, dh):
+        at = 0x100000  # never dereferenced: refused before the device is looked for
+        return P.lib().dsf_head_distill(at, at, P.BF16, 10, 64, 100, at, at, 8, T, None, scale, 0, at, at, dh, None, P.BF16, at,
+                                        1 << 45, None)
+    for scale in (3e38, -3e38, 4e32):
+        assert call(scale, 1e6, 0x100000) == 1 and "grad_scale" in P.last_error()
