@@ -711,7 +711,7 @@ int dsf_norm_backward(const void* x, const void* dy, const void* w, const void* 
  * as many rows as fit 4 GiB (calls of more take them in pieces), a copy of the
  * rows of h that take part, three values an entry of the lists, with gradients
  * fp32 partial sums (64 MiB at least; of dh for a piece's rows as many as fit 512
- * MiB, one at least), and for calls of several pieces the sum of dw in fp32. 0 on
+ * MiB, one at least; a piece has as many rows as make that one 4 GiB at most), and for calls of several pieces the sum of dw in fp32. 0 on
  * a bad argument. */
 size_t dsf_head_workspace_size(int dtype, int64_t n_rows, int d, int n_classes, int top, int gradients);
 

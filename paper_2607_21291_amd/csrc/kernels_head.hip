@@ -594,7 +594,8 @@ struct HeadPlan {
 
 size_t up(size_t v) { return (v + 255) & ~size_t(255); }
 
-// Bytes of a piece's logits (codes), at most: a piece more is a pass over dW more (in
+// Bytes of a piece's logits (codes), and of one share of its rows' dh (which is more where classes are
+// few and rows wide), at most: a piece more is a pass over dW more (in
 // fp32, read and written), so pieces are large; 4 GiB are 14000 rows of 151936 classes.
 constexpr size_t kPieceBytes = size_t(4) << 30;
 constexpr size_t kDhPartBytes = size_t(1) << 29;
@@ -607,7 +608,8 @@ HeadPlan head_plan(int dtype, int n, int d, int V, int k, bool grads) {
   p.tiles = f32 ? (p.ldz + kStatCols - 1) / kStatCols : p.ldz / kHeadTile;
   const int64_t n256 = (int64_t(n) + 255) / 256 * 256;
   // statistics alone (bf16): no logits are kept, a piece is bounded by its statistics
-  const size_t per_row = (grads || f32) ? size_t(p.ldz) * eb : size_t(p.tiles) * sizeof(float2);
+  size_t per_row = (grads || f32) ? size_t(p.ldz) * eb : size_t(p.tiles) * sizeof(float2);
+  if (grads) per_row = std::max(per_row, size_t(d) * 4);
   const int64_t most = std::max<int64_t>(256, int64_t(kPieceBytes / per_row) / 256 * 256);
   p.pieces = int((n256 + most - 1) / most);
   p.rows = int(((n256 + p.pieces - 1) / p.pieces + 255) / 256 * 256);

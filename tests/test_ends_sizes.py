@@ -56,3 +56,12 @@ def test_a_gradient_scale_that_overflows_with_the_temperature_is_refused():
                                         1 << 45, None)
     for scale in (3e38, -3e38, 4e32):
         assert call(scale, 1e6, 0x100000) == 1 and "grad_scale" in P.last_error()
+
+
+@pytest.mark.parametrize("dtype,nbytes", [(P.F32, 4), (P.BF16, 2)])
+def test_partial_sums_bound_a_piece(dtype, nbytes):
+    """Few classes and wide rows: dh's partial sums, not the logits, are what a piece's rows are bounded by: 4 GiB of
+    each, beside the copy of the rows, dW's sum and some values a row."""
+    n, d, V = 1 << 20, 4096, 1000
+    size = P.head_workspace_size(dtype, n, d, V)
+    assert 0 < size <= n * d * nbytes + (4 << 30) + (4 << 30) + V * d * 4 + n * 64 + (1 << 20)

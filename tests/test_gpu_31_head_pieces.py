@@ -138,3 +138,35 @@ def test_one_gradient_alone(dev, dtype, n, d, V, masked, k):
     for want in (("dh",), ("dw",), ("total", "dh"), ("row_loss", "dw"), ("dh", "dw"), ("total",), ("row_loss",)):
         got = run(*want)
         assert all(torch.equal(got[x], every[x]) for x in want), want
+
+
+def test_pieces_bounded_by_partial_sums(dev):
+    """Few classes of wide rows: 65536 rows of width 16384 are 4 GiB of dh's partial sums. Logits are sums below 10 of 528
+    additions: some 1e-5 off, 1e-4 at most; dz by 1.1 of its half step, dW's own additions (n / 32, 2 u each) make it 1.2."""
+    n, d, V = 66000, 16384, 6
+    g = torch.Generator(device=dev).manual_seed(3)
+    h = torch.randn(n, d, device=dev, dtype=torch.bfloat16, generator=g)
+    w = (torch.randn(V, d, device=dev, generator=g) * (2.5 / d ** 0.5)).bfloat16()
+    t = torch.randint(-1, V, (n,), device=dev, dtype=torch.int32, generator=g)
+    assert P.head_workspace_size(P.BF16, n, d, V) < n * d * 2 + (5 << 30)
+    loss, total, dh, dw = (torch.empty(x, device=dev, dtype=y) for x, y in (
+        (n, torch.float32), (2, torch.float32), ((n, d), torch.bfloat16), ((V, d), torch.float32)))
+    announce("pieces bounded by partial sums")
+    P.head_cross_entropy(h, w, t, row_loss=loss, total=total, dh=dh, dw=dw, mean=True)
+    W, e = w.double(), 1.2 * HALF["bf16"]
+    want_dw, size_dw = torch.zeros_like(W), torch.zeros_like(W)
+    live = t >= 0
+    scale, sum_loss = 1.0 / float(live.sum()), 0.0
+    for a in range(0, n, 4096):
+        H, tt, ok = h[a:a + 4096].double(), t[a:a + 4096].long(), live[a:a + 4096]
+        logp = torch.log_softmax(H @ W.t(), 1)
+        want = -logp.gather(1, tt.clamp(min=0)[:, None])[:, 0] * ok
+        assert (loss[a:a + 4096].double() - want).abs().max() <= 1e-4
+        sum_loss += float(want.sum())
+        dz = logp.exp().scatter_add_(1, tt.clamp(min=0)[:, None], -torch.ones_like(logp[:, :1])) * ok[:, None]
+        want, size = scale * (dz @ W), scale * (dz.abs() @ W.abs())
+        assert ((dh[a:a + 4096].double() - want).abs() <= e * size + 1.01 * HALF["bf16"] * want.abs() + 1e-30).all()
+        want_dw += scale * (dz.t() @ H)
+        size_dw += scale * (dz.abs().t() @ H.abs())
+    assert ((dw.double() - want_dw).abs() <= e * size_dw).all()
+    assert abs(float(total[0]) - sum_loss) <= 1e-4 * n and float(total[1]) == float(live.sum())
