@@ -594,9 +594,9 @@ struct HeadPlan {
 
 size_t up(size_t v) { return (v + 255) & ~size_t(255); }
 
-// Bytes of a piece's logits (codes), and of one share of its rows' dh (which is more where classes are
-// few and rows wide), at most: a piece more is a pass over dW more (in
-// fp32, read and written), so pieces are large; 4 GiB are 14000 rows of 151936 classes.
+// Bytes of a piece's logits (codes), and of one share of its rows' dh (which is more where
+// classes are few and rows wide), at most: a piece more is a pass over dW more (in fp32, read
+// and written), so pieces are large; 4 GiB are 14000 rows of 151936 classes.
 constexpr size_t kPieceBytes = size_t(4) << 30;
 constexpr size_t kDhPartBytes = size_t(1) << 29;
 
@@ -652,8 +652,11 @@ HeadPlan head_plan(int dtype, int n, int d, int V, int k, bool grads) {
 }
 }  // namespace
 
+// (for gradients: also enough without, where a piece has more rows: of 15 M rows over 700000
+// classes their statistics are 1 % more than the logits of a piece with gradients)
 size_t head_workspace_bytes(int dtype, int n, int d, int V, int k, bool grads) {
-  return head_plan(dtype, n, d, V, k, grads).total;
+  const size_t alone = head_plan(dtype, n, d, V, k, false).total;
+  return grads ? std::max(alone, head_plan(dtype, n, d, V, k, true).total) : alone;
 }
 
 hipError_t launch_head_loss(const HeadLossArgs& a, hipStream_t s) {

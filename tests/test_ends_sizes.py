@@ -65,3 +65,13 @@ def test_partial_sums_bound_a_piece(dtype, nbytes):
     n, d, V = 1 << 20, 4096, 1000
     size = P.head_workspace_size(dtype, n, d, V)
     assert 0 < size <= n * d * nbytes + (4 << 30) + (4 << 30) + V * d * 4 + n * 64 + (1 << 20)
+
+
+def test_workspaces_for_gradients_do_for_losses_alone():
+    g = torch.Generator().manual_seed(0)
+    log = lambda lo, hi: int(lo * (hi / lo) ** float(torch.rand((), generator=g)))  # noqa: E731
+    for _ in range(3000):
+        n, d, V, top = log(1, 1 << 24), 8 * log(1, 2048), log(1, 1 << 21), log(1, 1025) - 1
+        for dtype in (P.F32, P.BF16):
+            alone, every = (P.head_workspace_size(dtype, n, d, V, top=top, gradients=x) for x in (False, True))
+            assert 0 < alone <= every, (dtype, n, d, V, top)
