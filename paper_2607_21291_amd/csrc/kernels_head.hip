@@ -612,6 +612,7 @@ HeadPlan head_plan(int dtype, int n, int d, int V, int k, bool grads) {
   if (grads) per_row = std::max(per_row, size_t(d) * 4);
   const int64_t most = std::max<int64_t>(256, int64_t(kPieceBytes / per_row) / 256 * 256);
   p.pieces = int((n256 + most - 1) / most);
+  // (rows <= most, so that the pieces before the last leave it at least one row)
   p.rows = int(((n256 + p.pieces - 1) / p.pieces + 255) / 256 * 256);
   // shares of the classes for dh, at most
   const int64_t fit = int64_t(kDhPartBytes / (size_t(p.rows) * d * 4));
@@ -696,12 +697,12 @@ hipError_t launch_head_loss(const HeadLossArgs& a, hipStream_t s) {
     head_gather_kernel<<<wide_grid((int64_t(a.n) * k + kDots - 1) / kDots), 64, 0, s>>>(
         (const uint16_t*)a.h, (const uint16_t*)a.w, a.classes, k, a.V, a.d, act, n_active, (uint16_t*)(ws + p.hc), z2);
   DSF_TRY(hipGetLastError());
-  const int lse_wgs = (p.rows + kLseRows - 1) / kLseRows;
+  const int lse_wgs = p.rows / kLseRows, last_rows = a.n - (p.pieces - 1) * p.rows;
+  const int workgroups = (p.pieces - 1) * lse_wgs + (last_rows + kLseRows - 1) / kLseRows;
   for (int i = 0; i < p.pieces; ++i) {
     HeadGemmArgs g{};
     g.row0 = i * p.rows;
     g.rows = std::min(p.rows, a.n - g.row0);
-    if (g.rows <= 0) break;  // (the last piece may be rounded away)
     g.rows_ld = p.rows;
     g.h = ws + p.hc + size_t(g.row0) * a.d * (f32 ? 4 : 2);
     g.w = a.w;
@@ -749,9 +750,7 @@ hipError_t launch_head_loss(const HeadLossArgs& a, hipStream_t s) {
     l.rows = g.rows;
     l.k = k;
     l.first = i * lse_wgs;
-    l.workgroups = 0;
-    for (int b = 0; b < p.pieces; ++b)
-      l.workgroups += (std::max(0, std::min(p.rows, a.n - b * p.rows)) + kLseRows - 1) / kLseRows;
+    l.workgroups = workgroups;
     l.T = a.temperature;
     head_lse_kernel<<<(g.rows + kLseRows - 1) / kLseRows, 1024, 0, s>>>(l);
     DSF_TRY(hipGetLastError());
@@ -793,7 +792,7 @@ hipError_t launch_head_loss(const HeadLossArgs& a, hipStream_t s) {
       DSF_TRY(hipGetLastError());
     }
     if (a.dw) {
-      const bool last = i + 1 == p.pieces || (i + 1) * p.rows >= a.n;
+      const bool last = i + 1 == p.pieces;
       float* sum = a.dw_f32 ? (float*)a.dw : (float*)(ws + p.acc);
       g.prev = i > 0 ? sum : nullptr;
       g.out32 = a.dw_f32 || !last ? sum : nullptr;
