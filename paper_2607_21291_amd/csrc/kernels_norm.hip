@@ -257,14 +257,15 @@ __global__ __launch_bounds__(1024) void norm_grad_sums_kernel(const float* __res
 }
 
 namespace {
-// vectors a lane of four waves to a row, by the row's 16-byte vectors
-template <typename F>
+// vectors a lane of four waves to a row, by the row's 16-byte vectors (sixteen: fp32 alone,
+// the widest rows of bf16 have 2048)
+template <typename T, typename F>
 void norm_shape(int nv, F f) {
   if (nv <= 256) f(std::integral_constant<int, 1>());
   else if (nv <= 512) f(std::integral_constant<int, 2>());
   else if (nv <= 1024) f(std::integral_constant<int, 4>());
-  else if (nv <= 2048) f(std::integral_constant<int, 8>());
-  else f(std::integral_constant<int, 16>());
+  else if (sizeof(T) == 2 || nv <= 2048) f(std::integral_constant<int, 8>());
+  else if constexpr (sizeof(T) == 4) f(std::integral_constant<int, 16>());
 }
 }  // namespace
 
@@ -286,7 +287,7 @@ hipError_t launch_norm_rows(int dtype, bool rms, const void* x, const void* w, c
     using One = std::integral_constant<int, 1>;
     if (n >= 2048 && nv <= 64) go(One(), One());
     else if (n >= 2048 && nv <= 128) go(std::integral_constant<int, 2>(), One());
-    else norm_shape(nv, [&](auto Cc) { go(Cc, std::integral_constant<int, 4>()); });
+    else norm_shape<T>(nv, [&](auto Cc) { go(Cc, std::integral_constant<int, 4>()); });
   };
   if (dtype == DSF_F32) run(float());
   else run(uint16_t());
@@ -303,7 +304,7 @@ hipError_t launch_norm_backward(const NormBackwardArgs& a, hipStream_t s) {
     using T = decltype(Tz);
     // (a workgroup to a row also where rows are narrow: a wave to each leaves four times the partial
     // sums, 4096 rows of width 768 14.1 -> 27.3 us, 16384 29.4 -> 35.0)
-    norm_shape(a.d / Elem<T>::kVec, [&](auto Cc) {
+    norm_shape<T>(a.d / Elem<T>::kVec, [&](auto Cc) {
       constexpr int C = decltype(Cc)::value;
       // two rows or more for each partial sum once every CU has a workgroup (1024 rows of width 3584 on 1024
       // workgroups 16.9 us, on 512 13.1); up to 1024 (16384 rows: on 512 125 us, 1024 91, 2048 97)
