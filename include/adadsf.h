@@ -754,7 +754,8 @@ int dsf_head_cross_entropy(const void* h, const void* w, int dtype, int64_t n_ro
  * the outputs and the other arguments are dsf_head_cross_entropy's.
  * top_classes int32, top_logits float, [n_rows, top], top from 1 to 1024;
  * temperature from 1e-6 to 1e6, times grad_scale finite in fp32 (a loss, a
- * difference of terms in fp32, is off by some 1e-6 temperature^2). */
+ * difference of terms in fp32, is off by some 1e-6 temperature^2, and by its
+ * logits' errors, some 1e-6 of themselves, times temperature). */
 int dsf_head_distill(const void* h, const void* w, int dtype, int64_t n_rows, int d, int n_classes,
                      const int32_t* top_classes, const float* top_logits, int top, float temperature,
                      const float* row_weight, float grad_scale, int mean, float* row_loss, float* total, void* dh,

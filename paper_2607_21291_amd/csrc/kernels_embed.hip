@@ -10,8 +10,9 @@
 //
 // Memory bounds both. Lookup: 20000 rows of width 2048 21 us, 7.6 TB/s with what the
 // caches hold of common rows. Gradient: 16384 positions, table 151936 x 896, bf16: sort
-// and zero rows 49 us (245 MB, 5.0 TB/s), sums 17, join 5; of 6001 positions added to
-// a table of 50304 x 768 in fp32 20 us, three chains of dependent loads.
+// and zero rows 50 us (245 MB, 4.9 TB/s), sums 15, join 5; of 6001 positions added to
+// a table of 50304 x 768 in fp32 20 us, three chains of dependent loads; 40000 positions
+// of one token 221 us, 115 of them the join (a wave to 512 columns).
 #include <algorithm>
 
 #include "dsf_device.h"

@@ -11,7 +11,7 @@
 // too) has no effect.
 //
 // A row that is sure of its target has z = lse but for e^-z: both have to come from the
-// same sums, or the loss and p - 1 are a logit's rounding (6e-5 at 45 and width 3584).
+// same sums, or the loss and p - 1 are a logit's rounding (1e-4 at 45 and width 3584).
 // z at the targets is the product's own, bit by bit (bf16: the same matrix
 // instructions in the same order; fp32: read back), and lse stays in two terms, the
 // greatest logit and log2 of the sum relative to it: z - maximum is taken first.

@@ -22,7 +22,9 @@
 // (1.25-1.35 PFLOP/s), at the card's power limit: the clock falls to 1.8 GHz, of
 // which the matrix cores are busy 63-68 %. Width 768 over 50304: 740, 590, 540 us, the
 // logits' epilogue (two reductions over the tile's rows, an exponential and a code a logit)
-// being a quarter of theirs: accumulators fill the registers, so it stands alone.
+// being a quarter of theirs: accumulators fill the registers, so it stands alone. (Logits spill
+// 6 registers, dW of half-full tiles 7, between the products' loops and a few times a tile;
+// none in a loop over k.)
 #include <algorithm>
 #include <type_traits>
 
