@@ -708,11 +708,12 @@ int dsf_norm_backward(const void* x, const void* dy, const void* w, const void* 
 /* Workspace bytes of the head's losses: top = 0 for dsf_head_cross_entropy, the
  * entries of a row for dsf_head_distill; gradients != 0 if dh or dw are wanted
  * (also enough for calls without). It holds 16 bits (fp32: 32) for each logit of
- * as many rows as fit 4 GiB (calls of more take them in pieces), a copy of the
- * rows of h that take part, three values an entry of the lists, with gradients
- * fp32 partial sums (64 MiB at least; of dh for a piece's rows as many as fit 512
- * MiB, one at least; a piece has as many rows as make that one 4 GiB at most), and for calls of several pieces the sum of dw in fp32. 0 on
- * a bad argument. */
+ * as many rows as fit 4 GiB (calls of more take them in pieces; bf16 losses alone:
+ * 8 bytes for 256 logits), a copy of the rows of h that take part, three values an
+ * entry of the lists, with gradients fp32 partial sums (64 MiB at least; of dh for
+ * a piece's rows as many as fit 512 MiB, one at least, and no piece has rows for
+ * more than 4 GiB of one), and for calls of several pieces the sum of dw in fp32. 0
+ * on a bad argument. */
 size_t dsf_head_workspace_size(int dtype, int64_t n_rows, int d, int n_classes, int top, int gradients);
 
 /* Cross entropy of a linear head. For rows h[i] and logits z_i = h[i] W^T over
